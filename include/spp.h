@@ -8,6 +8,8 @@
  *                         (Sec. 2.3; steps (i)-(iii) of the random process of Sec. 3.1)
  *   spp_gather_features   cache-aware feature gather: local shard / replica cache / remote
  *                         rows on a miss (Secs. 4.1-4.3; stages 5-10 of Appendix D)
+ *   spp_mx4_*, spp_adamw_*  feature rows in 4 bits, the layer that reads them, its weight gradient and the
+ *                         optimiser's step: what a training loop does next with the gathered rows
  *
  * Conventions
  *   G        directed graph in CSR on the device: rowptr int64[N+1], col int32[M].  Row v,
@@ -44,6 +46,11 @@ extern "C" {
 #define SPP_MAX_GATHER_LISTS 64 /* most id lists in one spp_gather_features_multi call */
 #define SPP_MAX_SAMPLE_BATCHES 64 /* most minibatches in one spp_sample_mfg_multi call */
 #define SPP_STATIC_GATHER_MAX_ROWS 131072 /* most ids in one spp_gather_features_static call */
+#define SPP_MAX_ROW_LISTS 64   /* most lists, and most weight matrices, in one spp_mx4_product or spp_mx4_weight_grad call */
+#define SPP_MX4_MAX_COLS 4096  /* most columns of a row in MXFP4 */
+#define SPP_MAX_HIDDEN 65536   /* most columns of a product */
+#define SPP_ADAMW_BLOCK 256    /* elements whose 8-bit moments share a scale */
+#define SPP_ADAMW_MAX_ELEMENTS 17179869184 /* most elements of one tensor of spp_adamw_step: 2^34 */
 
 enum {
     SPP_OK          =  0,
@@ -348,13 +355,91 @@ typedef struct {
 int  spp_access_count(spp_ctx* ctx, const spp_id_list* lists, int32_t n_lists, int64_t N, float* d_count,
                       uint32_t flags);
 
+/* Operators on gathered rows: feature rows in 4 bits, the layer that reads them, its gradient and the optimiser's step.
+ *
+ * Element types of the arrays below. */
+enum { SPP_F32 = 0, SPP_F16 = 1, SPP_BF16 = 2 };
+
+/* (5) Rows in MXFP4.  A row of D columns (1 .. SPP_MX4_MAX_COLS) is nb = ceil(D/32) blocks of 32 columns, the last one filled up
+ *     with zeros.  With a = max |x| of a block and e = max(floor(log2 a) - 2, -127) its columns are held as the nearest of
+ *     0, 0.5, 1, 1.5, 2, 3, 4, 6 to |x| / 2^e, ties to the one of even code, 6 for what lies above, and a sign (E2M1); its
+ *     scale is the byte e + 127 (E8M0).  A block that holds a NaN or an infinity has scale byte 255 and reads as NaN.
+ *     Bytes of a row: the codes, 16 per block (column 2j of a block in the low half of its byte j), then nb scale bytes, then
+ *     zeros up to spp_mx4_row_bytes(D) = 17*nb rounded up to a multiple of 16.  A row is one piece of bytes, so that
+ *     the gather, the cache and the local store take it as rows of that many 1-byte elements.
+ *     d_x: n rows of D elements of `type`, ld >= D elements from a row to the next, aligned to the type (16-byte aligned
+ *     rows are read 16 bytes at a time).  d_rows: 16-byte aligned.  n at most 2^31 - 1, or an upper bound when d_n (device
+ *     int64) is given; rows from *d_n on are neither read nor written.  D out of range gives SPP_E_ARG, row_bytes too. */
+int64_t spp_mx4_row_bytes(int32_t D);
+int  spp_mx4_quantize(spp_ctx* ctx, const void* d_x, int32_t type, int64_t n, const int64_t* d_n, int32_t D, int64_t ld,
+                      void* d_rows, uint32_t flags);
+/*     The values that rows stand for, rounded to `type` (to nearest, ties to even). */
+int  spp_mx4_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64_t* d_n, int32_t D, void* d_x, int32_t type,
+                        int64_t ld, uint32_t flags);
+
+/* (6) The layer that reads such rows, over up to SPP_MAX_ROW_LISTS lists of rows in one launch (e.g. the minibatches that a
+ *     pipeline keeps in flight, each counted on the device by the sampler; or rows of several kinds, each kind a group):
+ *       product      Y_j[i,:] = sum_d X_j[i,d] W[g_j][:,d]     d_weights: n_groups matrices of H rows in MXFP4 of D columns,
+ *                                                              one behind the other; Y of `type`, written
+ *       weight grad  dW[g]    = sum over the lists j of group g of Y_j^T X_j     Y of `type`, read; d_grad fp32 [n_groups, H, D],
+ *                                                              written (a group without rows: zeros)
+ *     X and W are the values that the packed rows stand for; sums are formed in fp32 and rounded once to Y's type.  The
+ *     gradient is that of the product by W's values; the rows are data and have none.  It adds in an order that the lists'
+ *     lengths alone decide, so a call repeated gives the same bits; it keeps at most 64 MiB plus one matrix per group and
+ *     one more of device memory with the context.
+ *     d_rows 16-byte aligned; Y aligned to its type, ld >= H elements from a row to the next (16-byte aligned rows take
+ *     the wide path).  Rows from *d_n on are neither read nor written, whatever they hold.  H is 1 .. SPP_MAX_HIDDEN. */
+typedef struct {
+    const void*    d_rows;   /* [n, spp_mx4_row_bytes(D)] */
+    int64_t        n;        /* rows, or an upper bound when d_n is given; at most 2^31 - 1 */
+    const int64_t* d_n;      /* device int64 count, or NULL */
+    void*          d_y;      /* [n, H], row stride ld */
+    int64_t        ld;
+    int32_t        group;    /* which matrix, 0 .. n_groups - 1 */
+} spp_row_list;
+int  spp_mx4_product(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
+                     int32_t D, int32_t H, int32_t type, uint32_t flags);
+int  spp_mx4_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H,
+                         int32_t type, float* d_grad, uint32_t flags);
+
+/* (7) One AdamW step over any number of tensors (contiguous, n elements each), moments in 32 or 8 bits:
+ *       m' = b1 m + (1-b1) g      v' = b2 v + (1-b2) g^2
+ *       p' = (1 - lr wd) p - lr/(1-b1^t) * m' / (sqrt(v') / sqrt(1-b2^t) + eps)          t = 1 at the first step
+ *     computed in fp32.  An element whose v' would not be finite (its gradient is not, or its square is not) keeps p, m and v;
+ *     such elements are counted (spp_ctx_totals, out[9]).  p: SPP_F32 or SPP_BF16 (rounded to nearest, ties to even); g any type.
+ *     state_bits 32: d_m and d_v are fp32[n], zero before the first step.
+ *     state_bits 8:  d_m and d_v are uint8[n], d_scale fp32[2 * ceil(n / SPP_ADAMW_BLOCK)], all zero before the first step.
+ *       Each run of SPP_ADAMW_BLOCK elements has two scales, for m and for sqrt(v), such that the largest of the run is the
+ *       largest code; a code c of sqrt(v) stands for scale * 2^(c/16 - 15) * (1 + (c mod 16)/16), 0 for 0; of m likewise with
+ *       (c & 127), 8 in the place of 16, and the sign in bit 7.  Rounded to the nearest code, ties to even; a v above zero keeps at
+ *       least code 1.  The step itself uses the moments before this rounding.
+ *     spp_adamw_load sets the 8-bit moments from fp32 arrays (host arrays of device pointers; what is not finite, or a negative v,
+ *     counts as 0); spp_adamw_values gives the values that they stand for.  Both ignore d_p, d_g and their types. */
+typedef struct {
+    void*       d_p;
+    const void* d_g;
+    void*       d_m;
+    void*       d_v;
+    float*      d_scale;
+    int64_t     n;           /* at most SPP_ADAMW_MAX_ELEMENTS */
+    int32_t     p_type, g_type;
+} spp_adamw_tensor;
+typedef struct { double lr, beta1, beta2, eps, weight_decay; } spp_adamw_hyper;
+int  spp_adamw_step(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits,
+                    const spp_adamw_hyper* hyper, int64_t t, uint32_t flags);
+int  spp_adamw_load(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, const float* const* d_m,
+                    const float* const* d_v, uint32_t flags);
+int  spp_adamw_values(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, float* const* d_m, float* const* d_v,
+                      uint32_t flags);
+
 /* Device-time accounting.  After spp_ctx_timing(ctx, 1) every call brackets its pieces of device
  * work with events on the stream they run on (vip total and per hop, the whole sampling of a
  * batch, gather classify / hit copy / miss copy).  spp_ctx_times waits for the context's streams,
  * returns for each SPP_T_* index the summed duration in milliseconds and the number of pieces
  * since the last call, and starts a new accumulation.  spp_ctx_timing(ctx, 0) stops recording. */
 enum { SPP_T_VIP_TOTAL = 0, SPP_T_VIP_HOP_FIRST = 1 /* .. +L-1 */, SPP_T_SAMPLE = 9,
-       SPP_T_GATHER_HIT = 10, SPP_T_GATHER_MISS = 11, SPP_T_GATHER_CLASSIFY = 12, SPP_T_COUNT = 16 };
+       SPP_T_GATHER_HIT = 10, SPP_T_GATHER_MISS = 11, SPP_T_GATHER_CLASSIFY = 12,
+       SPP_T_MX4 = 13 /* quantise, dequantise */, SPP_T_LAYER = 14 /* product, weight gradient */, SPP_T_ADAMW = 15, SPP_T_COUNT = 16 };
 int  spp_ctx_timing(spp_ctx* ctx, int enable);
 int  spp_ctx_times(spp_ctx* ctx, float* sum_ms /* [SPP_T_COUNT] */, int64_t* count /* [SPP_T_COUNT] */);
 /*     The same with the shortest and the median piece per index (0 where there was none); any of the
@@ -376,7 +461,8 @@ int  spp_stream_rates(spp_ctx* ctx, const void* d_a, void* d_b, int64_t bytes, i
  *   out[3] gather calls, out[4] rows from the local shard, out[5] rows from the cache,
  *   out[6] rows missed (neither local nor cached), out[7] local rows read from host memory,
  *   out[8] missed rows served by a copy of another row of the same call (n_miss_shared),
- *   out[9..15] unused.
+ *   out[9] elements that spp_adamw_step left as they were,
+ *   out[10..15] unused.
  * Waits for the context's streams. */
 int  spp_ctx_totals(spp_ctx* ctx, int64_t* out /* [16] */, int reset);
 

@@ -32,6 +32,12 @@ SPP_SAMPLE_GLOBAL_TABLE = 0x40
 SPP_STATIC_GATHER_MAX_ROWS = 131072
 SPP_T_VIP_TOTAL, SPP_T_VIP_HOP_FIRST, SPP_T_SAMPLE = 0, 1, 9
 SPP_T_GATHER_HIT, SPP_T_GATHER_MISS, SPP_T_GATHER_CLASSIFY, SPP_T_COUNT = 10, 11, 12, 16
+SPP_T_MX4, SPP_T_LAYER, SPP_T_ADAMW = 13, 14, 15
+SPP_MAX_ROW_LISTS = 64
+SPP_MX4_MAX_COLS = 4096
+SPP_MAX_HIDDEN = 65536
+SPP_ADAMW_BLOCK = 256
+SPP_F32, SPP_F16, SPP_BF16 = 0, 1, 2
 
 EXPORTS = [
     "spp_last_error", "spp_ctx_create", "spp_ctx_destroy", "spp_ctx_sync", "spp_graph_create",
@@ -41,6 +47,8 @@ EXPORTS = [
     "spp_build_local_store", "spp_local_store_destroy", "spp_local_store_set_limit", "spp_local_store_rank",
     "spp_gather_features_split", "spp_access_count", "spp_vip_propagate_general", "spp_sample_mfg_general",
     "spp_stream_rates", "spp_gather_features_static",
+    "spp_mx4_row_bytes", "spp_mx4_quantize", "spp_mx4_dequantize", "spp_mx4_product", "spp_mx4_weight_grad",
+    "spp_adamw_step", "spp_adamw_load", "spp_adamw_values",
 ]
 
 
@@ -72,6 +80,20 @@ class _GatherList(C.Structure):
 
 class _IdList(C.Structure):
     _fields_ = [("d_ids", C.c_void_p), ("n", C.c_int64), ("d_n", C.c_void_p)]
+
+
+class _RowList(C.Structure):
+    _fields_ = [("d_rows", C.c_void_p), ("n", C.c_int64), ("d_n", C.c_void_p), ("d_y", C.c_void_p), ("ld", C.c_int64),
+                ("group", C.c_int32)]
+
+
+class _AdamwTensor(C.Structure):
+    _fields_ = [("d_p", C.c_void_p), ("d_g", C.c_void_p), ("d_m", C.c_void_p), ("d_v", C.c_void_p), ("d_scale", C.c_void_p),
+                ("n", C.c_int64), ("p_type", C.c_int32), ("g_type", C.c_int32)]
+
+
+class _AdamwHyper(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double)]
 
 
 class _GatherStats(C.Structure):
@@ -149,6 +171,21 @@ def load_library():
                                        C.POINTER(C.c_float)]
     lib.spp_ctx_totals.argtypes = [C.c_void_p, C.POINTER(C.c_int64), C.c_int]
     lib.spp_stream_rates.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.POINTER(C.c_float)]
+    lib.spp_mx4_row_bytes.argtypes = [C.c_int32]
+    lib.spp_mx4_row_bytes.restype = C.c_int64
+    lib.spp_mx4_quantize.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p,
+                                     C.c_uint32]
+    lib.spp_mx4_dequantize.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64,
+                                       C.c_uint32]
+    lib.spp_mx4_product.argtypes = [C.c_void_p, C.POINTER(_RowList), C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                                    C.c_int32, C.c_uint32]
+    lib.spp_mx4_weight_grad.argtypes = [C.c_void_p, C.POINTER(_RowList), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                        C.c_void_p, C.c_uint32]
+    lib.spp_adamw_step.argtypes = [C.c_void_p, C.POINTER(_AdamwTensor), C.c_int32, C.c_int32, C.POINTER(_AdamwHyper), C.c_int64,
+                                   C.c_uint32]
+    lib.spp_adamw_load.argtypes = [C.c_void_p, C.POINTER(_AdamwTensor), C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
+                                   C.c_uint32]
+    lib.spp_adamw_values.argtypes = lib.spp_adamw_load.argtypes
     _lib = lib
     return lib
 
@@ -694,3 +731,265 @@ def gather_last_stats(ctx: Context):
     st = _GatherStats()
     _check(load_library().spp_gather_last_stats(ctx._h, C.byref(st)))
     return _stats_dict(st)
+
+
+# ---- operators on gathered rows ------------------------------------------------------------------
+
+_TYPES = {torch.float32: SPP_F32, torch.float16: SPP_F16, torch.bfloat16: SPP_BF16}
+
+
+def _type(dtype, name: str) -> int:
+    if dtype not in _TYPES:
+        raise SppError(f"{name} must be float32, float16 or bfloat16")
+    return _TYPES[dtype]
+
+
+def _new(ctx: Context, shape, dtype) -> torch.Tensor:
+    """Memory of the context's stream, which is where it is written (torch's allocator goes by the stream)."""
+    with torch.cuda.stream(ctx.stream):
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", ctx.device))
+
+
+def _matrix(t: torch.Tensor, cols: Optional[int], name: str) -> torch.Tensor:
+    if not (t.is_cuda and t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
+        raise SppError(f"{name} must be a 2-D tensor on the GPU whose rows are contiguous")
+    if cols is not None and t.shape[1] != cols:
+        raise SppError(f"{name} must have {cols} columns, not {t.shape[1]}")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _packed(t: torch.Tensor, D: int, name: str) -> torch.Tensor:
+    rb = mx4_row_bytes(D)
+    if not (t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.dim() >= 2 and t.shape[-1] == rb):
+        raise SppError(f"{name} must be a contiguous uint8 tensor on the GPU with rows of {rb} bytes")
+    return t
+
+
+def _count(t: Optional[torch.Tensor], name: str = "n_device"):
+    if t is not None and not (t.is_cuda and t.dtype == torch.int64 and t.numel() == 1):
+        raise SppError(f"{name} must be one int64 on the GPU")
+    return t
+
+
+def mx4_row_bytes(D: int) -> int:
+    """Bytes of a row of D columns in MXFP4: 17 per block of 32 columns, rounded up to a multiple of 16."""
+    rb = load_library().spp_mx4_row_bytes(int(D))
+    if rb < 0:
+        _check(int(rb))
+    return int(rb)
+
+
+def mx4_quantize(ctx: Context, x: torch.Tensor, out: Optional[torch.Tensor] = None, n_device: Optional[torch.Tensor] = None,
+                 sync: bool = True) -> torch.Tensor:
+    """Rows [n, D] (float32, float16 or bfloat16, rows may be apart) in MXFP4: uint8 [n, mx4_row_bytes(D)].
+
+    The result is one piece of bytes per row: a row store of the gather, the cache and the local store like any other.
+    With n_device (one int64 on the GPU) only that many rows are read and written.
+    """
+    _matrix(x, None, "x")
+    ty = _type(x.dtype, "x")
+    n, D = x.shape
+    rb = mx4_row_bytes(D)
+    if out is None:
+        out = _new(ctx, (n, rb), torch.uint8)
+    elif _packed(out, D, "out").dim() != 2 or out.shape[0] < n:
+        raise SppError("out is too small")
+    _check(load_library().spp_mx4_quantize(ctx._h, _ptr(x), ty, n, _ptr(_count(n_device)), D, _ld(x), _ptr(out), SPP_SYNC if sync else 0))
+    return out
+
+
+def mx4_dequantize(ctx: Context, rows: torch.Tensor, D: int, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                   n_device: Optional[torch.Tensor] = None, sync: bool = True) -> torch.Tensor:
+    """The values [n, D] that packed rows stand for, as `dtype` (or the type of `out`)."""
+    if _packed(rows, D, "rows").dim() != 2:
+        raise SppError("rows must be a 2-D tensor")
+    n = rows.shape[0]
+    if out is None:
+        _type(dtype, "dtype")
+        out = _new(ctx, (n, D), dtype)
+    elif _matrix(out, D, "out").shape[0] < n:
+        raise SppError("out is too small")
+    _check(load_library().spp_mx4_dequantize(ctx._h, _ptr(rows), n, _ptr(_count(n_device)), D, _ptr(out), _type(out.dtype, "out"), _ld(out),
+                                             SPP_SYNC if sync else 0))
+    return out
+
+
+class RowLists:
+    """Lists of packed rows, each with a matrix Y: what the product and its gradient go over.
+
+    `lists` is a sequence of (rows, n, n_device or None, y[, group]): rows uint8 [>= n, row bytes], y [>= n, H] (rows may be
+    apart), group the index of the list's weight matrix.  Checked and marshalled once; a program that keeps its buffers keeps
+    this, and the tensors live as long as it does.
+    """
+
+    def __init__(self, lists):
+        self.lists = list(lists)
+        if len(self.lists) > SPP_MAX_ROW_LISTS:
+            raise SppError(f"{len(self.lists)} lists: at most {SPP_MAX_ROW_LISTS}")
+        self._arr = (_RowList * max(len(self.lists), 1))()
+        self.row_bytes = self.H = self.dtype = None
+        self.groups = 0
+        for j, item in enumerate(self.lists):
+            rows, n, n_dev, y = item[:4]
+            group = int(item[4]) if len(item) > 4 else 0
+            if not (rows.is_cuda and rows.dtype == torch.uint8 and rows.dim() == 2 and rows.is_contiguous()):
+                raise SppError(f"rows of list {j} must be a contiguous 2-D uint8 tensor on the GPU")
+            _matrix(y, None, f"y of list {j}")
+            _type(y.dtype, f"y of list {j}")
+            if j == 0:
+                self.row_bytes, self.H, self.dtype = rows.shape[1], y.shape[1], y.dtype
+            if rows.shape[1] != self.row_bytes or y.shape[1] != self.H or y.dtype != self.dtype:
+                raise SppError(f"list {j} has rows, columns or a type unlike list 0")
+            if not 0 <= int(n) <= min(rows.shape[0], y.shape[0]):
+                raise SppError(f"list {j}: n exceeds its rows or its y")
+            if group < 0:
+                raise SppError(f"list {j}: group {group}")
+            _count(n_dev, f"n_device of list {j}")
+            a = self._arr[j]
+            a.d_rows, a.n, a.d_n, a.d_y = rows.data_ptr(), int(n), n_dev.data_ptr() if n_dev is not None else None, y.data_ptr()
+            a.ld, a.group = _ld(y), group
+            self.groups = max(self.groups, group + 1)
+
+    def _fit(self, D: int, H: int, groups: int):
+        if self.lists and (self.row_bytes != mx4_row_bytes(D) or self.H != H):
+            raise SppError(f"the lists are not of {D} columns and {H} outputs")
+        if self.groups > groups:
+            raise SppError(f"a list names group {self.groups - 1} of {groups}")
+
+
+def mx4_product_multi(ctx: Context, lists, weights: torch.Tensor, D: int, sync: bool = True):
+    """Y_j = X_j W[group_j]^T for every list, in one launch; `lists` is a RowLists or what makes one.
+
+    weights: uint8 [groups, H, row bytes] or [H, row bytes], MXFP4 rows of D columns (mx4_quantize of a matrix [H, D]).
+    """
+    lists = lists if isinstance(lists, RowLists) else RowLists(lists)
+    _packed(weights, D, "weights")
+    if weights.dim() not in (2, 3):
+        raise SppError("weights must be [H, row bytes] or [groups, H, row bytes]")
+    groups, H = (1, weights.shape[0]) if weights.dim() == 2 else weights.shape[:2]
+    lists._fit(D, H, groups)
+    if lists.lists:
+        _check(load_library().spp_mx4_product(ctx._h, lists._arr, len(lists.lists), _ptr(weights), groups, D, H, _TYPES[lists.dtype],
+                                              SPP_SYNC if sync else 0))
+    elif sync:
+        ctx.sync()
+
+
+def mx4_product(ctx: Context, rows: torch.Tensor, weight: torch.Tensor, D: int, n: Optional[int] = None,
+                n_device: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                sync: bool = True) -> torch.Tensor:
+    """Y [n, H] = X W^T of one list of rows and one weight matrix [H, row bytes]."""
+    if weight.dim() != 2:
+        raise SppError("weight must be [H, row bytes]")
+    n = int(rows.shape[0] if n is None else n)
+    if out is None:
+        _type(dtype, "dtype")
+        out = _new(ctx, (n, weight.shape[0]), dtype)
+    mx4_product_multi(ctx, [(rows, n, n_device, out)], weight, D, sync=sync)
+    return out
+
+
+def mx4_weight_grad(ctx: Context, lists, H: int, D: int, groups: int = 1, out: Optional[torch.Tensor] = None,
+                    sync: bool = True) -> torch.Tensor:
+    """float32 [groups, H, D]: for every group the sum of Y_j^T X_j over its lists, Y_j being the product's gradient.
+
+    Zeros for a group without rows.  The same lengths give the same bits.
+    """
+    lists = lists if isinstance(lists, RowLists) else RowLists(lists)
+    lists._fit(D, H, groups)
+    if out is None:
+        out = _new(ctx, (groups, H, D), torch.float32)
+    elif _dev(out, torch.float32, "out").numel() != groups * H * D:
+        raise SppError("out must hold groups * H * D values")
+    _check(load_library().spp_mx4_weight_grad(ctx._h, lists._arr, len(lists.lists), groups, D, H, _TYPES[lists.dtype or torch.float32],
+                                              _ptr(out), SPP_SYNC if sync else 0))
+    return out
+
+
+class AdamW:
+    """AdamW over many tensors in one launch (per 64 of them), moments in 32 bits or in 8 with a scale per 256 elements.
+
+    params: contiguous float32 or bfloat16 tensors on the GPU, updated in place.  An element whose second moment would not be
+    finite (its gradient is not) keeps its value and moments; skipped() counts them.
+    """
+
+    def __init__(self, ctx: Context, params: Sequence[torch.Tensor], state_bits: int = 32, lr: float = 1e-3, betas=(0.9, 0.999),
+                 eps: float = 1e-8, weight_decay: float = 0.01):
+        if state_bits not in (8, 32):
+            raise SppError("state_bits must be 8 or 32")
+        self.ctx, self.state_bits, self.t = ctx, state_bits, 0
+        self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
+        self.params = list(params)
+        dev = torch.device("cuda", ctx.device)
+        self._arr = (_AdamwTensor * max(len(self.params), 1))()
+        self._state = []
+        with torch.cuda.stream(ctx.stream):
+            for j, p in enumerate(self.params):
+                if not (p.is_cuda and p.is_contiguous() and p.dtype in (torch.float32, torch.bfloat16)):
+                    raise SppError(f"parameter {j} must be a contiguous float32 or bfloat16 tensor on the GPU")
+                n = p.numel()
+                ty = torch.float32 if state_bits == 32 else torch.uint8
+                blocks = 0 if state_bits == 32 else -(-n // SPP_ADAMW_BLOCK)
+                s = (torch.zeros(n, dtype=ty, device=dev), torch.zeros(n, dtype=ty, device=dev),
+                     torch.zeros((blocks, 2), dtype=torch.float32, device=dev))
+                self._state.append(s)
+                a = self._arr[j]
+                a.d_p, a.n, a.p_type = p.data_ptr(), n, _TYPES[p.dtype]
+                a.d_m, a.d_v, a.d_scale = s[0].data_ptr(), s[1].data_ptr(), s[2].data_ptr() if blocks else None
+
+    def step(self, grads: Sequence[torch.Tensor], lr: Optional[float] = None, sync: bool = True):
+        """One step with a gradient (any of the three types) for every parameter."""
+        if len(grads) != len(self.params):
+            raise SppError("one gradient per parameter is needed")
+        for j, (p, g) in enumerate(zip(self.params, grads)):
+            if not (g.is_cuda and g.is_contiguous() and g.numel() == p.numel()):
+                raise SppError(f"gradient {j} must be a contiguous tensor on the GPU of its parameter's size")
+            self._arr[j].d_p, self._arr[j].d_g, self._arr[j].g_type = p.data_ptr(), g.data_ptr(), _type(g.dtype, f"gradient {j}")
+        h = _AdamwHyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.weight_decay)
+        _check(load_library().spp_adamw_step(self.ctx._h, self._arr, len(self.params), self.state_bits, C.byref(h), self.t + 1,
+                                             SPP_SYNC if sync else 0))
+        self.t += 1
+
+    def _moments(self, m, v):
+        n = len(self.params)
+        return (C.c_void_p * max(n, 1))(*[x.data_ptr() for x in m]), (C.c_void_p * max(n, 1))(*[x.data_ptr() for x in v])
+
+    def state(self, sync: bool = True):
+        """(m, v): float32 tensors, one per parameter: the moments themselves, or the values that 8 bits stand for."""
+        if self.state_bits == 32:
+            if sync:
+                self.ctx.sync()
+            return [s[0].view(p.shape) for s, p in zip(self._state, self.params)], [s[1].view(p.shape) for s, p in zip(self._state, self.params)]
+        m = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
+        v = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
+        pm, pv = self._moments(m, v)
+        _check(load_library().spp_adamw_values(self.ctx._h, self._arr, len(self.params), pm, pv, SPP_SYNC if sync else 0))
+        return m, v
+
+    def load(self, m: Sequence[torch.Tensor], v: Sequence[torch.Tensor], t: int):
+        """Continue from given moments (float32, one per parameter) after t steps."""
+        if len(m) != len(self.params) or len(v) != len(self.params) or int(t) < 0:
+            raise SppError("one m and one v per parameter and a step count are needed")
+        for j, (p, a, b) in enumerate(zip(self.params, m, v)):
+            if _dev(a, torch.float32, f"m {j}").numel() != p.numel() or _dev(b, torch.float32, f"v {j}").numel() != p.numel():
+                raise SppError(f"moments {j} must be of their parameter's size")
+        if self.state_bits == 32:
+            with torch.cuda.stream(self.ctx.stream):
+                for s, a, b in zip(self._state, m, v):
+                    s[0].copy_(a.view(-1))
+                    s[1].copy_(b.view(-1))
+        else:
+            pm, pv = self._moments(m, v)
+            _check(load_library().spp_adamw_load(self.ctx._h, self._arr, len(self.params), pm, pv, 0))
+        self.ctx.sync()
+        self.t = int(t)
+
+    def skipped(self) -> int:
+        """Elements that steps on this context have left as they were since its totals were last reset; waits for the streams."""
+        buf = (C.c_int64 * 16)()
+        _check(load_library().spp_ctx_totals(self.ctx._h, buf, 0))
+        return int(buf[9])

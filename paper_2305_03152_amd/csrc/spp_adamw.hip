@@ -1,0 +1,342 @@
+// One AdamW step over many tensors at once, with the two moments in 32 bits or in 8.
+//
+//   m' = b1 m + (1-b1) g      v' = b2 v + (1-b2) g^2
+//   p' = (1 - lr wd) p - lr/(1-b1^t) * m' / (sqrt(v') / sqrt(1-b2^t) + eps)
+//
+// each operation rounded once, in the order written.  An element whose v' is not finite (its gradient is not, or its square is
+// not) is left as it was, its moments too.
+//
+// In 8 bits the moments of 256 consecutive elements share a scale each: the largest |m| and the largest sqrt(v) of the block
+// are the largest code, and a code is a small float: m a sign, 4 bits of exponent and 3 of mantissa, sqrt(v) 4 and 4.  Steps
+// of a constant ratio, because both moments are divided by each other: an evenly spaced code would hold small second moments as
+// zero, and their updates would be m / eps.  For the same reason a v that is not zero keeps at least the smallest code.  The
+// update itself uses the moments before they are rounded to 8 bits.
+//
+// All of it is element by element and bound by HBM: 28 bytes per fp32 parameter and gradient with moments in 32 bits, 16 in 8.
+#include "spp_mx4.h"
+
+#include <math.h>
+
+namespace spp {
+
+constexpr int kAdamTensors = kWave;          // of one launch: a lane has a tensor's first chunk
+constexpr int kAdamBlock = 256, kAdamPer = 8, kAdamChunk = kAdamBlock * kAdamPer;
+constexpr int kAdamShared = SPP_ADAMW_BLOCK;
+static_assert(kAdamShared == 4 * kWave, "a wavefront has a block, four elements per lane");
+
+struct AdamTable {
+    void*       p[kAdamTensors];
+    const void* g[kAdamTensors];
+    void*       m[kAdamTensors];
+    void*       v[kAdamTensors];
+    float*      scale[kAdamTensors];
+    int64_t     n[kAdamTensors];
+    uint32_t    first[kAdamTensors];         // first chunk; behind the last tensor: all ones
+    uint8_t     kind[kAdamTensors];          // type of p, type of g << 2, and 16 if four elements may be taken at a time
+};
+struct AdamHyper { float b1, c1, b2, c2, rs, eps, decay, step; };
+
+__device__ __forceinline__ uint32_t chunk_owner(const AdamTable& t) {
+    return (uint32_t)__builtin_amdgcn_readfirstlane(__popcll(__ballot(t.first[lane_id()] <= blockIdx.x)) - 1);
+}
+
+template <class T>
+__device__ __forceinline__ void load4(const void* base, int64_t i, int have, bool wide, float (&x)[4]) {
+    const T* p = static_cast<const T*>(base) + i;
+    if (have >= 4 && wide) {
+        const typename Elem<T>::v4 a = *reinterpret_cast<const typename Elem<T>::v4*>(p);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = (float)a[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = k < have ? (float)p[k] : 0.0f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store4(void* base, int64_t i, int have, bool wide, const float (&x)[4]) {
+    T* p = static_cast<T*>(base) + i;
+    if (have >= 4 && wide) {
+        typename Elem<T>::v4 a;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = (T)x[k];
+        *reinterpret_cast<typename Elem<T>::v4*>(p) = a;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < have) p[k] = (T)x[k];
+    }
+}
+__device__ __forceinline__ void load_any(int type, const void* base, int64_t i, int have, bool wide, float (&x)[4]) {
+    if (type == SPP_F32) load4<float>(base, i, have, wide, x);
+    else if (type == SPP_F16) load4<_Float16>(base, i, have, wide, x);
+    else load4<__bf16>(base, i, have, wide, x);
+}
+__device__ __forceinline__ void load_codes(const void* base, int64_t i, int have, bool wide, uint32_t (&c)[4]) {
+    const uint8_t* p = static_cast<const uint8_t*>(base) + i;
+    if (have >= 4 && wide) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c[k] = (w >> (8 * k)) & 255u;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c[k] = k < have ? p[k] : 0u;
+    }
+}
+__device__ __forceinline__ void store_codes(void* base, int64_t i, int have, bool wide, const uint32_t (&c)[4]) {
+    uint8_t* p = static_cast<uint8_t*>(base) + i;
+    if (have >= 4 && wide) *reinterpret_cast<uint32_t*>(p) = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+    else
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < have) p[k] = (uint8_t)c[k];
+}
+
+// False: the element stays as it was.
+__device__ __forceinline__ bool adam_element(const AdamHyper& h, float g, float& p, float& m, float& v) {
+    const float m1 = m * h.b1 + g * h.c1;
+    const float v1 = v * h.b2 + (g * g) * h.c2;
+    if ((__float_as_uint(v1) & 0x7F800000u) == 0x7F800000u) return false;
+    const float den = sqrtf(v1) * h.rs + h.eps;
+    p = p * h.decay - (m1 / den) * h.step;
+    m = m1;
+    v = v1;
+    return true;
+}
+
+// The moments of a block as codes and back.  `most` is the largest code's value before the scale.
+constexpr float kMostM = 1.875f, kMostV = 1.9375f, kLeastScale = 0x1p-100f;
+struct Moment { float inv, scale; };
+__device__ __forceinline__ Moment moment_scale(float largest, float most) {
+    // below this 1 / scale would not be finite: the block counts as zeros
+    return largest >= kLeastScale ? Moment{most / largest, largest * (1.0f / most)} : Moment{0.0f, 0.0f};
+}
+template <int DROP, int BASE, int TOP>
+__device__ __forceinline__ uint32_t small_float(float q) {
+    const uint32_t u = __float_as_uint(q);
+    const int c = (int)((u + ((1u << (DROP - 1)) - 1) + ((u >> DROP) & 1u)) >> DROP) - BASE;
+    return (uint32_t)(c < 0 ? 0 : c > TOP ? TOP : c);
+}
+__device__ __forceinline__ uint32_t code_m(float m, const Moment& s) {
+    const uint32_t c = small_float<20, 896, 127>(fabsf(m) * s.inv);
+    return c ? c | (__float_as_uint(m) >> 31) << 7 : 0u;
+}
+__device__ __forceinline__ uint32_t code_v(float r, const Moment& s) {
+    const uint32_t c = small_float<19, 1792, 255>(r * s.inv);
+    return r > 0.0f && s.scale > 0.0f ? (c ? c : 1u) : 0u;
+}
+__device__ __forceinline__ float value_m(uint32_t c, float scale) {
+    const float a = __uint_as_float(((c & 127u) + 896u) << 20) * scale;
+    return (c & 127u) ? (c & 128u ? -a : a) : 0.0f;
+}
+__device__ __forceinline__ float value_v(uint32_t c, float scale) {
+    const float r = __uint_as_float((c + 1792u) << 19) * scale;
+    return c ? r * r : 0.0f;
+}
+__device__ __forceinline__ float wave_max(float x) {            // of values that are not negative
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)wave_inclusive_max(__float_as_uint(x)), kWave - 1));
+}
+__device__ __forceinline__ void put_moments(const AdamTable& t, uint32_t j, int64_t i, int have, bool wide, const float (&m)[4], const float (&v)[4]) {
+    float am = 0.f, r[4], ar = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        r[k] = sqrtf(v[k]);
+        am = fmaxf(am, fabsf(m[k]));
+        ar = fmaxf(ar, r[k]);
+    }
+    const Moment sm = moment_scale(wave_max(am), kMostM), sv = moment_scale(wave_max(ar), kMostV);
+    uint32_t cm[4], cv[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { cm[k] = code_m(m[k], sm); cv[k] = code_v(r[k], sv); }
+    store_codes(t.m[j], i, have, wide, cm);
+    store_codes(t.v[j], i, have, wide, cv);
+    if (lane_id() == 0) {
+        float* s = t.scale[j] + 2 * (i / kAdamShared);
+        s[0] = sm.scale; s[1] = sv.scale;
+    }
+}
+__device__ __forceinline__ void get_moments(const AdamTable& t, uint32_t j, int64_t i, int have, bool wide, float (&m)[4], float (&v)[4]) {
+    uint32_t cm[4], cv[4];
+    load_codes(t.m[j], i, have, wide, cm);
+    load_codes(t.v[j], i, have, wide, cv);
+    const float* s = t.scale[j] + 2 * (i / kAdamShared);
+    const float sm = s[0], sv = s[1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { m[k] = value_m(cm[k], sm); v[k] = value_v(cv[k], sv); }
+}
+
+template <bool Small>
+__global__ void __launch_bounds__(kAdamBlock) adamw_kernel(AdamTable t, AdamHyper h, int64_t* skipped) {
+    const uint32_t j = chunk_owner(t);
+    const int64_t n = t.n[j], at = (int64_t)(blockIdx.x - t.first[j]) * kAdamChunk;
+    const int kind = t.kind[j];
+    const bool wide = kind & 16;
+    int left_alone = 0;
+#pragma unroll
+    for (int round = 0; round < kAdamPer / 4; ++round) {
+        const int64_t i = at + (round * kAdamBlock + (int)threadIdx.x) * 4;
+        const int64_t rest = n - i;
+        // in 8 bits a wavefront has a block: all of it goes or none, and lanes behind the last element bring zeros
+        if (Small ? n - (i - 4 * lane_id()) <= 0 : rest <= 0) break;
+        const int have = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+        float p[4], g[4], m[4], v[4];
+        load_any(kind & 3, t.p[j], i, have, wide, p);
+        load_any((kind >> 2) & 3, t.g[j], i, have, wide, g);
+        if constexpr (Small) get_moments(t, j, have ? i : n - 1, have, wide, m, v);
+        else { load4<float>(t.m[j], i, have, wide, m); load4<float>(t.v[j], i, have, wide, v); }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) left_alone += !adam_element(h, g[k], p[k], m[k], v[k]);
+        if ((kind & 3) == SPP_F32) store4<float>(t.p[j], i, have, wide, p);
+        else store4<__bf16>(t.p[j], i, have, wide, p);
+        if constexpr (Small) put_moments(t, j, i, have, wide, m, v);
+        else { store4<float>(t.m[j], i, have, wide, m); store4<float>(t.v[j], i, have, wide, v); }
+    }
+    if (left_alone) atomicAdd(reinterpret_cast<unsigned long long*>(skipped), (unsigned long long)left_alone);
+}
+
+// Moments in 8 bits from fp32 arrays, and back.  t.p: fp32 m, t.g: fp32 v.
+__global__ void __launch_bounds__(kAdamBlock) adamw_load_kernel(AdamTable t) {
+    const uint32_t j = chunk_owner(t);
+    const int64_t n = t.n[j], at = (int64_t)(blockIdx.x - t.first[j]) * kAdamChunk;
+    const bool wide = t.kind[j] & 16;
+    for (int round = 0; round < kAdamPer / 4; ++round) {
+        const int64_t i = at + (round * kAdamBlock + (int)threadIdx.x) * 4;
+        if (n - (i - 4 * lane_id()) <= 0) break;
+        const int have = n - i >= 4 ? 4 : n - i > 0 ? (int)(n - i) : 0;
+        float m[4], v[4];
+        load4<float>(t.p[j], i, have, wide, m);
+        load4<float>(t.g[j], i, have, wide, v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {                       // what no step can have left there counts as zero
+            if ((__float_as_uint(m[k]) & 0x7F800000u) == 0x7F800000u) m[k] = 0.0f;
+            if (!(v[k] >= 0.0f) || (__float_as_uint(v[k]) & 0x7F800000u) == 0x7F800000u) v[k] = 0.0f;
+        }
+        put_moments(t, j, i, have, wide, m, v);
+    }
+}
+__global__ void __launch_bounds__(kAdamBlock) adamw_values_kernel(AdamTable t) {
+    const uint32_t j = chunk_owner(t);
+    const int64_t n = t.n[j], at = (int64_t)(blockIdx.x - t.first[j]) * kAdamChunk;
+    const bool wide = t.kind[j] & 16;
+#pragma unroll
+    for (int round = 0; round < kAdamPer / 4; ++round) {
+        const int64_t i = at + (round * kAdamBlock + (int)threadIdx.x) * 4;
+        if (i >= n) break;
+        const int have = n - i >= 4 ? 4 : (int)(n - i);
+        float m[4], v[4];
+        get_moments(t, j, i, have, wide, m, v);
+        store4<float>(t.p[j], i, have, wide, m);
+        store4<float>(const_cast<void*>(t.g[j]), i, have, wide, v);
+    }
+}
+
+static int adam_check(const char* who, const spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, int32_t bits) {
+    SPP_CHECK(ctx && (tensors || n_tensors == 0), SPP_E_ARG, "%s: null argument", who);
+    SPP_CHECK(n_tensors >= 0, SPP_E_ARG, "%s: %d tensors", who, n_tensors);
+    SPP_CHECK(bits == 32 || bits == 8, SPP_E_ARG, "%s: states of %d bits (32 or 8)", who, bits);
+    for (int k = 0; k < n_tensors; ++k) {
+        const spp_adamw_tensor& a = tensors[k];
+        SPP_CHECK(a.n >= 0 && a.n <= SPP_ADAMW_MAX_ELEMENTS, SPP_E_ARG, "%s: tensor %d: n = %lld", who, k, (long long)a.n);
+        SPP_CHECK((a.p_type == SPP_F32 || a.p_type == SPP_BF16) && is_type(a.g_type), SPP_E_ARG, "%s: tensor %d: types %d, %d", who, k, a.p_type,
+                  a.g_type);
+        SPP_CHECK(a.n == 0 || (a.d_p && a.d_g && a.d_m && a.d_v && (bits == 32 || a.d_scale)), SPP_E_ARG, "%s: tensor %d: null argument", who, k);
+        const size_t state = bits == 32 ? 4 : 1;
+        SPP_CHECK((uintptr_t)a.d_p % type_bytes(a.p_type) == 0 && (uintptr_t)a.d_g % type_bytes(a.g_type) == 0 && (uintptr_t)a.d_m % state == 0 &&
+                      (uintptr_t)a.d_v % state == 0 && (bits == 32 || (uintptr_t)a.d_scale % 4 == 0),
+                  SPP_E_ARG, "%s: tensor %d: an array is not aligned to its type", who, k);
+    }
+    return SPP_OK;
+}
+// Launches over as many tensors at a time as a table holds.  run(table, chunks)
+template <class Run>
+static int adam_launches(const spp_adamw_tensor* tensors, int32_t n_tensors, int32_t bits, Run run) {
+    for (int k = 0; k < n_tensors;) {
+        AdamTable t;
+        memset(&t, 0, sizeof(t));
+        memset(t.first, 0xFF, sizeof(t.first));
+        int64_t chunks = 0;
+        for (int j = 0; j < kAdamTensors && k < n_tensors; ++k) {
+            const spp_adamw_tensor& a = tensors[k];
+            if (a.n == 0) continue;
+            const int64_t more = (a.n + kAdamChunk - 1) / kAdamChunk;
+            if (chunks + more > 0xFFFFFFll) break;             // a grid has fewer than 2^32 threads
+            const size_t state = bits == 32 ? 4 : 1;
+            const bool wide = (uintptr_t)a.d_p % (4 * type_bytes(a.p_type)) == 0 && (uintptr_t)a.d_g % (4 * type_bytes(a.g_type)) == 0 &&
+                              (uintptr_t)a.d_m % (4 * state) == 0 && (uintptr_t)a.d_v % (4 * state) == 0;
+            t.p[j] = a.d_p; t.g[j] = a.d_g; t.m[j] = a.d_m; t.v[j] = a.d_v; t.scale[j] = a.d_scale; t.n[j] = a.n;
+            t.first[j] = (uint32_t)chunks;
+            t.kind[j] = (uint8_t)(a.p_type | a.g_type << 2 | (wide ? 16 : 0));
+            chunks += more;
+            ++j;
+        }
+        if (chunks == 0) break;
+        run(t, (unsigned)chunks);
+        SPP_HIP(hipGetLastError());
+    }
+    return SPP_OK;
+}
+
+}  // namespace spp
+
+extern "C" int spp_adamw_step(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, const spp_adamw_hyper* hyper,
+                              int64_t t, uint32_t flags) {
+    using namespace spp;
+    SPP_TRY(adam_check("spp_adamw_step", ctx, tensors, n_tensors, state_bits));
+    SPP_CHECK(hyper, SPP_E_ARG, "spp_adamw_step: hyper is null");
+    const double b1 = hyper->beta1, b2 = hyper->beta2;
+    SPP_CHECK(b1 >= 0.0 && b1 < 1.0 && b2 >= 0.0 && b2 < 1.0 && (float)b1 < 1.0f && (float)b2 < 1.0f, SPP_E_ARG, "spp_adamw_step: betas %g, %g", b1, b2);
+    SPP_CHECK((float)hyper->eps >= 0x1p-126f && isfinite((float)hyper->eps) && isfinite(hyper->lr) && hyper->lr >= 0.0 && isfinite(hyper->weight_decay) &&
+                  hyper->weight_decay >= 0.0,
+              SPP_E_ARG, "spp_adamw_step: lr %g, eps %g, weight decay %g", hyper->lr, hyper->eps, hyper->weight_decay);
+    SPP_CHECK(t >= 1, SPP_E_ARG, "spp_adamw_step: step %lld (the first is 1)", (long long)t);
+    AdamHyper h;
+    h.b1 = (float)b1; h.c1 = (float)(1.0 - b1); h.b2 = (float)b2; h.c2 = (float)(1.0 - b2);
+    h.rs = (float)(1.0 / sqrt(1.0 - pow(b2, (double)t)));
+    h.eps = (float)hyper->eps;
+    h.decay = (float)(1.0 - hyper->lr * hyper->weight_decay);
+    h.step = (float)(hyper->lr / (1.0 - pow(b1, (double)t)));
+    SPP_HIP(hipSetDevice(ctx->device));
+    ScopedTimer timer(ctx, SPP_T_ADAMW, ctx->stream);
+    int64_t* skipped = ctx->totals + 9;
+    SPP_TRY(adam_launches(tensors, n_tensors, state_bits, [&](const AdamTable& table, unsigned chunks) {
+        if (state_bits == 32) adamw_kernel<false><<<chunks, kAdamBlock, 0, ctx->stream>>>(table, h, skipped);
+        else adamw_kernel<true><<<chunks, kAdamBlock, 0, ctx->stream>>>(table, h, skipped);
+    }));
+    if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(ctx->stream));
+    return SPP_OK;
+}
+
+// Load and values: the 8-bit state of `tensors`, their fp32 moments in place of parameter and gradient.
+static int adam_moments(const char* who, spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, float* const* d_m, float* const* d_v,
+                        uint32_t flags, bool load) {
+    using namespace spp;
+    SPP_CHECK(ctx && ((tensors && d_m && d_v) || n_tensors == 0), SPP_E_ARG, "%s: null argument", who);
+    SPP_CHECK(n_tensors >= 0, SPP_E_ARG, "%s: %d tensors", who, n_tensors);
+    for (int k = 0; k < n_tensors; ++k) {                   // all of them before any work
+        spp_adamw_tensor a = tensors[k];
+        a.d_p = d_m[k]; a.d_g = d_v[k]; a.p_type = SPP_F32; a.g_type = SPP_F32;
+        SPP_TRY(adam_check(who, ctx, &a, 1, 8));
+    }
+    SPP_HIP(hipSetDevice(ctx->device));
+    for (int k = 0; k < n_tensors; k += kAdamTensors) {
+        spp_adamw_tensor part[kAdamTensors];
+        const int here = n_tensors - k < kAdamTensors ? n_tensors - k : kAdamTensors;
+        for (int j = 0; j < here; ++j) {
+            part[j] = tensors[k + j];
+            part[j].d_p = d_m[k + j]; part[j].d_g = d_v[k + j]; part[j].p_type = SPP_F32; part[j].g_type = SPP_F32;
+        }
+        SPP_TRY(adam_launches(part, here, 8, [&](const AdamTable& table, unsigned chunks) {
+            if (load) adamw_load_kernel<<<chunks, kAdamBlock, 0, ctx->stream>>>(table);
+            else adamw_values_kernel<<<chunks, kAdamBlock, 0, ctx->stream>>>(table);
+        }));
+    }
+    if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(ctx->stream));
+    return SPP_OK;
+}
+extern "C" int spp_adamw_load(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, const float* const* d_m, const float* const* d_v,
+                              uint32_t flags) {
+    return adam_moments("spp_adamw_load", ctx, tensors, n_tensors, const_cast<float* const*>(d_m), const_cast<float* const*>(d_v), flags, true);
+}
+extern "C" int spp_adamw_values(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, float* const* d_m, float* const* d_v,
+                                uint32_t flags) {
+    return adam_moments("spp_adamw_values", ctx, tensors, n_tensors, d_m, d_v, flags, false);
+}

@@ -1,0 +1,423 @@
+// The layer that reads feature rows in MXFP4, and its gradient, over up to 64 lists of rows whose lengths may be known on the
+// device only (the minibatches that a pipeline keeps in flight; rows of several kinds, each kind with a matrix of its own):
+//
+//   product       Y_j = X_j W[g_j]^T           X_j [n_j, D] and W[g] [H, D] in MXFP4, Y_j fp32, fp16 or bf16
+//   weight grad   dW[g] = sum_j dY_j^T X_j     over the lists of group g; dY_j fp32, fp16 or bf16, dW fp32
+//
+// What a code and a scale stand for is exact in bf16, as is an fp32 as the sum of three bf16: the products of both kernels are
+// exact and are added in fp32, so the only other roundings are those of the sums and of Y.
+#include "spp_mx4.h"
+
+namespace spp {
+
+// Lane j has list j: its rows, and the tiles of all lists up to it.  The count of a list may have to be fetched: one round trip.
+struct Lists {
+    int rows, upto, tiles;
+    __device__ __forceinline__ Lists(const RowTable& t, int tile_rows) {
+        const int j = lane_id();
+        rows = j < t.n_lists ? (int)rows_of(t.n[j], t.d_n[j]) : 0;
+        tiles = (int)(((int64_t)rows + tile_rows - 1) / tile_rows);
+        upto = wave_inclusive_scan(tiles);
+    }
+    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(upto, kWave - 1); }
+    __device__ __forceinline__ int list_of(int tile) const { return __builtin_amdgcn_readfirstlane(__popcll(__ballot(upto <= tile))); }
+    __device__ __forceinline__ int rows_in(int list) const { return __builtin_amdgcn_readlane(rows, list); }
+    __device__ __forceinline__ int first_tile(int list) const { return __builtin_amdgcn_readlane(upto - tiles, list); }
+};
+
+// ---- product --------------------------------------------------------------------------------------
+
+struct ProductArgs {
+    RowTable       t;
+    const uint8_t* w;
+    int32_t        D, H, nb, rb;
+};
+
+constexpr int kProdBlock = 256, kProdWaves = 4;
+
+// Four consecutive 32-bit words of operand for a scaled 16x16x128 product in E2M1: the lane's block of 32 columns.
+__device__ __forceinline__ i32x8 mx4_operand(u32x4 v) {
+    return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+}
+
+template <class T, int TR, int RN>
+__global__ void __launch_bounds__(kProdBlock) mx4_product_kernel(ProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t xs[];
+    constexpr int RS = TR / (16 * RN);
+    constexpr bool kHalf = sizeof(T) == 2;
+    const Lists lists(a.t, TR);
+    const int total = lists.total();
+    if (total == 0) return;
+    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
+    const int tasks = (a.H + 63) / 64 * RS;
+    const int most = (tasks + kProdWaves - 1) / kProdWaves;
+    int parts = (int)gridDim.x / total;
+    parts = parts < 1 ? 1 : parts > most ? most : parts;
+    const int64_t items = (int64_t)total * parts;
+    const int steps = (a.nb + 3) / 4;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int tile = (int)(item / parts), part = (int)(item - (int64_t)tile * parts);
+        const int list = lists.list_of(tile);
+        const int64_t r0 = (int64_t)(tile - lists.first_tile(list)) * TR;
+        const int64_t left = lists.rows_in(list) - r0;
+        const int here = left < TR ? (int)left : TR;
+        const u32x4* src = reinterpret_cast<const u32x4*>(a.t.rows[list] + r0 * a.rb);
+        __syncthreads();                                   // the tile before has been read
+        for (int i = threadIdx.x; i < here * (a.rb / 16); i += kProdBlock) reinterpret_cast<u32x4*>(xs)[i] = src[i];
+        __syncthreads();
+        const uint8_t* w = a.w + (int64_t)a.t.group[list] * a.H * a.rb;
+        const int64_t ld = a.t.ld[list];
+        T* y = static_cast<T*>(a.t.y[list]) + r0 * ld;
+        const bool wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0;
+        for (int task = part * kProdWaves + wave; task < tasks; task += parts * kProdWaves) {
+            const int h0 = task / RS * 64, c0 = task % RS * (16 * RN);
+            if (c0 >= here) continue;
+            f32x4 acc[4][RN];
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int c = 0; c < RN; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int s = 0; s < steps; ++s) {
+                const bool in = 4 * s + q < a.nb;                  // else the lane has no block at this step: zeros
+                const int b = in ? 4 * s + q : a.nb - 1;
+                u32x4 wv[4], xv[RN];
+                uint32_t ws[4], xc[RN];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    // which column of Y row m of the operand stands for: a lane's results are then consecutive columns
+                    int h = h0 + (kHalf ? 32 * (f >> 1) + 8 * (m >> 2) + 4 * (f & 1) + (m & 3) : 16 * f + m);
+                    h = h < a.H ? h : a.H - 1;
+                    const uint8_t* p = w + (int64_t)h * a.rb;
+                    wv[f] = *reinterpret_cast<const u32x4*>(p + 16 * b);
+                    ws[f] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * s) >> (8 * q);
+                    if (!in) { wv[f] = u32x4{0, 0, 0, 0}; ws[f] = 127; }
+                }
+#pragma unroll
+                for (int c = 0; c < RN; ++c) {
+                    const uint8_t* p = xs + (c0 + 16 * c + m) * a.rb;
+                    xv[c] = *reinterpret_cast<const u32x4*>(p + 16 * b);
+                    xc[c] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * s) >> (8 * q);
+                    if (!in) { xv[c] = u32x4{0, 0, 0, 0}; xc[c] = 127; }
+                }
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int c = 0; c < RN; ++c)
+                        acc[f][c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(wv[f]), mx4_operand(xv[c]), acc[f][c],
+                                                                                     4, 4, 0, (int)ws[f], 0, (int)xc[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < RN; ++c) {
+                const int row = c0 + 16 * c + m;
+                if (row >= here) continue;
+                T* out = y + row * ld;
+                if constexpr (kHalf) {
+#pragma unroll
+                    for (int f = 0; f < 4; f += 2) {
+                        const int h = h0 + 16 * f + 8 * q;
+                        typename Elem<T>::v8 v;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { v[i] = (T)acc[f][c][i]; v[4 + i] = (T)acc[f + 1][c][i]; }
+                        if (wide && h + 8 <= a.H) *reinterpret_cast<typename Elem<T>::v8*>(out + h) = v;
+                        else
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if (h + i < a.H) out[h + i] = v[i];
+                    }
+                } else {
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        const int h = h0 + 16 * f + 4 * q;
+                        if (wide && h + 4 <= a.H) *reinterpret_cast<f32x4*>(out + h) = acc[f][c];
+                        else
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (h + i < a.H) out[h + i] = acc[f][c][i];
+                    }
+                }
+            }
+        }
+    }
+}
+
+// ---- weight gradient ------------------------------------------------------------------------------
+
+// The rows of all lists, in the order of their groups, are cut into chunks of kGradRows, and the chunks into `splits` runs of equal
+// length.  A workgroup has one run and one tile of dW; where its run passes from a group to the next it writes down what it has as
+// piece (run + group) and starts again, and the second kernel adds up each group's pieces in the order of the rows.  No atomics:
+// the same counts give the same bits.
+constexpr int kGradRows = 64, kGradTile = 128, kGradBlock = 256, kGradLd = kGradTile + 16;     // LDS row: 4 rows apart are 4 x 32 bytes of other banks
+
+struct GradArgs {
+    RowTable t;
+    float*   pieces;       // [splits + groups][H * D]
+    float*   dw;           // [groups][H * D]
+    int32_t  D, H, nb, rb;
+    int32_t  splits, tiles_d, n_groups;
+};
+
+// dY as bf16 numbers that add up to it exactly: one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
+// finite value becomes infinite; what is not finite is its first piece alone.
+template <class T> struct Pieces { static constexpr int n = 1; };
+template <> struct Pieces<_Float16> { static constexpr int n = 2; };
+template <> struct Pieces<float> { static constexpr int n = 3; };
+template <int P>
+__device__ __forceinline__ void cut(float x, __bf16 (&out)[P]) {
+    const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const float head = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+        out[p] = (__bf16)(p == 0 && !finite ? x : head);
+        x = finite ? x - head : 0.0f;
+    }
+}
+
+__device__ __forceinline__ bf16x8 column8(const __bf16* p) {         // eight rows of the lane's column, see below
+    typedef __attribute__((address_space(3))) i16x4* lds4;
+    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p));
+    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 4 * kGradLd));
+    const bf16x4 x = __builtin_bit_cast(bf16x4, a), y = __builtin_bit_cast(bf16x4, b);
+    return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+}
+
+template <class T>
+__global__ void __launch_bounds__(kGradBlock) mx4_grad_kernel(GradArgs a) {
+    constexpr int P = Pieces<T>::n;
+    __shared__ __attribute__((aligned(16))) __bf16 gy[P][kGradRows * kGradLd];
+    __shared__ __attribute__((aligned(16))) __bf16 gx[kGradRows * kGradLd];
+    const Lists lists(a.t, kGradRows);
+    const int total = lists.total();
+    const int splits = a.splits < total ? a.splits : total;
+    const int tiles = (int)gridDim.x / a.splits, tile = (int)blockIdx.x % tiles, split = (int)blockIdx.x / tiles;
+    if (split >= splits) return;
+    const int from = (int)((int64_t)split * total / splits), to = (int)((int64_t)(split + 1) * total / splits);
+    const int h0 = tile / a.tiles_d * kGradTile, d0 = tile % a.tiles_d * kGradTile;
+    const int wave = threadIdx.x >> 6, l = lane_id();
+    const int wh = (wave >> 1) * 64, wd = (wave & 1) * 64;
+
+    f32x4 acc[4][4];
+    auto clear = [&]() {
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    auto flush = [&](int group) {
+        float* out = a.pieces + (int64_t)(split + group) * a.H * a.D;
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int h = h0 + wh + 16 * f + 4 * (l >> 4) + i, d = d0 + wd + 16 * c + (l & 15);
+                    if (h < a.H && d < a.D) out[(int64_t)h * a.D + d] = acc[f][c][i];
+                }
+    };
+    clear();
+    int group = -1;
+    for (int chunk = from; chunk < to; ++chunk) {
+        const int list = lists.list_of(chunk);
+        const int g = a.t.group[list];
+        if (g != group && group >= 0) { flush(group); clear(); }
+        group = g;
+        const int64_t r0 = (int64_t)(chunk - lists.first_tile(list)) * kGradRows;
+        const int64_t left = lists.rows_in(list) - r0;
+        const int here = left < kGradRows ? (int)left : kGradRows;
+        const int64_t ld = a.t.ld[list];
+        const T* y = static_cast<const T*>(a.t.y[list]) + r0 * ld;
+        const bool wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0;
+        __syncthreads();
+        // dY: four columns per thread and round, 32 threads side by side
+        for (int i = threadIdx.x; i < kGradRows * (kGradTile / 4); i += kGradBlock) {
+            const int r = i / (kGradTile / 4), h = i % (kGradTile / 4) * 4;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (r < here) {
+                const T* p = y + r * ld + h0 + h;
+                if (wide && h0 + h + 4 <= a.H) {
+                    const typename Elem<T>::v4 x = *reinterpret_cast<const typename Elem<T>::v4*>(p);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = (float)x[k];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (h0 + h + k < a.H) v[k] = (float)p[k];
+                }
+            }
+            bf16x4 o[P];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                __bf16 c[P];
+                cut<P>(v[k], c);
+#pragma unroll
+                for (int p = 0; p < P; ++p) o[p][k] = c[p];
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) *reinterpret_cast<bf16x4*>(&gy[p][r * kGradLd + h]) = o[p];
+        }
+        // X: a block of 32 columns per thread
+        {
+            const int r = threadIdx.x >> 2, k = threadIdx.x & 3, b = d0 / 32 + k;
+            bf16x8 o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = bf16x8{};
+            if (r < here && b < a.nb) {
+                const uint8_t* p = a.t.rows[list] + (r0 + r) * a.rb;
+                const u32x4 c = *reinterpret_cast<const u32x4*>(p + 16 * b);
+                const float s = mx4_scale(p[16 * a.nb + b]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], s, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], s, 1),
+                                 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], s, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], s, 3);
+                    o[i] = bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<bf16x8*>(&gx[r * kGradLd + 32 * k + 8 * i]) = o[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kGradRows; k += 32) {
+            // 16 lanes read four rows of 16 columns and get a column of four rows each
+            const int at = (k + 8 * (l >> 4) + ((l & 15) >> 2)) * kGradLd + 4 * (l & 3);
+            bf16x8 bx[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) bx[c] = column8(gx + at + wd + 16 * c);
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    const bf16x8 ay = column8(gy[p] + at + wh + 16 * f);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ay, bx[c], acc[f][c], 0, 0, 0);
+                }
+        }
+    }
+    if (group >= 0) flush(group);
+}
+
+__global__ void __launch_bounds__(256) mx4_grad_sum_kernel(GradArgs a) {
+    const Lists lists(a.t, kGradRows);
+    const int total = lists.total(), group = blockIdx.y;
+    const int splits = a.splits < total ? a.splits : total;
+    const int64_t size = (int64_t)a.H * a.D;
+    // the chunks of the group: from its first list's first to its last list's last
+    const uint64_t mine = __ballot(lane_id() < a.t.n_lists && (int)a.t.group[lane_id()] == group && lists.tiles > 0);
+    int lo = 0, hi = -1;
+    if (mine) {
+        const int first = lists.first_tile(__builtin_ctzll(mine)), last = __builtin_amdgcn_readlane(lists.upto, 63 - __builtin_clzll(mine)) - 1;
+        lo = (int)((((int64_t)first + 1) * splits - 1) / total);
+        hi = (int)((((int64_t)last + 1) * splits - 1) / total);
+    }
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+        double sum = 0.0;
+        for (int s = lo; s <= hi; ++s) sum += a.pieces[(int64_t)(s + group) * size + i];
+        a.dw[group * size + i] = (float)sum;
+    }
+}
+
+int row_table(const char* who, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H, int32_t type,
+              RowTable& t, int64_t* most) {
+    SPP_CHECK(n_lists >= 0 && n_lists <= kRowLists && (lists || n_lists == 0), SPP_E_ARG, "%s: %d lists (at most %d)", who, n_lists, kRowLists);
+    SPP_CHECK(n_groups >= 1 && n_groups <= kRowLists, SPP_E_ARG, "%s: %d groups (1 .. %d)", who, n_groups, kRowLists);
+    SPP_CHECK(D >= 1 && D <= SPP_MX4_MAX_COLS && H >= 1 && H <= SPP_MAX_HIDDEN, SPP_E_ARG, "%s: D = %d (1 .. %d), H = %d (1 .. %d)", who, D,
+              SPP_MX4_MAX_COLS, H, SPP_MAX_HIDDEN);
+    SPP_CHECK(is_type(type), SPP_E_ARG, "%s: element type %d", who, type);
+    memset(&t, 0, sizeof(t));
+    *most = 0;
+    for (int j = 0; j < n_lists; ++j) {
+        const spp_row_list& a = lists[j];
+        SPP_CHECK(a.n >= 0 && a.n <= 0x7FFFFFFFll && a.ld >= H && a.group >= 0 && a.group < n_groups, SPP_E_ARG,
+                  "%s: list %d: n = %lld, ld = %lld, group = %d", who, j, (long long)a.n, (long long)a.ld, a.group);
+        SPP_CHECK(a.n == 0 || (a.d_rows && a.d_y), SPP_E_ARG, "%s: list %d: null argument", who, j);
+        SPP_CHECK((uintptr_t)a.d_rows % 16 == 0 && (uintptr_t)a.d_y % type_bytes(type) == 0 && (uintptr_t)a.d_n % 8 == 0, SPP_E_ARG,
+                  "%s: list %d: rows must be 16-byte aligned, Y to its type and the count to 8 bytes", who, j);
+        *most += a.n;
+    }
+    for (int g = 0, k = 0; g < n_groups; ++g)               // the lists in the order of their groups
+        for (int j = 0; j < n_lists; ++j) {
+            if (lists[j].group != g) continue;
+            t.rows[k] = static_cast<const uint8_t*>(lists[j].d_rows);
+            t.y[k] = lists[j].d_y; t.d_n[k] = lists[j].n ? lists[j].d_n : nullptr; t.ld[k] = lists[j].ld;
+            t.n[k] = (int32_t)lists[j].n; t.group[k] = (uint8_t)g;
+            ++k;
+        }
+    t.n_lists = n_lists;
+    return SPP_OK;
+}
+
+template <class T, int TR, int RN>
+static int launch_product(spp_ctx* ctx, const ProductArgs& a, int64_t tiles) {
+    const int lds = TR * a.rb;
+    auto kernel = mx4_product_kernel<T, TR, RN>;
+    if (lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    const int64_t parts = ((a.H + 63) / 64 * (TR / (16 * RN)) + kProdWaves - 1) / kProdWaves;
+    const int64_t want = tiles * parts, most = (int64_t)ctx->num_cu * 4;
+    kernel<<<(unsigned)(want < most ? want : most), kProdBlock, lds, ctx->stream>>>(a);
+    SPP_HIP(hipGetLastError());
+    return SPP_OK;
+}
+template <class T>
+static int product_of(spp_ctx* ctx, const ProductArgs& a) {
+    const int tr = a.rb <= 544 ? 128 : 64;              // a tile of rows fits the LDS, twice where it can
+    int64_t tiles = 0;
+    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)tr - 1) / tr;
+    return tr == 128 ? launch_product<T, 128, 4>(ctx, a, tiles) : launch_product<T, 64, 4>(ctx, a, tiles);
+}
+
+}  // namespace spp
+
+extern "C" int spp_mx4_product(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
+                               int32_t D, int32_t H, int32_t type, uint32_t flags) {
+    using namespace spp;
+    SPP_CHECK(ctx && d_weights, SPP_E_ARG, "spp_mx4_product: null argument");
+    SPP_CHECK((uintptr_t)d_weights % 16 == 0, SPP_E_ARG, "spp_mx4_product: weights must be 16-byte aligned");
+    ProductArgs a;
+    int64_t most = 0;
+    SPP_TRY(row_table("spp_mx4_product", lists, n_lists, n_groups, D, H, type, a.t, &most));
+    if (most > 0) {
+        a.w = static_cast<const uint8_t*>(d_weights);
+        a.D = D; a.H = H; a.nb = mx4_blocks(D); a.rb = mx4_bytes(D);
+        SPP_HIP(hipSetDevice(ctx->device));
+        ScopedTimer timer(ctx, SPP_T_LAYER, ctx->stream);
+        SPP_TRY(type == SPP_F32 ? product_of<float>(ctx, a) : type == SPP_F16 ? product_of<_Float16>(ctx, a) : product_of<__bf16>(ctx, a));
+    }
+    if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(ctx->stream));
+    return SPP_OK;
+}
+
+extern "C" int spp_mx4_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H,
+                                   int32_t type, float* d_grad, uint32_t flags) {
+    using namespace spp;
+    SPP_CHECK(ctx && d_grad, SPP_E_ARG, "spp_mx4_weight_grad: null argument");
+    SPP_CHECK((uintptr_t)d_grad % 4 == 0, SPP_E_ARG, "spp_mx4_weight_grad: the gradient must be 4-byte aligned");
+    GradArgs a;
+    int64_t most = 0;
+    SPP_TRY(row_table("spp_mx4_weight_grad", lists, n_lists, n_groups, D, H, type, a.t, &most));
+    SPP_HIP(hipSetDevice(ctx->device));
+    a.dw = d_grad; a.D = D; a.H = H; a.nb = mx4_blocks(D); a.rb = mx4_bytes(D); a.n_groups = n_groups;
+    a.tiles_d = (D + kGradTile - 1) / kGradTile;
+    const int tiles = a.tiles_d * ((H + kGradTile - 1) / kGradTile);
+    int64_t chunks = 0;
+    for (int j = 0; j < n_lists; ++j) chunks += (a.t.n[j] + (int64_t)kGradRows - 1) / kGradRows;
+    int64_t splits = ((int64_t)ctx->num_cu * 2 + tiles - 1) / tiles;
+    if (splits > (chunks + 1) / 2) splits = (chunks + 1) / 2;
+    a.splits = (int32_t)(splits < 1 ? 1 : splits);
+    const int64_t size = (int64_t)H * D;
+    SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float)));
+    a.pieces = ctx->gradws.as<float>();
+    hipStream_t st = ctx->stream;
+    ScopedTimer timer(ctx, SPP_T_LAYER, st);
+    if (chunks > 0) {
+        const unsigned grid = (unsigned)(a.splits * tiles);
+        if (type == SPP_F32) mx4_grad_kernel<float><<<grid, kGradBlock, 0, st>>>(a);
+        else if (type == SPP_F16) mx4_grad_kernel<_Float16><<<grid, kGradBlock, 0, st>>>(a);
+        else mx4_grad_kernel<__bf16><<<grid, kGradBlock, 0, st>>>(a);
+        SPP_HIP(hipGetLastError());
+    }
+    const int64_t sums = (size + 255) / 256;
+    mx4_grad_sum_kernel<<<dim3((unsigned)(sums < 4096 ? sums : 4096), n_groups), 256, 0, st>>>(a);
+    SPP_HIP(hipGetLastError());
+    if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(st));
+    return SPP_OK;
+}

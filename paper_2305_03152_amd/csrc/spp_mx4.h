@@ -1,0 +1,63 @@
+// Rows in MXFP4 and the element types of the operators on gathered rows: what their kernels share.
+//
+// A row of D columns is nb = ceil(D/32) blocks of 32 columns (the last one filled up with zeros): sixteen bytes of E2M1 codes
+// per block (column 2j of a block in the low half of its byte j), then one E8M0 byte per block, then zeros up to a multiple
+// of sixteen bytes.  Codes before scales, so that a lane takes a block in one aligned 16-byte load.
+#pragma once
+
+#include "spp_common.h"
+#include "spp_device.h"
+
+namespace spp {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct Elem;                      // four and eight elements of a type as vectors
+template <> struct Elem<float> { typedef f32x4 v4; };
+template <> struct Elem<_Float16> { typedef f16x4 v4; typedef f16x8 v8; };
+template <> struct Elem<__bf16> { typedef bf16x4 v4; typedef bf16x8 v8; };
+
+static inline size_t type_bytes(int32_t type) { return type == SPP_F32 ? 4 : 2; }
+static inline bool is_type(int32_t type) { return type == SPP_F32 || type == SPP_F16 || type == SPP_BF16; }
+static inline int mx4_blocks(int32_t D) { return (D + 31) / 32; }
+static inline int mx4_bytes(int32_t D) { return (17 * mx4_blocks(D) + 15) / 16 * 16; }
+
+// 2^(byte - 127) as a float; byte 255 is the format's NaN.
+__device__ __forceinline__ float mx4_scale(uint32_t byte) {
+    return __uint_as_float(byte == 255u ? 0x7FC00000u : byte == 0u ? 0x00400000u : byte << 23);
+}
+
+// Which rows a call has: as given, or counted on the device, never more than the caller's buffers hold.
+__device__ __forceinline__ int64_t rows_of(int64_t n, const int64_t* d_n) {
+    if (!d_n) return n;
+    const int64_t c = *d_n;
+    return c < 0 ? 0 : c < n ? c : n;
+}
+
+// Lists of packed rows, each with a matrix Y of its own: the operands of the product and of its gradient.
+constexpr int kRowLists = SPP_MAX_ROW_LISTS;
+static_assert(kRowLists == kWave, "a wavefront's lanes hold a list each");
+struct RowTable {
+    const uint8_t* rows[kRowLists];
+    void*          y[kRowLists];
+    const int64_t* d_n[kRowLists];
+    int64_t        ld[kRowLists];
+    int32_t        n[kRowLists];
+    uint8_t        group[kRowLists];
+    int32_t        n_lists;
+};
+// Host: the checks that the product and the gradient share; fills the table, and *most with the rows the lists can hold.
+int row_table(const char* who, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H, int32_t type,
+              RowTable& t, int64_t* most);
+
+}  // namespace spp

@@ -1,0 +1,156 @@
+"""Feature rows in MXFP4 on the GPU: every code and scale byte against the definition in 64 bits, and back."""
+import numpy as np
+import pytest
+import torch
+
+import mx4_reference as R
+import paper_2305_03152_amd as spp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = spp.Context(0)
+    yield c
+    c.close()
+
+
+def _bytes(ctx, x, **kw):
+    return spp.mx4_quantize(ctx, x, **kw).cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D", [(1, 1), (1, 32), (3, 31), (5, 33), (257, 100), (1000, 128), (513, 256), (70, 768), (2, 4096), (4099, 7), (0, 64)])
+def test_codes_and_scales_are_the_definition_s(ctx, dtype, n, D):
+    gen = torch.Generator().manual_seed(n * 5000 + D)
+    x = (torch.randn(n, D, generator=gen) * torch.exp2(torch.randint(-8, 8, (n, 1), generator=gen).float())).to(dtype)
+    x[torch.rand(n, D, generator=gen) < 0.1] = 0
+    got = _bytes(ctx, x.to(DEV))
+    assert got.shape == (n, R.row_bytes(D)) and spp.mx4_row_bytes(D) == R.row_bytes(D)
+    assert np.array_equal(got, R.quantize(x.double().numpy()))
+
+
+def test_every_tie_and_every_neighbour_of_one(ctx):
+    """Quarters of the code range with their neighbours in fp32, at several scales: a block is led by 6 times its scale."""
+    t = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 0.5, 1, 1.5, 2, 3, 4, 6, 7, 7.999], np.float32)
+    t = np.concatenate([t, np.nextafter(t, np.float32(0)), np.nextafter(t, np.float32(9))])
+    t = np.concatenate([t, -t, [0.0, -0.0]]).astype(np.float32)
+    rows = []
+    for e in (-126, -125, -100, -3, 0, 1, 90, 124, 125):
+        for i in range(0, len(t), 31):
+            b = np.zeros(32, np.float32)
+            part = t[i:i + 31]
+            b[1:1 + len(part)] = part * np.float32(2.0 ** e)
+            b[0] = 6 * 2.0 ** e
+            rows.append(b)
+    x = np.stack(rows)
+    assert np.isfinite(x).all()
+    assert np.array_equal(_bytes(ctx, torch.from_numpy(x).to(DEV)), R.quantize(x))
+
+
+def test_smallest_values_zeros_and_largest(ctx):
+    x = np.zeros((6, 64), np.float32)
+    x[0, :3] = [1e-45, -1e-45, 3e-45]                    # subnormal: the least scale
+    x[1, :3] = [2.0 ** -126, 2.0 ** -127, 2.0 ** -128]
+    x[2, 0] = 2.0 ** -125
+    x[3, :4] = [3.4028235e38, -3.4028235e38, 1e38, 1e-38]
+    x[4, :] = -0.0
+    got = _bytes(ctx, torch.from_numpy(x).to(DEV))
+    assert np.array_equal(got, R.quantize(x))
+    back = spp.mx4_dequantize(ctx, torch.from_numpy(got).to(DEV), 64).cpu().numpy()
+    assert np.array_equal(back.astype(np.float64), R.values(got, 64))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_block_with_nan_or_infinity_is_nan_and_only_that_block(ctx, dtype):
+    x = torch.randn(7, 96).to(dtype)
+    x[1, 40] = float("nan")
+    x[2, 0] = float("inf")
+    x[3, 95] = -float("inf")
+    if dtype == torch.float32:
+        x.view(torch.int32)[4, 33] = 0x7F800001             # a NaN whose upper half is an infinity
+    else:
+        x[4, 33] = float("nan")
+    got = _bytes(ctx, x.to(DEV))
+    assert np.array_equal(got, R.quantize(x.double().numpy()))
+    back = spp.mx4_dequantize(ctx, torch.from_numpy(got).to(DEV), 96, dtype=dtype).cpu()
+    nan = torch.zeros(7, 3, dtype=torch.bool)
+    for r, b in ((1, 1), (2, 0), (3, 2), (4, 1)):
+        nan[r, b] = True
+    assert torch.equal(torch.isnan(back).view(7, 3, 32).all(2), nan) and torch.equal(torch.isnan(back).view(7, 3, 32).any(2), nan)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D", [(1, 1), (300, 100), (64, 128), (9, 800)])
+def test_values_are_those_of_the_codes(ctx, dtype, n, D):
+    """All bytes of codes and scales from 2^-20 to 2^9: no rounding in fp32, one to nearest in 16 bits."""
+    rng = np.random.default_rng(n * 1000 + D)
+    nb = -(-D // 32)
+    rows = np.zeros((n, R.row_bytes(D)), np.uint8)
+    rows[:, :16 * nb] = rng.integers(0, 256, (n, 16 * nb))
+    rows[:, 16 * nb:17 * nb] = rng.integers(107, 137, (n, nb))
+    rows[:, 17 * nb:] = 255                                     # what lies behind the scales is not looked at
+    got = spp.mx4_dequantize(ctx, torch.from_numpy(rows).to(DEV), D, dtype=dtype).cpu()
+    want = torch.from_numpy(R.values(rows, D)).to(dtype)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offset,pad", [(0, 0), (1, 3), (4, 4), (8, 13)])
+def test_rows_apart_and_at_odd_addresses(ctx, dtype, offset, pad):
+    n, D = 37, 100
+    buf = torch.randn(offset + n * (D + pad) + 8, device=DEV).to(dtype)
+    x = torch.as_strided(buf, (n, D), (D + pad, 1), offset)
+    got = spp.mx4_quantize(ctx, x)
+    assert np.array_equal(got.cpu().numpy(), R.quantize(x.double().cpu().numpy()))
+    out = torch.full((offset + n * (D + pad) + 8,), 7.0, device=DEV).to(dtype)
+    view = torch.as_strided(out, (n, D), (D + pad, 1), offset)
+    spp.mx4_dequantize(ctx, got, D, out=view)
+    assert torch.equal(view.cpu(), torch.from_numpy(R.values(got.cpu().numpy(), D)).to(dtype))
+    keep = torch.ones(out.numel(), dtype=torch.bool)
+    keep.as_strided((n, D), (D + pad, 1), offset).fill_(False)
+    assert (out.cpu()[keep] == 7).all()                          # nothing between or behind the rows
+
+
+@pytest.mark.parametrize("count,rows", [(0, 0), (1, 1), (63, 63), (200, 100), (-5, 0)])
+def test_a_count_on_the_device_bounds_both_ways(ctx, count, rows):
+    n, D = 100, 48
+    x = torch.randn(n, D, device=DEV)
+    c = torch.tensor([count], dtype=torch.int64, device=DEV)
+    out = torch.full((n, spp.mx4_row_bytes(D)), 9, dtype=torch.uint8, device=DEV)
+    spp.mx4_quantize(ctx, x, out=out, n_device=c)
+    assert np.array_equal(out[:rows].cpu().numpy(), R.quantize(x[:rows].double().cpu().numpy())) and (out[rows:] == 9).all()
+    back = torch.full((n, D), 9.0, device=DEV)
+    spp.mx4_dequantize(ctx, out, D, out=back, n_device=c)
+    assert np.array_equal(back[:rows].double().cpu().numpy(), R.values(out[:rows].cpu().numpy(), D)) and (back[rows:] == 9).all()
+
+
+def test_rows_of_a_large_array_beyond_32_bits_of_bytes(ctx):
+    n, D = 3_000_000, 768                                        # 4.6 GB of fp16 in, 1.2 GB of rows
+    x = torch.zeros(n, D, dtype=torch.float16, device=DEV)
+    pick = torch.tensor([0, 1, 1_400_000, 2_796_203, n - 1], device=DEV)
+    x[pick] = torch.randn(len(pick), D, device=DEV).half()
+    rows = spp.mx4_quantize(ctx, x)
+    assert np.array_equal(rows[pick].cpu().numpy(), R.quantize(x[pick].double().cpu().numpy()))
+    back = spp.mx4_dequantize(ctx, rows, D, dtype=torch.float16)
+    assert np.array_equal(back[pick].double().cpu().numpy(), R.values(rows[pick].cpu().numpy(), D))
+    assert int(back[2:1_400_000].count_nonzero()) == 0
+
+
+def test_gathered_rows_are_the_store_s(ctx):
+    """A store of packed rows through cache, shard and pinned host memory: the gather moves them unchanged."""
+    N, lo, hi, D = 4000, 1000, 2000, 100
+    rb = spp.mx4_row_bytes(D)
+    x = torch.randn(N, D)
+    rows = spp.mx4_quantize(ctx, x.to(DEV))
+    remote = torch.cat([rows[:lo], rows[hi:]]).cpu().pin_memory()
+    score = torch.rand(N, device=DEV)
+    cache = spp.build_vip_cache(ctx, score, lo, hi, 4, 0.5, remote, rb, 1)
+    ids = torch.randint(0, N, (3000,), dtype=torch.int32, device=DEV)
+    out, stats = spp.gather_features(ctx, cache, rows[lo:hi].contiguous(), N, lo, hi, remote, ids)
+    assert min(stats["n_local"], stats["n_cache_hit"], stats["n_miss"]) > 0
+    assert torch.equal(out, rows[ids.long()])
+    assert np.array_equal(out.cpu().numpy(), R.quantize(x[ids.cpu().long()].double().numpy()))
