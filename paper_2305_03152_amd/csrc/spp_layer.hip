@@ -31,6 +31,8 @@ struct ProductArgs {
     RowTable       t;
     const uint8_t* w;
     int32_t        D, H, nb, rb;
+    int32_t        ls;           // bytes of a row of W in LDS: an odd number of 16, so that 16 rows lie in banks of their own
+    uint32_t       magic;        // ceil(2^32 / (rb / 16))
 };
 
 constexpr int kProdBlock = 256, kProdWaves = 4;
@@ -40,11 +42,159 @@ __device__ __forceinline__ i32x8 mx4_operand(u32x4 v) {
     return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
 }
 
+// A product's operands: rows of X as the 16 rows of the result, columns 4m + f of a 64-column tile of Y as column m of result f.
+// A lane then has four columns side by side, and the 16 lanes of a row 64: stores of whole 128-byte lines.
+__device__ __forceinline__ int tile_column(int f, int m) { return 4 * m + f; }
+
+// A vector at an address that is aligned to its elements only: one access all the same.
+template <class V> struct Loose { V v; } __attribute__((packed, aligned(2)));
+
+// Columns h .. h+3 of rows y[0..3], of which `have` are there.
+template <class T>
+__device__ __forceinline__ void put_tile(T* y, int64_t ld, int have, int h, int H, bool wide, const f32x4 (&acc)[4]) {
+    typedef typename Elem<T>::v4 V;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= have) continue;
+        const V v = {(T)acc[0][i], (T)acc[1][i], (T)acc[2][i], (T)acc[3][i]};
+        T* out = y + i * ld + h;
+        if (wide && h + 4 <= H) *reinterpret_cast<V*>(out) = v;
+        else if (h + 4 <= H) reinterpret_cast<Loose<V>*>(out)->v = v;
+        else
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (h + k < H) out[k] = v[k];
+    }
+}
+
+// The ordinary form, for D up to 768.  A wavefront holds its 16 RN rows of X in registers, all columns of them, and goes over the
+// columns of Y 64 at a time; W comes from LDS, where a workgroup's wavefronts share it.  If all of W fits it stays there
+// (Stream false), else 64 of its rows at a time, the next ones asked for while these are used.  X is read once and Y, which is most
+// of what moves, written once.
+template <class T, int KS, int RN, int WAVES, bool Stream>
+__global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t ws[];
+    constexpr int TB = WAVES * 16 * RN, threads = 64 * WAVES;
+    constexpr int kVec = (64 * (KS * 4 * 17 + 15) / 16 + threads - 1) / threads;       // vectors of 64 rows of W per thread
+    const Lists lists(a.t, TB);
+    const int total = lists.total();
+    if (total == 0) return;
+    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
+    const int ht = (a.H + 63) / 64;
+    int parts = (int)gridDim.x / total;                // few rows: the columns of Y are dealt out too
+    parts = parts < 1 ? 1 : parts > ht ? ht : parts;
+    const int64_t items = (int64_t)total * parts;
+    const int rv = a.rb / 16, lv = a.ls / 16;          // vectors of a row of W in memory and in LDS
+    int held_group = -1, held_from = -1;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int part = (int)(item / total), tile = (int)(item - (int64_t)part * total);
+        const int t0 = (int)((int64_t)part * ht / parts), t1 = (int)((int64_t)(part + 1) * ht / parts);
+        const int list = lists.list_of(tile);
+        const int64_t r0 = (int64_t)(tile - lists.first_tile(list)) * TB;
+        const int64_t left = lists.rows_in(list) - r0;
+        const int here = left < TB ? (int)left : TB, mine = here - wave * 16 * RN;       // rows of the workgroup, of the wavefront
+        const int group = a.t.group[list];
+        const uint8_t* w = a.w + (int64_t)group * a.H * a.rb;
+        // X: a lane has row m of each 16 and every fourth block
+        const uint8_t* x = a.t.rows[list] + r0 * a.rb;
+        u32x4 xv[KS][RN];
+        uint32_t xc[KS][RN];
+#pragma unroll
+        for (int c = 0; c < RN; ++c) {
+            const int row = (wave * RN + c) * 16 + m;
+            const uint8_t* p = x + (row < here ? row : here - 1) * a.rb;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bool in = 4 * s + q < a.nb;
+                xv[s][c] = *reinterpret_cast<const u32x4*>(p + 16 * (in ? 4 * s + q : 0));
+                xc[s][c] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * (4 * s < a.nb ? s : 0));
+            }
+        }
+        const int64_t ld = a.t.ld[list];
+        T* y = static_cast<T*>(a.t.y[list]) + (r0 + wave * 16 * RN) * ld;
+        const bool wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0;
+
+        u32x4 next[kVec];
+        auto ask = [&](int t) {                        // rows 64 t .. of W
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const uint32_t i = k * threads + threadIdx.x, r = __umulhi(i, a.magic);
+                const int h = 64 * t + (int)r < a.H ? 64 * t + (int)r : a.H - 1;
+                next[k] = *reinterpret_cast<const u32x4*>(w + (int64_t)h * a.rb + 16 * (i - r * rv));
+            }
+        };
+        auto keep = [&](uint8_t* to) {
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const uint32_t i = k * threads + threadIdx.x, r = __umulhi(i, a.magic);
+                if (r < 64) reinterpret_cast<u32x4*>(to)[((r & 3) * 16 + (r >> 2)) * lv + (i - r * rv)] = next[k];        // by operand
+            }
+        };
+        if (Stream) {
+            ask(t0);
+            __syncthreads();                           // the item before has been worked off
+            keep(ws + (t0 & 1) * (64 * a.ls + 64));
+            __syncthreads();
+        } else if (group != held_group || t0 != held_from) {
+            __syncthreads();
+            for (int t = t0; t < t1; ++t) {
+                ask(t);
+                keep(ws + (t - t0) * 64 * a.ls);
+            }
+            held_group = group; held_from = t0;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int c = 0; c < RN; ++c) {
+                const bool in = 4 * s + q < a.nb;
+                xc[s][c] = in ? xc[s][c] >> (8 * q) : 127u;
+                if (!in) xv[s][c] = u32x4{0, 0, 0, 0};
+            }
+        for (int t = t0; t < t1; ++t) {
+            const uint8_t* tile_w = Stream ? ws + (t & 1) * (64 * a.ls + 64) : ws + (t - t0) * 64 * a.ls;
+            if (Stream && t + 1 < t1) ask(t + 1);
+            f32x4 acc[RN][4];
+#pragma unroll
+            for (int c = 0; c < RN; ++c)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (mine > 0)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    u32x4 wv[4];
+                    uint32_t wc[4];
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        // a lane without a block at this step reads what lies behind: X has zeros there, the scale is made finite
+                        const uint8_t* p = tile_w + (16 * f + m) * a.ls;
+                        wv[f] = *reinterpret_cast<const u32x4*>(p + 16 * (4 * s + q));
+                        wc[f] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * s) >> (8 * q);
+                        if (s == KS - 1) wc[f] = 4 * s + q < a.nb ? wc[f] : 127u;
+                    }
+#pragma unroll
+                    for (int f = 0; f < 4; ++f)
+#pragma unroll
+                        for (int c = 0; c < RN; ++c)
+                            acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(xv[s][c]), mx4_operand(wv[f]), acc[c][f], 4, 4,
+                                                                                         0, (int)xc[s][c], 0, (int)wc[f]);
+                }
+            if (Stream && t + 1 < t1) keep(ws + ((t + 1) & 1) * (64 * a.ls + 64));
+#pragma unroll
+            for (int c = 0; c < RN; ++c)
+                put_tile<T>(y + (16 * c + 4 * q) * ld, ld, mine - 16 * c - 4 * q, 64 * t + 4 * m, a.H, wide, acc[c]);
+            if (Stream) __syncthreads();
+        }
+    }
+}
+
+// The form for wider rows, and for calls of few rows, whose W is better read once by those who need it: a workgroup takes a tile of
+// TR rows into LDS and its wavefronts take 16 RN of them by 64 columns of Y at a time, W straight from memory.
 template <class T, int TR, int RN>
 __global__ void __launch_bounds__(kProdBlock) mx4_product_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t xs[];
     constexpr int RS = TR / (16 * RN);
-    constexpr bool kHalf = sizeof(T) == 2;
     const Lists lists(a.t, TR);
     const int total = lists.total();
     if (total == 0) return;
@@ -72,25 +222,24 @@ __global__ void __launch_bounds__(kProdBlock) mx4_product_kernel(ProductArgs a) 
         for (int task = part * kProdWaves + wave; task < tasks; task += parts * kProdWaves) {
             const int h0 = task / RS * 64, c0 = task % RS * (16 * RN);
             if (c0 >= here) continue;
-            f32x4 acc[4][RN];
+            f32x4 acc[RN][4];
 #pragma unroll
-            for (int f = 0; f < 4; ++f)
+            for (int c = 0; c < RN; ++c)
 #pragma unroll
-                for (int c = 0; c < RN; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
             for (int s = 0; s < steps; ++s) {
                 const bool in = 4 * s + q < a.nb;                  // else the lane has no block at this step: zeros
                 const int b = in ? 4 * s + q : a.nb - 1;
                 u32x4 wv[4], xv[RN];
-                uint32_t ws[4], xc[RN];
+                uint32_t wc[4], xc[RN];
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
-                    // which column of Y row m of the operand stands for: a lane's results are then consecutive columns
-                    int h = h0 + (kHalf ? 32 * (f >> 1) + 8 * (m >> 2) + 4 * (f & 1) + (m & 3) : 16 * f + m);
+                    int h = h0 + tile_column(f, m);
                     h = h < a.H ? h : a.H - 1;
                     const uint8_t* p = w + (int64_t)h * a.rb;
                     wv[f] = *reinterpret_cast<const u32x4*>(p + 16 * b);
-                    ws[f] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * s) >> (8 * q);
-                    if (!in) { wv[f] = u32x4{0, 0, 0, 0}; ws[f] = 127; }
+                    wc[f] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * s) >> (8 * q);
+                    if (!in) { wv[f] = u32x4{0, 0, 0, 0}; wc[f] = 127; }
                 }
 #pragma unroll
                 for (int c = 0; c < RN; ++c) {
@@ -103,39 +252,12 @@ __global__ void __launch_bounds__(kProdBlock) mx4_product_kernel(ProductArgs a) 
                 for (int f = 0; f < 4; ++f)
 #pragma unroll
                     for (int c = 0; c < RN; ++c)
-                        acc[f][c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(wv[f]), mx4_operand(xv[c]), acc[f][c],
-                                                                                     4, 4, 0, (int)ws[f], 0, (int)xc[c]);
+                        acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(xv[c]), mx4_operand(wv[f]), acc[c][f],
+                                                                                     4, 4, 0, (int)xc[c], 0, (int)wc[f]);
             }
 #pragma unroll
-            for (int c = 0; c < RN; ++c) {
-                const int row = c0 + 16 * c + m;
-                if (row >= here) continue;
-                T* out = y + row * ld;
-                if constexpr (kHalf) {
-#pragma unroll
-                    for (int f = 0; f < 4; f += 2) {
-                        const int h = h0 + 16 * f + 8 * q;
-                        typename Elem<T>::v8 v;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { v[i] = (T)acc[f][c][i]; v[4 + i] = (T)acc[f + 1][c][i]; }
-                        if (wide && h + 8 <= a.H) *reinterpret_cast<typename Elem<T>::v8*>(out + h) = v;
-                        else
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                if (h + i < a.H) out[h + i] = v[i];
-                    }
-                } else {
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        const int h = h0 + 16 * f + 4 * q;
-                        if (wide && h + 4 <= a.H) *reinterpret_cast<f32x4*>(out + h) = acc[f][c];
-                        else
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (h + i < a.H) out[h + i] = acc[f][c][i];
-                    }
-                }
-            }
+            for (int c = 0; c < RN; ++c)
+                put_tile<T>(y + (c0 + 16 * c + 4 * q) * ld, ld, here - c0 - 16 * c - 4 * q, h0 + 4 * m, a.H, wide, acc[c]);
         }
     }
 }
@@ -467,22 +589,51 @@ int row_table(const char* who, const spp_row_list* lists, int32_t n_lists, int32
 }
 
 template <class T, int TR, int RN>
-static int launch_product(spp_ctx* ctx, const ProductArgs& a, int64_t tiles) {
+static int launch_product(spp_ctx* ctx, const ProductArgs& a) {
     const int lds = TR * a.rb;
     auto kernel = mx4_product_kernel<T, TR, RN>;
     if (lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    int64_t tiles = 0;
+    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)TR - 1) / TR;
     const int64_t parts = ((a.H + 63) / 64 * (TR / (16 * RN)) + kProdWaves - 1) / kProdWaves;
     const int64_t want = tiles * parts, most = (int64_t)ctx->num_cu * 4;
     kernel<<<(unsigned)(want < most ? want : most), kProdBlock, lds, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
-template <class T>
-static int product_of(spp_ctx* ctx, const ProductArgs& a) {
-    const int tr = a.rb <= 544 ? 128 : 64;              // a tile of rows fits the LDS, twice where it can
+template <class T, int KS, int RN, int WAVES, bool Stream>
+static int launch_rows_as(spp_ctx* ctx, const ProductArgs& a, int lds) {
+    auto kernel = mx4_rows_kernel<T, KS, RN, WAVES, Stream>;
+    if (lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     int64_t tiles = 0;
-    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)tr - 1) / tr;
-    return tr == 128 ? launch_product<T, 128, 4>(ctx, a, tiles) : launch_product<T, 64, 4>(ctx, a, tiles);
+    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)(WAVES * 16 * RN) - 1) / (WAVES * 16 * RN);
+    const int64_t want = tiles * ((a.H + 63) / 64), most = (int64_t)ctx->num_cu * (163840 / lds < 16 / WAVES ? 163840 / lds : 16 / WAVES);
+    kernel<<<(unsigned)(want < most ? want : most), 64 * WAVES, lds, ctx->stream>>>(a);
+    SPP_HIP(hipGetLastError());
+    return SPP_OK;
+}
+constexpr int kHeldW = 65536;            // LDS for a W that stays
+template <class T, int KS>
+static int launch_rows(spp_ctx* ctx, const ProductArgs& a) {
+    const int all = (a.H + 63) / 64 * 64 * a.ls + 64;
+    return all <= kHeldW ? launch_rows_as<T, KS, 2, 4, false>(ctx, a, all) : launch_rows_as<T, KS, 2, 8, true>(ctx, a, 2 * (64 * a.ls + 64));
+}
+constexpr int kFewRows = 64;
+template <class T>
+static int product_of(spp_ctx* ctx, ProductArgs& a, int64_t most) {
+    if (most <= kFewRows) return launch_product<T, 64, 1>(ctx, a);
+    const int rv = a.rb / 16;
+    a.ls = 16 * (rv | 1);
+    a.magic = (uint32_t)((0x100000000ull + rv - 1) / rv);
+    switch ((a.nb + 3) / 4) {
+        case 1: return launch_rows<T, 1>(ctx, a);
+        case 2: return launch_rows<T, 2>(ctx, a);
+        case 3: return launch_rows<T, 3>(ctx, a);
+        case 4: return launch_rows<T, 4>(ctx, a);
+        case 5: return launch_rows<T, 5>(ctx, a);
+        case 6: return launch_rows<T, 6>(ctx, a);
+        default: return a.rb <= 544 ? launch_product<T, 128, 4>(ctx, a) : launch_product<T, 64, 4>(ctx, a);
+    }
 }
 
 }  // namespace spp
@@ -500,7 +651,7 @@ extern "C" int spp_mx4_product(spp_ctx* ctx, const spp_row_list* lists, int32_t 
         a.D = D; a.H = H; a.nb = mx4_blocks(D); a.rb = mx4_bytes(D);
         SPP_HIP(hipSetDevice(ctx->device));
         ScopedTimer timer(ctx, SPP_T_LAYER, ctx->stream);
-        SPP_TRY(type == SPP_F32 ? product_of<float>(ctx, a) : type == SPP_F16 ? product_of<_Float16>(ctx, a) : product_of<__bf16>(ctx, a));
+        SPP_TRY(type == SPP_F32 ? product_of<float>(ctx, a, most) : type == SPP_F16 ? product_of<_Float16>(ctx, a, most) : product_of<__bf16>(ctx, a, most));
     }
     if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(ctx->stream));
     return SPP_OK;
