@@ -33,6 +33,8 @@ struct ProductArgs {
     int32_t        D, H, nb, rb;
     int32_t        ls;           // bytes of a row of W in LDS: an odd number of 16, so that 16 rows lie in banks of their own
     uint32_t       magic;        // ceil(2^32 / (rb / 16))
+    int32_t        w_lds;        // bytes of W in LDS; behind them, per wavefront, out_lds for rows of Y on their way:
+    int32_t        out_lds, out_pitch, out_tiles;      // bytes, bytes of a row, 64-column tiles that go out together
 };
 
 constexpr int kProdBlock = 256, kProdWaves = 4;
@@ -55,9 +57,9 @@ __device__ __forceinline__ void put_tile(T* y, int64_t ld, int have, int h, int 
     typedef typename Elem<T>::v4 V;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (i >= have) continue;
         const V v = {(T)acc[0][i], (T)acc[1][i], (T)acc[2][i], (T)acc[3][i]};
         T* out = y + i * ld + h;
+        if (i >= have) continue;
         if (wide && h + 4 <= H) *reinterpret_cast<V*>(out) = v;
         else if (h + 4 <= H) reinterpret_cast<Loose<V>*>(out)->v = v;
         else
@@ -66,16 +68,95 @@ __device__ __forceinline__ void put_tile(T* y, int64_t ld, int have, int h, int 
                 if (h + k < H) out[k] = v[k];
     }
 }
+// All of them, aligned.
+template <class T>
+__device__ __forceinline__ void put_whole(T* y, int64_t ld, const f32x4 (&acc)[4]) {
+    typedef typename Elem<T>::v4 V;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<V*>(y + i * ld) = V{(T)acc[0][i], (T)acc[1][i], (T)acc[2][i], (T)acc[3][i]};
+}
+
+// A wavefront's rows of Y on their way to memory: put together in LDS, where each 16-byte piece lies as it does in memory, and
+// written side by side, so that whatever the rows' length and alignment whole lines go out.  Rows that follow each other without
+// a gap are one run.  The ends of a run, less than 16 bytes, are written by element.
+template <class T>
+struct RowsOut {
+    uint8_t* lds;
+    char*    y;              // first row, column c0
+    int64_t  step;           // bytes from a row to the next
+    int      rows, bytes;    // of the run of columns
+    int      pitch;          // bytes of a row in LDS
+    bool     run;            // one run of bytes
+    __device__ __forceinline__ int at(int row) const {           // where the row starts
+        return run ? (int)((uintptr_t)y & 15) + row * (int)step : row * pitch + (int)(((uintptr_t)y + row * step) & 15);
+    }
+    // Columns c .. c+3 of rows 4q .. 4q+3, of which `have` columns are there.
+    __device__ __forceinline__ void put(int row, int c, int have, const f32x4 (&acc)[4]) const {
+        typedef typename Elem<T>::v4 V;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint8_t* p = lds + at(row + i) + c * (int)sizeof(T);
+            const V v = {(T)acc[0][i], (T)acc[1][i], (T)acc[2][i], (T)acc[3][i]};
+            if (row + i >= rows) continue;
+            if (have >= 4) reinterpret_cast<Loose<V>*>(p)->v = v;
+            else
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (k < have) reinterpret_cast<T*>(p)[k] = v[k];
+        }
+    }
+    __device__ __forceinline__ void flush() const {
+        wave_lds_order();
+        const int l = lane_id();
+        const int n = run ? 1 : rows, len = run ? (rows - 1) * (int)step + bytes : bytes;
+        if (run || n == 1) {
+            const int head = (int)((uintptr_t)y & 15), first = head ? 1 : 0, end = (head + len) / 16;
+            u32x4* to = reinterpret_cast<u32x4*>(y - head);
+            const u32x4* from = reinterpret_cast<const u32x4*>(lds);
+            int k = first + l;
+            for (; k + 3 * kWave < end; k += 4 * kWave) {
+                u32x4 v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = from[k + u * kWave];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) to[k + u * kWave] = v[u];
+            }
+            for (; k < end; k += kWave) to[k] = from[k];
+        } else {
+            const int slots = (len + 30) / 16;                   // 16-byte pieces that a row can touch
+            const uint32_t magic = slots > 1 ? 0xFFFFFFFFu / (uint32_t)slots + 1 : 0;
+            for (int i = l; i < n * slots; i += kWave) {
+                const int r = slots > 1 ? (int)__umulhi((uint32_t)i, magic) : i, k = i - r * slots;
+                char* start = y + r * step;
+                const int head = (int)((uintptr_t)start & 15);
+                if (16 * k >= head && 16 * k + 16 <= head + len)
+                    *reinterpret_cast<u32x4*>(start - head + 16 * k) = *reinterpret_cast<const u32x4*>(lds + at(r) - head + 16 * k);
+            }
+        }
+        if (((uintptr_t)y | (uintptr_t)len | (n > 1 ? (uintptr_t)step : 0)) & 15) {
+            // 16 lanes per run: eight elements at most before its first whole piece, eight at most behind its last
+            for (int i = l; i < n * 16; i += kWave) {
+                const int r = i / 16, k = i % 8;
+                char* start = y + r * step;
+                const int head = (int)((uintptr_t)start & 15), end = head + len;
+                const int off = i & 8 ? (end & ~15) + k * (int)sizeof(T) : head + k * (int)sizeof(T);
+                const bool mine = i & 8 ? off < end && (end >= 16 || !head) : head && off < 16 && off < end;
+                if (mine) *reinterpret_cast<T*>(start - head + off) = *reinterpret_cast<const T*>(lds + at(r) - head + off);
+            }
+        }
+        wave_lds_order();
+    }
+};
 
 // The ordinary form, for D up to 768.  A wavefront holds its 16 RN rows of X in registers, all columns of them, and goes over the
 // columns of Y 64 at a time; W comes from LDS, where a workgroup's wavefronts share it.  If all of W fits it stays there
 // (Stream false), else 64 of its rows at a time, the next ones asked for while these are used.  X is read once and Y, which is most
 // of what moves, written once.
-template <class T, int KS, int RN, int WAVES, bool Stream>
+template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
 __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t ws[];
     constexpr int TB = WAVES * 16 * RN, threads = 64 * WAVES;
-    constexpr int kVec = (64 * (KS * 4 * 17 + 15) / 16 + threads - 1) / threads;       // vectors of 64 rows of W per thread
+    constexpr int kVec = (64 * ((KS * 4 * 17 + 15) / 16) + threads - 1) / threads;       // vectors of 64 rows of W per thread
     const Lists lists(a.t, TB);
     const int total = lists.total();
     if (total == 0) return;
@@ -86,33 +167,53 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     const int64_t items = (int64_t)total * parts;
     const int rv = a.rb / 16, lv = a.ls / 16;          // vectors of a row of W in memory and in LDS
     int held_group = -1, held_from = -1;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int part = (int)(item / total), tile = (int)(item - (int64_t)part * total);
-        const int t0 = (int)((int64_t)part * ht / parts), t1 = (int)((int64_t)(part + 1) * ht / parts);
-        const int list = lists.list_of(tile);
-        const int64_t r0 = (int64_t)(tile - lists.first_tile(list)) * TB;
-        const int64_t left = lists.rows_in(list) - r0;
-        const int here = left < TB ? (int)left : TB, mine = here - wave * 16 * RN;       // rows of the workgroup, of the wavefront
-        const int group = a.t.group[list];
-        const uint8_t* w = a.w + (int64_t)group * a.H * a.rb;
-        // X: a lane has row m of each 16 and every fourth block
-        const uint8_t* x = a.t.rows[list] + r0 * a.rb;
-        u32x4 xv[KS][RN];
-        uint32_t xc[KS][RN];
+    RowsOut<T> out;
+    out.lds = ws + a.w_lds + wave * a.out_lds;
+    out.pitch = a.out_pitch;
+    struct Item { int part, list, here, group; int64_t r0; };
+    auto find = [&](int64_t item) {
+        Item it;
+        it.part = (int)(item / total);
+        const int tile = (int)(item - (int64_t)it.part * total);
+        it.list = lists.list_of(tile);
+        it.r0 = (int64_t)(tile - lists.first_tile(it.list)) * TB;
+        const int64_t left = lists.rows_in(it.list) - it.r0;
+        it.here = left < TB ? (int)left : TB;
+        it.group = a.t.group[it.list];
+        return it;
+    };
+    // X: a lane has row m of each 16 and every fourth block.  Asked for an item ahead.
+    u32x4 ahead[KS][RN];
+    uint32_t ahead_scale[KS][RN];
+    auto ask_rows = [&](const Item& it) {
+        const uint8_t* x = a.t.rows[it.list] + it.r0 * a.rb;
 #pragma unroll
         for (int c = 0; c < RN; ++c) {
             const int row = (wave * RN + c) * 16 + m;
-            const uint8_t* p = x + (row < here ? row : here - 1) * a.rb;
+            const uint8_t* p = x + (row < it.here ? row : it.here - 1) * a.rb;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const bool in = 4 * s + q < a.nb;
-                xv[s][c] = *reinterpret_cast<const u32x4*>(p + 16 * (in ? 4 * s + q : 0));
-                xc[s][c] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * (4 * s < a.nb ? s : 0));
+                ahead[s][c] = *reinterpret_cast<const u32x4*>(p + 16 * (in ? 4 * s + q : 0));
+                ahead_scale[s][c] = *reinterpret_cast<const uint32_t*>(p + 16 * a.nb + 4 * s);
             }
         }
+    };
+    const Share share(items);
+    if (share.at >= share.end) return;
+    constexpr bool kAhead = !Stream;                   // streams have fewer registers than KS = 6 would need for it
+    Item it = find(share.at);
+    if (kAhead) ask_rows(it);
+    for (int64_t item = share.at; item < share.end; item += share.step) {
+        if (!kAhead) { it = find(item); ask_rows(it); }
+        const int t0 = (int)((int64_t)it.part * ht / parts), t1 = (int)((int64_t)(it.part + 1) * ht / parts);
+        const int list = it.list, here = it.here, group = it.group, mine = here - wave * 16 * RN;       // rows of the workgroup, of the wavefront
+        const int64_t r0 = it.r0;
+        const uint8_t* w = a.w + (int64_t)group * a.H * a.rb;
         const int64_t ld = a.t.ld[list];
         T* y = static_cast<T*>(a.t.y[list]) + (r0 + wave * 16 * RN) * ld;
-        const bool wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0;
+        out.rows = mine < 16 * RN ? mine : 16 * RN;
+        out.step = ld * (int64_t)sizeof(T);
 
         u32x4 next[kVec];
         auto ask = [&](int t) {                        // rows 64 t .. of W
@@ -144,14 +245,18 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
             held_group = group; held_from = t0;
             __syncthreads();
         }
+        u32x4 xv[KS][RN];
+        uint32_t xc[KS][RN];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int c = 0; c < RN; ++c) {
                 const bool in = 4 * s + q < a.nb;
-                xc[s][c] = in ? xc[s][c] >> (8 * q) : 127u;
-                if (!in) xv[s][c] = u32x4{0, 0, 0, 0};
+                xc[s][c] = in ? ahead_scale[s][c] >> (8 * q) : 127u;
+                xv[s][c] = in ? ahead[s][c] : u32x4{0, 0, 0, 0};
             }
+        if (kAhead && item + share.step < share.end) { it = find(item + share.step); ask_rows(it); }
+        int c0 = 64 * t0;                              // first column of the run that is being put together
         for (int t = t0; t < t1; ++t) {
             const uint8_t* tile_w = Stream ? ws + (t & 1) * (64 * a.ls + 64) : ws + (t - t0) * 64 * a.ls;
             if (Stream && t + 1 < t1) ask(t + 1);
@@ -181,9 +286,25 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
                                                                                          0, (int)xc[s][c], 0, (int)wc[f]);
                 }
             if (Stream && t + 1 < t1) keep(ws + ((t + 1) & 1) * (64 * a.ls + 64));
+            if constexpr (Lines) {
+                if (mine >= 16 * RN && 64 * t + 64 <= a.H) {
 #pragma unroll
-            for (int c = 0; c < RN; ++c)
-                put_tile<T>(y + (16 * c + 4 * q) * ld, ld, mine - 16 * c - 4 * q, 64 * t + 4 * m, a.H, wide, acc[c]);
+                    for (int c = 0; c < RN; ++c) put_whole<T>(y + (16 * c + 4 * q) * ld + 64 * t + 4 * m, ld, acc[c]);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < RN; ++c) put_tile<T>(y + (16 * c + 4 * q) * ld, ld, mine - 16 * c - 4 * q, 64 * t + 4 * m, a.H, true, acc[c]);
+                }
+            } else if (mine > 0) {
+                const int last = t + 1 - c0 / 64 == a.out_tiles || t + 1 == t1;
+                const int end = c0 + 64 * a.out_tiles < 64 * t1 ? c0 + 64 * a.out_tiles : 64 * t1;       // where the run ends
+                out.y = reinterpret_cast<char*>(y + c0);
+                out.bytes = ((end < a.H ? end : a.H) - c0) * (int)sizeof(T);
+                out.run = out.bytes == out.step;
+                const int h = 64 * t + 4 * m;
+#pragma unroll
+                for (int c = 0; c < RN; ++c) out.put(16 * c + 4 * q, h - c0, a.H - h, acc[c]);
+                if (last) { out.flush(); c0 = 64 * (t + 1); }
+            }
             if (Stream) __syncthreads();
         }
     }
@@ -601,22 +722,36 @@ static int launch_product(spp_ctx* ctx, const ProductArgs& a) {
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
-template <class T, int KS, int RN, int WAVES, bool Stream>
-static int launch_rows_as(spp_ctx* ctx, const ProductArgs& a, int lds) {
-    auto kernel = mx4_rows_kernel<T, KS, RN, WAVES, Stream>;
+constexpr int kHeldW = 65536;            // LDS for a W that stays
+constexpr int kRowOut = 768;             // bytes of Y's rows that go out whole; longer ones 512 bytes at a time
+template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
+static int launch_rows_as(spp_ctx* ctx, ProductArgs& a, int out_tiles) {
+    auto kernel = mx4_rows_kernel<T, KS, RN, WAVES, Stream, Lines>;
+    const int ht = (a.H + 63) / 64;
+    a.w_lds = Stream ? 2 * (64 * a.ls + 64) : ht * 64 * a.ls + 64;
+    a.out_tiles = out_tiles;
+    const int cols = out_tiles < ht ? 64 * out_tiles : a.H;
+    a.out_pitch = (cols * (int)sizeof(T) + 15) / 16 * 16 + 16;
+    a.out_lds = 16 * RN * a.out_pitch;
+    const int lds = a.w_lds + (Lines ? 0 : WAVES * a.out_lds);
     if (lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     int64_t tiles = 0;
     for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)(WAVES * 16 * RN) - 1) / (WAVES * 16 * RN);
-    const int64_t want = tiles * ((a.H + 63) / 64), most = (int64_t)ctx->num_cu * (163840 / lds < 16 / WAVES ? 163840 / lds : 16 / WAVES);
+    const int64_t want = tiles * ht, most = (int64_t)ctx->num_cu * (163840 / lds < 16 / WAVES ? 163840 / lds : 16 / WAVES);
     kernel<<<(unsigned)(want < most ? want : most), 64 * WAVES, lds, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
-constexpr int kHeldW = 65536;            // LDS for a W that stays
 template <class T, int KS>
-static int launch_rows(spp_ctx* ctx, const ProductArgs& a) {
-    const int all = (a.H + 63) / 64 * 64 * a.ls + 64;
-    return all <= kHeldW ? launch_rows_as<T, KS, 2, 4, false>(ctx, a, all) : launch_rows_as<T, KS, 2, 8, true>(ctx, a, 2 * (64 * a.ls + 64));
+static int launch_rows(spp_ctx* ctx, ProductArgs& a) {
+    const int ht = (a.H + 63) / 64;
+    // Y's rows begin with a line each: stored as they come, 128 or 256 bytes of a row at a time
+    bool lines = true;
+    for (int j = 0; j < a.t.n_lists; ++j) lines = lines && ((uintptr_t)a.t.y[j] | (uint64_t)(a.t.ld[j] * (int64_t)sizeof(T))) % 128 == 0;
+    const int whole = a.H * (int)sizeof(T) <= kRowOut ? ht : 512 / 64 / (int)sizeof(T);
+    if (ht * 64 * a.ls <= kHeldW)
+        return lines ? launch_rows_as<T, KS, 2, 4, false, true>(ctx, a, 1) : launch_rows_as<T, KS, 1, 4, false, false>(ctx, a, whole);
+    return lines ? launch_rows_as<T, KS, 2, 8, true, true>(ctx, a, 1) : launch_rows_as<T, KS, 2, 8, true, false>(ctx, a, 1);
 }
 constexpr int kFewRows = 64;
 template <class T>

@@ -44,6 +44,19 @@ __device__ __forceinline__ int64_t rows_of(int64_t n, const int64_t* d_n) {
     return c < 0 ? 0 : c < n ? c : n;
 }
 
+// Which of `items` equal pieces of a stream of memory a workgroup takes, from `at` by `step` up to `end`.  Consecutive workgroups go
+// to the eight XCDs in turn: each XCD gets a contiguous eighth of the stream.  Plain writes of 1.3 GB, tiles of 16 KB: 6.1 to 6.4 TB/s so,
+// 4.8 to 5.5 with the tiles dealt out in order.
+struct Share {
+    int64_t at, end, step;
+    __device__ __forceinline__ explicit Share(int64_t items) {
+        const unsigned groups = gridDim.x < 8 ? gridDim.x : 8, x = blockIdx.x % groups;
+        at = items * x / groups + blockIdx.x / groups;
+        end = items * (x + 1) / groups;
+        step = (gridDim.x - x + groups - 1) / groups;
+    }
+};
+
 // Lists of packed rows, each with a matrix Y of its own: the operands of the product and of its gradient.
 constexpr int kRowLists = SPP_MAX_ROW_LISTS;
 static_assert(kRowLists == kWave, "a wavefront's lanes hold a list each");
