@@ -33,8 +33,8 @@ struct ProductArgs {
     int32_t        D, H, nb, rb;
     int32_t        ls;           // bytes of a row of W in LDS: an odd number of 16, so that 16 rows lie in banks of their own
     uint32_t       magic;        // ceil(2^32 / (rb / 16))
-    int32_t        w_lds;        // bytes of W in LDS; behind them, per wavefront, out_lds for rows of Y on their way:
-    int32_t        out_lds, out_pitch, out_tiles;      // bytes, bytes of a row, 64-column tiles that go out together
+    int32_t        w_lds;        // bytes of W in LDS; behind them, per wavefront, room for rows of Y on their way:
+    int32_t        out_lds;      // bytes
 };
 
 constexpr int kProdBlock = 256, kProdWaves = 4;
@@ -73,76 +73,139 @@ template <class T>
 __device__ __forceinline__ void put_whole(T* y, int64_t ld, const f32x4 (&acc)[4]) {
     typedef typename Elem<T>::v4 V;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<V*>(y + i * ld) = V{(T)acc[0][i], (T)acc[1][i], (T)acc[2][i], (T)acc[3][i]};
+    for (int i = 0; i < 4; ++i) __builtin_nontemporal_store(V{(T)acc[0][i], (T)acc[1][i], (T)acc[2][i], (T)acc[3][i]}, reinterpret_cast<V*>(y + i * ld));
 }
 
-// A wavefront's rows of Y on their way to memory: put together in LDS, where each 16-byte piece lies as it does in memory, and
-// written side by side, so that whatever the rows' length and alignment whole lines go out.  Rows that follow each other without
-// a gap are one run.  The ends of a run, less than 16 bytes, are written by element.
-template <class T>
+// A wavefront's 16 RN rows of Y on their way to memory where they do not begin with a line each.  They are put together in LDS and
+// written by whole 16-byte pieces, side by side; the ends of a row or a run, less than a piece, by element.
+//   run    the rows follow each other without a gap and fit: all of them are put together as one run of bytes
+//   lines  64 columns of every row at a time, each byte where it lies in its 128-byte line: what they fill of lines goes out, the
+//          begun line stays for the next 64
+// Offsets that every 64 columns share are computed once a tile of rows: a tile of 16 x 64 results costs a SIMD some 150 clocks of
+// matrix work, which is not many instructions.
+template <class T, int RN>
 struct RowsOut {
+    static constexpr int kBytes = 64 * (int)sizeof(T), kPitch = kBytes + 128, kPieces = 2 * RN;     // per lane: rows lane/8 + 8j, a piece of each line
+    typedef typename Elem<T>::v4 V;
     uint8_t* lds;
-    char*    y;              // first row, column c0
+    char*    y;              // first row, first of the wavefront's columns
     int64_t  step;           // bytes from a row to the next
-    int      rows, bytes;    // of the run of columns
-    int      pitch;          // bytes of a row in LDS
-    bool     run;            // one run of bytes
-    __device__ __forceinline__ int at(int row) const {           // where the row starts
-        return run ? (int)((uintptr_t)y & 15) + row * (int)step : row * pitch + (int)(((uintptr_t)y + row * step) & 15);
+    int      rows, bytes;    // bytes of the wavefront's columns of a row
+    bool     run;
+    int      to[RN][4];      // where in LDS the lane's four columns of its rows go
+    __device__ __forceinline__ int phase(int row) const { return (int)(((uintptr_t)y + row * step) & 127); }
+    __device__ __forceinline__ void begin() {
+        const int q = lane_id() >> 4, m = lane_id() & 15;
+#pragma unroll
+        for (int c = 0; c < RN; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * c + 4 * q + i;
+                to[c][i] = 4 * m * (int)sizeof(T) + (run ? (int)((uintptr_t)y & 15) + row * (int)step : row * kPitch + phase(row));
+            }
     }
-    // Columns c .. c+3 of rows 4q .. 4q+3, of which `have` columns are there.
-    __device__ __forceinline__ void put(int row, int c, int have, const f32x4 (&acc)[4]) const {
-        typedef typename Elem<T>::v4 V;
+    // The t-th 64 columns from the wavefront's first.  An LDS write that is not aligned to its size takes many times one that is
+    // (rows of 2002 bytes 424 us, of 2008 246), so each alignment has writes of its own.
+    template <class W>
+    __device__ __forceinline__ void put_as(uint8_t* at, const f32x4 (&acc)[RN][4]) const {
+        constexpr int n = (int)(sizeof(V) / sizeof(W));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint8_t* p = lds + at(row + i) + c * (int)sizeof(T);
-            const V v = {(T)acc[0][i], (T)acc[1][i], (T)acc[2][i], (T)acc[3][i]};
-            if (row + i >= rows) continue;
-            if (have >= 4) reinterpret_cast<Loose<V>*>(p)->v = v;
-            else
+        for (int c = 0; c < RN; ++c)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (k < have) reinterpret_cast<T*>(p)[k] = v[k];
+            for (int i = 0; i < 4; ++i) {
+                const V v = {(T)acc[c][0][i], (T)acc[c][1][i], (T)acc[c][2][i], (T)acc[c][3][i]};
+                struct Words { W w[n]; } words = __builtin_bit_cast(Words, v);
+#pragma unroll
+                for (int k = 0; k < n; ++k) {
+                    if constexpr (sizeof(W) == 2) reinterpret_cast<volatile W*>(at + to[c][i])[k] = words.w[k];      // the compiler would join them again
+                    else reinterpret_cast<W*>(at + to[c][i])[k] = words.w[k];
+                }
+            }
+    }
+    __device__ __forceinline__ void put(int t, const f32x4 (&acc)[RN][4]) const {
+        uint8_t* at = lds + (run ? t * kBytes : 0);
+        if (run && (t + 1) * kBytes > bytes) {                   // behind a row's last column the next one lies
+            const int left = (bytes - t * kBytes) / (int)sizeof(T) - 4 * (lane_id() & 15);
+#pragma unroll
+            for (int c = 0; c < RN; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < left) reinterpret_cast<T*>(at + to[c][i])[k] = (T)acc[c][k][i];
+            return;
         }
+        const uintptr_t bits = (uintptr_t)y | (uintptr_t)step;
+        if (bits % sizeof(V) == 0) put_as<V>(at, acc);
+        else if (sizeof(T) == 4 && bits % 8 == 0) put_as<uint64_t>(at, acc);
+        else if (bits % 4 == 0) put_as<uint32_t>(at, acc);
+        else if constexpr (sizeof(T) == 2) put_as<uint16_t>(at, acc);
     }
-    __device__ __forceinline__ void flush() const {
+    __device__ __forceinline__ void flush_run() const {
         wave_lds_order();
-        const int l = lane_id();
-        const int n = run ? 1 : rows, len = run ? (rows - 1) * (int)step + bytes : bytes;
-        if (run || n == 1) {
-            const int head = (int)((uintptr_t)y & 15), first = head ? 1 : 0, end = (head + len) / 16;
-            u32x4* to = reinterpret_cast<u32x4*>(y - head);
-            const u32x4* from = reinterpret_cast<const u32x4*>(lds);
-            int k = first + l;
-            for (; k + 3 * kWave < end; k += 4 * kWave) {
-                u32x4 v[4];
+        const int head = (int)((uintptr_t)y & 15), len = (rows - 1) * (int)step + bytes, end = (head + len) / 16;
+        u32x4* out = reinterpret_cast<u32x4*>(y - head);
+        const u32x4* from = reinterpret_cast<const u32x4*>(lds);
+        int k = (head ? 1 : 0) + lane_id();
+        for (; k + 3 * kWave < end; k += 4 * kWave) {
+            u32x4 v[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = from[k + u * kWave];
+            for (int u = 0; u < 4; ++u) v[u] = from[k + u * kWave];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) to[k + u * kWave] = v[u];
+            for (int u = 0; u < 4; ++u) __builtin_nontemporal_store(v[u], &out[k + u * kWave]);
+        }
+        for (; k < end; k += kWave) __builtin_nontemporal_store(from[k], &out[k]);
+        if (((uintptr_t)y | (uintptr_t)len) & 15) {
+            // lanes 0..7: what lies before the first whole piece; 8..15: behind the last; a run inside one piece that it begins, too
+            const int l = lane_id(), kk = l & 7, off = l < 8 ? head + kk * (int)sizeof(T) : 16 * end + kk * (int)sizeof(T);
+            if (l < 8 ? head && off < 16 && off < head + len : l < 16 && off < head + len && (end > 0 || !head))
+                *reinterpret_cast<T*>(y - head + off) = *reinterpret_cast<const T*>(lds + off);
+        }
+        wave_lds_order();
+    }
+    // After the t-th 64 columns.
+    __device__ __forceinline__ void flush_lines(int t, bool first, bool last) const {
+        wave_lds_order();
+        const int l = lane_id(), k = l & 7;
+        const uint8_t* mine = lds + (l >> 3) * kPitch + 16 * k;
+        char* out = y + t * kBytes;
+        if (!first && !last) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int r = (l >> 3) + 8 * j;
+                char* line = out + r * step;
+                line -= (uintptr_t)line & 127;
+#pragma unroll
+                for (int u = 0; u < kBytes / 128; ++u) {
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(mine + 8 * j * kPitch + 128 * u);
+                    if (r < rows) *reinterpret_cast<u32x4*>(line + 128 * u + 16 * k) = v;
+                }
             }
-            for (; k < end; k += kWave) to[k] = from[k];
         } else {
-            const int slots = (len + 30) / 16;                   // 16-byte pieces that a row can touch
-            const uint32_t magic = slots > 1 ? 0xFFFFFFFFu / (uint32_t)slots + 1 : 0;
-            for (int i = l; i < n * slots; i += kWave) {
-                const int r = slots > 1 ? (int)__umulhi((uint32_t)i, magic) : i, k = i - r * slots;
-                char* start = y + r * step;
-                const int head = (int)((uintptr_t)start & 15);
-                if (16 * k >= head && 16 * k + 16 <= head + len)
-                    *reinterpret_cast<u32x4*>(start - head + 16 * k) = *reinterpret_cast<const u32x4*>(lds + at(r) - head + 16 * k);
+            const int fresh = last ? bytes - t * kBytes : kBytes;
+            for (int j = 0; j < kPieces; ++j) {
+                const int r = (l >> 3) + 8 * j, head = phase(r);
+                char* line = out + r * step - head;
+                const int from = first ? head : 0, end = last ? head + fresh : kBytes;
+                if (r < rows)
+                    for (int u = 0; u <= kBytes; u += 128) {
+                        const int at = u + 16 * k;
+                        if (at >= from && at + 16 <= end) {
+                            *reinterpret_cast<u32x4*>(line + at) = *reinterpret_cast<const u32x4*>(mine + 8 * j * kPitch + u);
+                        } else if (at + 16 > from && at < end) {             // the row's first or last piece, a part of it
+                            for (int e = 0; e < 16; e += (int)sizeof(T))
+                                if (at + e >= from && at + e < end)
+                                    *reinterpret_cast<T*>(line + at + e) = *reinterpret_cast<const T*>(mine + 8 * j * kPitch + u + e);
+                        }
+                    }
             }
         }
-        if (((uintptr_t)y | (uintptr_t)len | (n > 1 ? (uintptr_t)step : 0)) & 15) {
-            // 16 lanes per run: eight elements at most before its first whole piece, eight at most behind its last
-            for (int i = l; i < n * 16; i += kWave) {
-                const int r = i / 16, k = i % 8;
-                char* start = y + r * step;
-                const int head = (int)((uintptr_t)start & 15), end = head + len;
-                const int off = i & 8 ? (end & ~15) + k * (int)sizeof(T) : head + k * (int)sizeof(T);
-                const bool mine = i & 8 ? off < end && (end >= 16 || !head) : head && off < 16 && off < end;
-                if (mine) *reinterpret_cast<T*>(start - head + off) = *reinterpret_cast<const T*>(lds + at(r) - head + off);
-            }
+        if (!last) {                                             // the begun line to where the next columns will find it
+            u32x4 v[kPieces];
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) v[j] = *reinterpret_cast<const u32x4*>(mine + 8 * j * kPitch + kBytes);
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) *reinterpret_cast<u32x4*>(const_cast<uint8_t*>(mine) + 8 * j * kPitch) = v[j];
         }
         wave_lds_order();
     }
@@ -167,9 +230,8 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     const int64_t items = (int64_t)total * parts;
     const int rv = a.rb / 16, lv = a.ls / 16;          // vectors of a row of W in memory and in LDS
     int held_group = -1, held_from = -1;
-    RowsOut<T> out;
+    RowsOut<T, RN> out;
     out.lds = ws + a.w_lds + wave * a.out_lds;
-    out.pitch = a.out_pitch;
     struct Item { int part, list, here, group; int64_t r0; };
     auto find = [&](int64_t item) {
         Item it;
@@ -212,8 +274,14 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
         const uint8_t* w = a.w + (int64_t)group * a.H * a.rb;
         const int64_t ld = a.t.ld[list];
         T* y = static_cast<T*>(a.t.y[list]) + (r0 + wave * 16 * RN) * ld;
-        out.rows = mine < 16 * RN ? mine : 16 * RN;
-        out.step = ld * (int64_t)sizeof(T);
+        if (!Lines) {
+            out.rows = mine < 16 * RN ? mine : 16 * RN;
+            out.step = ld * (int64_t)sizeof(T);
+            out.y = reinterpret_cast<char*>(y + 64 * t0);
+            out.bytes = ((64 * t1 < a.H ? 64 * t1 : a.H) - 64 * t0) * (int)sizeof(T);
+            out.run = !Stream && out.bytes == out.step && 16 * RN * out.bytes + 16 <= a.out_lds;
+            out.begin();
+        }
 
         u32x4 next[kVec];
         auto ask = [&](int t) {                        // rows 64 t .. of W
@@ -256,7 +324,6 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
                 xv[s][c] = in ? ahead[s][c] : u32x4{0, 0, 0, 0};
             }
         if (kAhead && item + share.step < share.end) { it = find(item + share.step); ask_rows(it); }
-        int c0 = 64 * t0;                              // first column of the run that is being put together
         for (int t = t0; t < t1; ++t) {
             const uint8_t* tile_w = Stream ? ws + (t & 1) * (64 * a.ls + 64) : ws + (t - t0) * 64 * a.ls;
             if (Stream && t + 1 < t1) ask(t + 1);
@@ -295,15 +362,9 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
                     for (int c = 0; c < RN; ++c) put_tile<T>(y + (16 * c + 4 * q) * ld, ld, mine - 16 * c - 4 * q, 64 * t + 4 * m, a.H, true, acc[c]);
                 }
             } else if (mine > 0) {
-                const int last = t + 1 - c0 / 64 == a.out_tiles || t + 1 == t1;
-                const int end = c0 + 64 * a.out_tiles < 64 * t1 ? c0 + 64 * a.out_tiles : 64 * t1;       // where the run ends
-                out.y = reinterpret_cast<char*>(y + c0);
-                out.bytes = ((end < a.H ? end : a.H) - c0) * (int)sizeof(T);
-                out.run = out.bytes == out.step;
-                const int h = 64 * t + 4 * m;
-#pragma unroll
-                for (int c = 0; c < RN; ++c) out.put(16 * c + 4 * q, h - c0, a.H - h, acc[c]);
-                if (last) { out.flush(); c0 = 64 * (t + 1); }
+                out.put(t - t0, acc);
+                if (!out.run) out.flush_lines(t - t0, t == t0, t + 1 == t1);
+                else if (t + 1 == t1) out.flush_run();
             }
             if (Stream) __syncthreads();
         }
@@ -723,21 +784,25 @@ static int launch_product(spp_ctx* ctx, const ProductArgs& a) {
     return SPP_OK;
 }
 constexpr int kHeldW = 65536;            // LDS for a W that stays
-constexpr int kRowOut = 768;             // bytes of Y's rows that go out whole; longer ones 512 bytes at a time
+constexpr int kRowOut = 768;             // bytes of Y's rows that go out in one run
 template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
-static int launch_rows_as(spp_ctx* ctx, ProductArgs& a, int out_tiles) {
+static int launch_rows_as(spp_ctx* ctx, ProductArgs& a) {
     auto kernel = mx4_rows_kernel<T, KS, RN, WAVES, Stream, Lines>;
-    const int ht = (a.H + 63) / 64;
+    const int ht = (a.H + 63) / 64, row = a.H * (int)sizeof(T);
     a.w_lds = Stream ? 2 * (64 * a.ls + 64) : ht * 64 * a.ls + 64;
-    a.out_tiles = out_tiles;
-    const int cols = out_tiles < ht ? 64 * out_tiles : a.H;
-    a.out_pitch = (cols * (int)sizeof(T) + 15) / 16 * 16 + 16;
-    a.out_lds = 16 * RN * a.out_pitch;
+    a.out_lds = 16 * RN * RowsOut<T, RN>::kPitch;
+    if (!Stream && row <= kRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
     const int lds = a.w_lds + (Lines ? 0 : WAVES * a.out_lds);
     if (lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     int64_t tiles = 0;
     for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)(WAVES * 16 * RN) - 1) / (WAVES * 16 * RN);
-    const int64_t want = tiles * ht, most = (int64_t)ctx->num_cu * (163840 / lds < 16 / WAVES ? 163840 / lds : 16 / WAVES);
+    // Workgroups per CU.  A stream of whole lines is fastest from few wavefronts (2.56M rows 128 -> 256: 221 us with one workgroup per CU,
+    // 245 to 250 with two to eight) once each has enough to do; with less, or two steps of columns and more to wait for (800k
+    // rows 256 -> 256: 102, 86, 92 us with one, two, three), more are better.
+    const int64_t want = tiles * ht;
+    int per_cu = WAVES >= 8 ? 2 : Lines ? (KS > 1 ? 2 : tiles >= 8 * ctx->num_cu ? 1 : 3) : 4;
+    if (per_cu > 163840 / lds) per_cu = 163840 / lds;
+    const int64_t most = (int64_t)ctx->num_cu * per_cu;
     kernel<<<(unsigned)(want < most ? want : most), 64 * WAVES, lds, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
     return SPP_OK;
@@ -748,10 +813,9 @@ static int launch_rows(spp_ctx* ctx, ProductArgs& a) {
     // Y's rows begin with a line each: stored as they come, 128 or 256 bytes of a row at a time
     bool lines = true;
     for (int j = 0; j < a.t.n_lists; ++j) lines = lines && ((uintptr_t)a.t.y[j] | (uint64_t)(a.t.ld[j] * (int64_t)sizeof(T))) % 128 == 0;
-    const int whole = a.H * (int)sizeof(T) <= kRowOut ? ht : 512 / 64 / (int)sizeof(T);
     if (ht * 64 * a.ls <= kHeldW)
-        return lines ? launch_rows_as<T, KS, 2, 4, false, true>(ctx, a, 1) : launch_rows_as<T, KS, 1, 4, false, false>(ctx, a, whole);
-    return lines ? launch_rows_as<T, KS, 2, 8, true, true>(ctx, a, 1) : launch_rows_as<T, KS, 2, 8, true, false>(ctx, a, 1);
+        return lines ? launch_rows_as<T, KS, 2, 4, false, true>(ctx, a) : launch_rows_as<T, KS, 1, 4, false, false>(ctx, a);
+    return lines ? launch_rows_as<T, KS, 2, 8, true, true>(ctx, a) : launch_rows_as<T, KS, 2, 8, true, false>(ctx, a);
 }
 constexpr int kFewRows = 64;
 template <class T>
