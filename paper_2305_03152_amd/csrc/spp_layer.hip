@@ -33,6 +33,7 @@ struct ProductArgs {
     int32_t        D, H, nb, rb;
     int32_t        ls;           // bytes of a row of W in LDS: an odd number of 16, so that 16 rows lie in banks of their own
     uint32_t       magic;        // ceil(2^32 / (rb / 16))
+    int32_t        fill;         // workgroups that few rows are dealt out to
     int32_t        w_lds;        // bytes of W in LDS; behind them, per wavefront, room for rows of Y on their way:
     int32_t        out_lds;      // bytes
 };
@@ -225,7 +226,7 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     if (total == 0) return;
     const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
     const int ht = (a.H + 63) / 64;
-    int parts = (int)gridDim.x / total;                // few rows: the columns of Y are dealt out too
+    int parts = a.fill / total;                        // few rows: the columns of Y are dealt out too
     parts = parts < 1 ? 1 : parts > ht ? ht : parts;
     const int64_t items = (int64_t)total * parts;
     const int rv = a.rb / 16, lv = a.ls / 16;          // vectors of a row of W in memory and in LDS
@@ -798,10 +799,12 @@ static int launch_rows_as(spp_ctx* ctx, ProductArgs& a) {
     for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)(WAVES * 16 * RN) - 1) / (WAVES * 16 * RN);
     // Workgroups per CU.  A stream of whole lines is fastest from few wavefronts (2.56M rows 128 -> 256: 221 us with one workgroup per CU,
     // 245 to 250 with two to eight) once each has enough to do; with less, or two steps of columns and more to wait for (800k
-    // rows 256 -> 256: 102, 86, 92 us with one, two, three), more are better.
-    const int64_t want = tiles * ht;
-    int per_cu = WAVES >= 8 ? 2 : Lines ? (KS > 1 ? 2 : tiles >= 8 * ctx->num_cu ? 1 : 3) : 4;
-    if (per_cu > 163840 / lds) per_cu = 163840 / lds;
+    // rows 256 -> 256: 102, 86, 92 us with one, two, three), more are better.  Rows of other lengths take unequal times: many
+    // workgroups even them out where there are many more tiles (2.56M rows 100 -> 172: 236 us with four per CU, 197 with
+    // sixteen; 300k rows in fp32 42 and 49).
+    a.fill = 2 * ctx->num_cu;
+    const int64_t want = tiles >= a.fill ? tiles : tiles * ht < a.fill ? tiles * ht : a.fill;
+    const int per_cu = Stream ? 2 : Lines ? (KS > 1 ? 2 : tiles >= 8 * ctx->num_cu ? 1 : 3) : tiles >= 64 * ctx->num_cu ? 16 : 4;
     const int64_t most = (int64_t)ctx->num_cu * per_cu;
     kernel<<<(unsigned)(want < most ? want : most), 64 * WAVES, lds, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
@@ -815,7 +818,7 @@ static int launch_rows(spp_ctx* ctx, ProductArgs& a) {
     for (int j = 0; j < a.t.n_lists; ++j) lines = lines && ((uintptr_t)a.t.y[j] | (uint64_t)(a.t.ld[j] * (int64_t)sizeof(T))) % 128 == 0;
     if (ht * 64 * a.ls <= kHeldW)
         return lines ? launch_rows_as<T, KS, 2, 4, false, true>(ctx, a) : launch_rows_as<T, KS, 1, 4, false, false>(ctx, a);
-    return lines ? launch_rows_as<T, KS, 2, 8, true, true>(ctx, a) : launch_rows_as<T, KS, 2, 8, true, false>(ctx, a);
+    return lines ? launch_rows_as<T, KS, 2, 8, true, true>(ctx, a) : launch_rows_as<T, KS, KS >= 4 ? 1 : 2, 8, true, false>(ctx, a);
 }
 constexpr int kFewRows = 64;
 template <class T>
