@@ -49,9 +49,6 @@ __device__ __forceinline__ i32x8 mx4_operand(u32x4 v) {
 // A lane then has four columns side by side, and the 16 lanes of a row 64: stores of whole 128-byte lines.
 __device__ __forceinline__ int tile_column(int f, int m) { return 4 * m + f; }
 
-// A vector at an address that is aligned to its elements only: one access all the same.
-template <class V> struct Loose { V v; } __attribute__((packed, aligned(2)));
-
 // Columns h .. h+3 of rows y[0..3], of which `have` are there.
 template <class T>
 __device__ __forceinline__ void put_tile(T* y, int64_t ld, int have, int h, int H, bool wide, const f32x4 (&acc)[4]) {

@@ -49,13 +49,19 @@ __device__ __forceinline__ int64_t rows_of(int64_t n, const int64_t* d_n) {
 // 4.8 to 5.5 with the tiles dealt out in order.
 struct Share {
     int64_t at, end, step;
-    __device__ __forceinline__ explicit Share(int64_t items) {
+    __device__ __forceinline__ explicit Share(int64_t items) : Share(items, 1, 0) {}
+    // The same for the wavefronts of a workgroup, side by side.
+    __device__ __forceinline__ Share(int64_t items, int waves) : Share(items, waves, (int)threadIdx.x >> 6) {}
+    __device__ __forceinline__ Share(int64_t items, int waves, int wave) {
         const unsigned groups = gridDim.x < 8 ? gridDim.x : 8, x = blockIdx.x % groups;
-        at = items * x / groups + blockIdx.x / groups;
+        at = items * x / groups + (int64_t)(blockIdx.x / groups) * waves + wave;
         end = items * (x + 1) / groups;
-        step = (gridDim.x - x + groups - 1) / groups;
+        step = (int64_t)((gridDim.x - x + groups - 1) / groups) * waves;
     }
 };
+
+// A vector at an address that is aligned to its elements only: one access all the same.
+template <class V> struct Loose { V v; } __attribute__((packed, aligned(2)));
 
 // Lists of packed rows, each with a matrix Y of its own: the operands of the product and of its gradient.
 constexpr int kRowLists = SPP_MAX_ROW_LISTS;

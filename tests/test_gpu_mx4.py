@@ -23,7 +23,7 @@ def _bytes(ctx, x, **kw):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,D", [(1, 1), (1, 32), (3, 31), (5, 33), (257, 100), (1000, 128), (513, 256), (70, 768), (2, 4096), (4099, 7), (0, 64)])
+@pytest.mark.parametrize("n,D", [(1, 1), (1, 32), (3, 31), (5, 33), (257, 100), (1000, 128), (513, 256), (70, 768), (2, 4096), (4099, 7), (0, 64), (3, 2049), (1, 3000), (1025, 4), (2, 2500)])
 def test_codes_and_scales_are_the_definition_s(ctx, dtype, n, D):
     gen = torch.Generator().manual_seed(n * 5000 + D)
     x = (torch.randn(n, D, generator=gen) * torch.exp2(torch.randint(-8, 8, (n, 1), generator=gen).float())).to(dtype)
@@ -84,7 +84,7 @@ def test_a_block_with_nan_or_infinity_is_nan_and_only_that_block(ctx, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,D", [(1, 1), (300, 100), (64, 128), (9, 800)])
+@pytest.mark.parametrize("n,D", [(1, 1), (300, 100), (64, 128), (9, 800), (1030, 4), (700, 8), (3, 4095), (2, 2500)])
 def test_values_are_those_of_the_codes(ctx, dtype, n, D):
     """All bytes of codes and scales from 2^-20 to 2^9: no rounding in fp32, one to nearest in 16 bits."""
     rng = np.random.default_rng(n * 1000 + D)
@@ -126,6 +126,30 @@ def test_a_count_on_the_device_bounds_both_ways(ctx, count, rows):
     back = torch.full((n, D), 9.0, device=DEV)
     spp.mx4_dequantize(ctx, out, D, out=back, n_device=c)
     assert np.array_equal(back[:rows].double().cpu().numpy(), R.values(out[:rows].cpu().numpy(), D)) and (back[rows:] == 9).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_every_16_bit_value_under_several_scales(ctx, dtype):
+    """All 65536 patterns, 31 at a time behind a leader that sets the block's scale; NaN and infinities among them."""
+    all_of = torch.arange(65536, dtype=torch.int32)
+    pad = -65536 % 31
+    v = torch.cat([all_of, torch.zeros(pad, dtype=torch.int32)]).view(-1, 31)
+    blocks = []
+    for lead in (0x0000, 0x0001, 0x0400, 0x3C00, 0x3F80, 0x5BFF, 0x7BFF, 0x7F7F):
+        lead = 0 if dtype == torch.float16 and lead > 0x7BFF else lead
+        blocks.append(torch.cat([torch.full((v.shape[0], 1), lead, dtype=torch.int32), v], 1))
+    x = torch.cat(blocks).to(torch.int16).view(dtype)
+    got = _bytes(ctx, x.to(DEV))
+    assert np.array_equal(got, R.quantize(x.double().numpy()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_every_code_under_every_scale(ctx, dtype):
+    rows = np.zeros((255, 32), np.uint8)
+    rows[:, :16] = np.arange(0, 256, 16) + np.arange(16)[::-1]
+    rows[:, 16] = np.arange(255)
+    got = spp.mx4_dequantize(ctx, torch.from_numpy(rows).to(DEV), 32, dtype=dtype).cpu()
+    assert torch.equal(got, torch.from_numpy(R.values(rows, 32)).to(dtype))
 
 
 def test_rows_of_a_large_array_beyond_32_bits_of_bytes(ctx):
