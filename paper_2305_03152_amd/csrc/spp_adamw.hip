@@ -36,8 +36,9 @@ struct AdamTable {
 };
 struct AdamHyper { float b1, c1, b2, c2, rs, eps, decay, step; };
 
-__device__ __forceinline__ uint32_t chunk_owner(const AdamTable& t) {
-    return (uint32_t)__builtin_amdgcn_readfirstlane(__popcll(__ballot(t.first[lane_id()] <= blockIdx.x)) - 1);
+// The tensor that a chunk is of.
+__device__ __forceinline__ uint32_t chunk_owner(const AdamTable& t, uint32_t chunk) {
+    return (uint32_t)__builtin_amdgcn_readfirstlane(__popcll(__ballot(t.first[lane_id()] <= chunk)) - 1);
 }
 
 template <class T>
@@ -59,17 +60,12 @@ __device__ __forceinline__ void store4(void* base, int64_t i, int have, bool wid
         typename Elem<T>::v4 a;
 #pragma unroll
         for (int k = 0; k < 4; ++k) a[k] = (T)x[k];
-        *reinterpret_cast<typename Elem<T>::v4*>(p) = a;
+        __builtin_nontemporal_store(a, reinterpret_cast<typename Elem<T>::v4*>(p));
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (k < have) p[k] = (T)x[k];
     }
-}
-__device__ __forceinline__ void load_any(int type, const void* base, int64_t i, int have, bool wide, float (&x)[4]) {
-    if (type == SPP_F32) load4<float>(base, i, have, wide, x);
-    else if (type == SPP_F16) load4<_Float16>(base, i, have, wide, x);
-    else load4<__bf16>(base, i, have, wide, x);
 }
 __device__ __forceinline__ void load_codes(const void* base, int64_t i, int have, bool wide, uint32_t (&c)[4]) {
     const uint8_t* p = static_cast<const uint8_t*>(base) + i;
@@ -84,23 +80,39 @@ __device__ __forceinline__ void load_codes(const void* base, int64_t i, int have
 }
 __device__ __forceinline__ void store_codes(void* base, int64_t i, int have, bool wide, const uint32_t (&c)[4]) {
     uint8_t* p = static_cast<uint8_t*>(base) + i;
-    if (have >= 4 && wide) *reinterpret_cast<uint32_t*>(p) = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+    if (have >= 4 && wide) __builtin_nontemporal_store(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, reinterpret_cast<uint32_t*>(p));
     else
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (k < have) p[k] = (uint8_t)c[k];
 }
 
-// False: the element stays as it was.
-__device__ __forceinline__ bool adam_element(const AdamHyper& h, float g, float& p, float& m, float& v) {
+// The root of v, rounded correctly: of the instruction's result r, off by less than a step, and its neighbours the one with
+// (r - step) r < v <= (r + step) r.  Below 2^-96 the products would leave the normal range: scaled by 2^32 there.
+__device__ __forceinline__ float root_of(float v) {
+    const bool tiny = v < 0x1p-96f;
+    const float x = tiny ? v * 0x1p32f : v;
+    float r = __builtin_amdgcn_sqrtf(x);
+    const float below = __uint_as_float(__float_as_uint(r) - 1), above = __uint_as_float(__float_as_uint(r) + 1);
+    const float down = __builtin_fmaf(-below, r, x), up = __builtin_fmaf(-above, r, x);
+    r = down <= 0.0f ? below : r;
+    r = up > 0.0f ? above : r;
+    r = tiny ? r * 0x1p-16f : r;
+    return v == 0.0f ? 0.0f : r;
+}
+
+// False: the element stays as it was.  root: of the v that it then has.
+__device__ __forceinline__ bool adam_element(const AdamHyper& h, float g, float& p, float& m, float& v, float& root) {
     const float m1 = m * h.b1 + g * h.c1;
     const float v1 = v * h.b2 + (g * g) * h.c2;
-    if ((__float_as_uint(v1) & 0x7F800000u) == 0x7F800000u) return false;
-    const float den = sqrtf(v1) * h.rs + h.eps;
-    p = p * h.decay - (m1 / den) * h.step;
-    m = m1;
-    v = v1;
-    return true;
+    const bool finite = (__float_as_uint(v1) & 0x7F800000u) != 0x7F800000u;
+    v = finite ? v1 : v;
+    root = root_of(v);
+    const float den = root * h.rs + h.eps;
+    const float p1 = p * h.decay - (m1 / den) * h.step;
+    p = finite ? p1 : p;
+    m = finite ? m1 : m;
+    return finite;
 }
 
 // The moments of a block as codes and back.  `most` is the largest code's value before the scale.
@@ -135,11 +147,10 @@ __device__ __forceinline__ float value_v(uint32_t c, float scale) {
 __device__ __forceinline__ float wave_max(float x) {            // of values that are not negative
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)wave_inclusive_max(__float_as_uint(x)), kWave - 1));
 }
-__device__ __forceinline__ void put_moments(const AdamTable& t, uint32_t j, int64_t i, int have, bool wide, const float (&m)[4], const float (&v)[4]) {
-    float am = 0.f, r[4], ar = 0.f;
+__device__ __forceinline__ void put_moments(const AdamTable& t, uint32_t j, int64_t i, int have, bool wide, const float (&m)[4], const float (&r)[4]) {
+    float am = 0.f, ar = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        r[k] = sqrtf(v[k]);
         am = fmaxf(am, fabsf(m[k]));
         ar = fmaxf(ar, r[k]);
     }
@@ -164,39 +175,65 @@ __device__ __forceinline__ void get_moments(const AdamTable& t, uint32_t j, int6
     for (int k = 0; k < 4; ++k) { m[k] = value_m(cm[k], sm); v[k] = value_v(cv[k], sv); }
 }
 
+// A workgroup's chunk: kAdamPer elements per thread, four at a time; all of them are asked for before any is worked on, so that
+// a wavefront's loads are under way together.  Whole: a chunk without an end in it, all arrays aligned.
+template <bool Small, class P, class G, bool Whole>
+__device__ __forceinline__ int adam_chunk(const AdamTable& t, const AdamHyper& h, uint32_t j, int64_t at, int64_t n, bool wide) {
+    constexpr int R = kAdamPer / 4;
+    float p[R][4], g[R][4], m[R][4], v[R][4];
+    int have[R];
+    int left_alone = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int64_t i = at + (r * kAdamBlock + (int)threadIdx.x) * 4, rest = n - i;
+        have[r] = Whole || rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+        // in 8 bits a wavefront has a block: all of it goes or none, and lanes behind the last element bring zeros
+        if (!Whole && (Small ? n - (i - 4 * lane_id()) <= 0 : rest <= 0)) { have[r] = -1; continue; }
+        load4<P>(t.p[j], i, have[r], Whole || wide, p[r]);
+        load4<G>(t.g[j], i, have[r], Whole || wide, g[r]);
+        if constexpr (Small) get_moments(t, j, have[r] ? i : n - 1, have[r], Whole || wide, m[r], v[r]);
+        else { load4<float>(t.m[j], i, have[r], Whole || wide, m[r]); load4<float>(t.v[j], i, have[r], Whole || wide, v[r]); }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (!Whole && have[r] < 0) continue;
+        const int64_t i = at + (r * kAdamBlock + (int)threadIdx.x) * 4;
+        float root[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) left_alone += adam_element(h, g[r][k], p[r][k], m[r][k], v[r][k], root[k]) ? 0 : 1;
+        store4<P>(t.p[j], i, have[r], Whole || wide, p[r]);
+        if constexpr (Small) put_moments(t, j, i, have[r], Whole || wide, m[r], root);
+        else { store4<float>(t.m[j], i, have[r], Whole || wide, m[r]); store4<float>(t.v[j], i, have[r], Whole || wide, v[r]); }
+    }
+    return left_alone;
+}
+template <bool Small, class P, class G>
+__device__ __forceinline__ int adam_chunk(const AdamTable& t, const AdamHyper& h, uint32_t j, int64_t at, int64_t n, bool wide) {
+    return wide && n - at >= kAdamChunk ? adam_chunk<Small, P, G, true>(t, h, j, at, n, true) : adam_chunk<Small, P, G, false>(t, h, j, at, n, wide);
+}
+
 template <bool Small>
 __global__ void __launch_bounds__(kAdamBlock) adamw_kernel(AdamTable t, AdamHyper h, int64_t* skipped) {
-    const uint32_t j = chunk_owner(t);
-    const int64_t n = t.n[j], at = (int64_t)(blockIdx.x - t.first[j]) * kAdamChunk;
+    const uint32_t chunk = blockIdx.x, j = chunk_owner(t, chunk);
+    const int64_t n = t.n[j], at = (int64_t)(chunk - t.first[j]) * kAdamChunk;
     const int kind = t.kind[j];
     const bool wide = kind & 16;
     int left_alone = 0;
-#pragma unroll
-    for (int round = 0; round < kAdamPer / 4; ++round) {
-        const int64_t i = at + (round * kAdamBlock + (int)threadIdx.x) * 4;
-        const int64_t rest = n - i;
-        // in 8 bits a wavefront has a block: all of it goes or none, and lanes behind the last element bring zeros
-        if (Small ? n - (i - 4 * lane_id()) <= 0 : rest <= 0) break;
-        const int have = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
-        float p[4], g[4], m[4], v[4];
-        load_any(kind & 3, t.p[j], i, have, wide, p);
-        load_any((kind >> 2) & 3, t.g[j], i, have, wide, g);
-        if constexpr (Small) get_moments(t, j, have ? i : n - 1, have, wide, m, v);
-        else { load4<float>(t.m[j], i, have, wide, m); load4<float>(t.v[j], i, have, wide, v); }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) left_alone += !adam_element(h, g[k], p[k], m[k], v[k]);
-        if ((kind & 3) == SPP_F32) store4<float>(t.p[j], i, have, wide, p);
-        else store4<__bf16>(t.p[j], i, have, wide, p);
-        if constexpr (Small) put_moments(t, j, i, have, wide, m, v);
-        else { store4<float>(t.m[j], i, have, wide, m); store4<float>(t.v[j], i, have, wide, v); }
+    switch (kind & 15) {
+        case SPP_F32 | SPP_F32 << 2: left_alone = adam_chunk<Small, float, float>(t, h, j, at, n, wide); break;
+        case SPP_F32 | SPP_F16 << 2: left_alone = adam_chunk<Small, float, _Float16>(t, h, j, at, n, wide); break;
+        case SPP_F32 | SPP_BF16 << 2: left_alone = adam_chunk<Small, float, __bf16>(t, h, j, at, n, wide); break;
+        case SPP_BF16 | SPP_F32 << 2: left_alone = adam_chunk<Small, __bf16, float>(t, h, j, at, n, wide); break;
+        case SPP_BF16 | SPP_F16 << 2: left_alone = adam_chunk<Small, __bf16, _Float16>(t, h, j, at, n, wide); break;
+        case SPP_BF16 | SPP_BF16 << 2: left_alone = adam_chunk<Small, __bf16, __bf16>(t, h, j, at, n, wide); break;
     }
     if (left_alone) atomicAdd(reinterpret_cast<unsigned long long*>(skipped), (unsigned long long)left_alone);
 }
 
-// Moments in 8 bits from fp32 arrays, and back.  t.p: fp32 m, t.g: fp32 v.
+// m and the root of v, as codes, from fp32 arrays, and back.  t.p: fp32 m, t.g: fp32 v.
 __global__ void __launch_bounds__(kAdamBlock) adamw_load_kernel(AdamTable t) {
-    const uint32_t j = chunk_owner(t);
-    const int64_t n = t.n[j], at = (int64_t)(blockIdx.x - t.first[j]) * kAdamChunk;
+    const uint32_t chunk = blockIdx.x, j = chunk_owner(t, chunk);
+    const int64_t n = t.n[j], at = (int64_t)(chunk - t.first[j]) * kAdamChunk;
     const bool wide = t.kind[j] & 16;
     for (int round = 0; round < kAdamPer / 4; ++round) {
         const int64_t i = at + (round * kAdamBlock + (int)threadIdx.x) * 4;
@@ -209,13 +246,14 @@ __global__ void __launch_bounds__(kAdamBlock) adamw_load_kernel(AdamTable t) {
         for (int k = 0; k < 4; ++k) {                       // what no step can have left there counts as zero
             if ((__float_as_uint(m[k]) & 0x7F800000u) == 0x7F800000u) m[k] = 0.0f;
             if (!(v[k] >= 0.0f) || (__float_as_uint(v[k]) & 0x7F800000u) == 0x7F800000u) v[k] = 0.0f;
+            v[k] = root_of(v[k]);
         }
         put_moments(t, j, i, have, wide, m, v);
     }
 }
 __global__ void __launch_bounds__(kAdamBlock) adamw_values_kernel(AdamTable t) {
-    const uint32_t j = chunk_owner(t);
-    const int64_t n = t.n[j], at = (int64_t)(blockIdx.x - t.first[j]) * kAdamChunk;
+    const uint32_t chunk = blockIdx.x, j = chunk_owner(t, chunk);
+    const int64_t n = t.n[j], at = (int64_t)(chunk - t.first[j]) * kAdamChunk;
     const bool wide = t.kind[j] & 16;
 #pragma unroll
     for (int round = 0; round < kAdamPer / 4; ++round) {

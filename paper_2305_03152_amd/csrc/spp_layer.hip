@@ -512,10 +512,8 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
     const int total = lists.total();
     const int splits = a.splits < total ? a.splits : total;
     const int tiles = (int)gridDim.x / a.splits;
-    // consecutive workgroups go to the eight XCDs in turn: an XCD takes a contiguous part of (run, tile), so that the tiles
-    // of a run, which read the same rows, share its L2
-    const int per = (int)gridDim.x / 8, more = (int)gridDim.x % 8, xcd = (int)blockIdx.x % 8;
-    const int id = xcd * per + (xcd < more ? xcd : more) + (int)blockIdx.x / 8;
+    // the tiles of a run, which read the same rows, share an XCD's L2
+    const int id = (int)own_piece();
     const int tile = id % tiles, split = id / tiles;
     if (split >= splits) return;
     const int from = (int)((int64_t)split * total / splits), to = (int)((int64_t)(split + 1) * total / splits);

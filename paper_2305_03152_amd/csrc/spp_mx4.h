@@ -53,12 +53,18 @@ struct Share {
     // The same for the wavefronts of a workgroup, side by side.
     __device__ __forceinline__ Share(int64_t items, int waves) : Share(items, waves, (int)threadIdx.x >> 6) {}
     __device__ __forceinline__ Share(int64_t items, int waves, int wave) {
-        const unsigned groups = gridDim.x < 8 ? gridDim.x : 8, x = blockIdx.x % groups;
-        at = items * x / groups + (int64_t)(blockIdx.x / groups) * waves + wave;
-        end = items * (x + 1) / groups;
-        step = (int64_t)((gridDim.x - x + groups - 1) / groups) * waves;
+        const bool all = gridDim.x >= 8;
+        const unsigned x = all ? blockIdx.x & 7 : 0;
+        at = (all ? items * x >> 3 : 0) + (int64_t)(all ? blockIdx.x >> 3 : blockIdx.x) * waves + wave;
+        end = all ? items * (x + 1) >> 3 : items;
+        step = (int64_t)(all ? (gridDim.x - x + 7) >> 3 : gridDim.x) * waves;
     }
 };
+// The same with as many pieces as there are workgroups: a workgroup's one.
+__device__ __forceinline__ unsigned own_piece() {
+    const unsigned x = blockIdx.x & 7, more = gridDim.x & 7;
+    return x * (gridDim.x >> 3) + (x < more ? x : more) + (blockIdx.x >> 3);
+}
 
 // A vector at an address that is aligned to its elements only: one access all the same.
 template <class V> struct Loose { V v; } __attribute__((packed, aligned(2)));
