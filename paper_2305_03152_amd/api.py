@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import atexit
 import ctypes as C
+import functools
 import os
 import sys
 import threading
@@ -746,8 +747,11 @@ def _type(dtype, name: str) -> int:
 
 def _new(ctx: Context, shape, dtype) -> torch.Tensor:
     """Memory of the context's stream, which is where it is written (torch's allocator goes by the stream)."""
+    dev = ctx.stream.device
+    if torch.cuda.current_stream(ctx.device) == ctx.stream:
+        return torch.empty(shape, dtype=dtype, device=dev)
     with torch.cuda.stream(ctx.stream):
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", ctx.device))
+        return torch.empty(shape, dtype=dtype, device=dev)
 
 
 def _matrix(t: torch.Tensor, cols: Optional[int], name: str) -> torch.Tensor:
@@ -770,11 +774,15 @@ def _packed(t: torch.Tensor, D: int, name: str) -> torch.Tensor:
 
 
 def _count(t: Optional[torch.Tensor], name: str = "n_device"):
-    if t is not None and not (t.is_cuda and t.dtype == torch.int64 and t.numel() == 1):
+    """Address of a count on the GPU, or None."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == torch.int64 and t.numel() == 1):
         raise SppError(f"{name} must be one int64 on the GPU")
-    return t
+    return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=None)
 def mx4_row_bytes(D: int) -> int:
     """Bytes of a row of D columns in MXFP4: 17 per block of 32 columns, rounded up to a multiple of 16."""
     rb = load_library().spp_mx4_row_bytes(int(D))
@@ -798,7 +806,7 @@ def mx4_quantize(ctx: Context, x: torch.Tensor, out: Optional[torch.Tensor] = No
         out = _new(ctx, (n, rb), torch.uint8)
     elif _packed(out, D, "out").dim() != 2 or out.shape[0] < n:
         raise SppError("out is too small")
-    _check(load_library().spp_mx4_quantize(ctx._h, _ptr(x), ty, n, _ptr(_count(n_device)), D, _ld(x), _ptr(out), SPP_SYNC if sync else 0))
+    _check(load_library().spp_mx4_quantize(ctx._h, x.data_ptr(), ty, n, _count(n_device), D, _ld(x), out.data_ptr(), SPP_SYNC if sync else 0))
     return out
 
 
@@ -813,7 +821,7 @@ def mx4_dequantize(ctx: Context, rows: torch.Tensor, D: int, dtype: torch.dtype 
         out = _new(ctx, (n, D), dtype)
     elif _matrix(out, D, "out").shape[0] < n:
         raise SppError("out is too small")
-    _check(load_library().spp_mx4_dequantize(ctx._h, _ptr(rows), n, _ptr(_count(n_device)), D, _ptr(out), _type(out.dtype, "out"), _ld(out),
+    _check(load_library().spp_mx4_dequantize(ctx._h, rows.data_ptr(), n, _count(n_device), D, out.data_ptr(), _type(out.dtype, "out"), _ld(out),
                                              SPP_SYNC if sync else 0))
     return out
 
@@ -848,9 +856,8 @@ class RowLists:
                 raise SppError(f"list {j}: n exceeds its rows or its y")
             if group < 0:
                 raise SppError(f"list {j}: group {group}")
-            _count(n_dev, f"n_device of list {j}")
             a = self._arr[j]
-            a.d_rows, a.n, a.d_n, a.d_y = rows.data_ptr(), int(n), n_dev.data_ptr() if n_dev is not None else None, y.data_ptr()
+            a.d_rows, a.n, a.d_n, a.d_y = rows.data_ptr(), int(n), _count(n_dev, f"n_device of list {j}"), y.data_ptr()
             a.ld, a.group = _ld(y), group
             self.groups = max(self.groups, group + 1)
 
@@ -873,7 +880,7 @@ def mx4_product_multi(ctx: Context, lists, weights: torch.Tensor, D: int, sync: 
     groups, H = (1, weights.shape[0]) if weights.dim() == 2 else weights.shape[:2]
     lists._fit(D, H, groups)
     if lists.lists:
-        _check(load_library().spp_mx4_product(ctx._h, lists._arr, len(lists.lists), _ptr(weights), groups, D, H, _TYPES[lists.dtype],
+        _check(load_library().spp_mx4_product(ctx._h, lists._arr, len(lists.lists), weights.data_ptr(), groups, D, H, _TYPES[lists.dtype],
                                               SPP_SYNC if sync else 0))
     elif sync:
         ctx.sync()
@@ -906,7 +913,7 @@ def mx4_weight_grad(ctx: Context, lists, H: int, D: int, groups: int = 1, out: O
     elif _dev(out, torch.float32, "out").numel() != groups * H * D:
         raise SppError("out must hold groups * H * D values")
     _check(load_library().spp_mx4_weight_grad(ctx._h, lists._arr, len(lists.lists), groups, D, H, _TYPES[lists.dtype or torch.float32],
-                                              _ptr(out), SPP_SYNC if sync else 0))
+                                              out.data_ptr(), SPP_SYNC if sync else 0))
     return out
 
 
@@ -926,7 +933,7 @@ class AdamW:
         self.params = list(params)
         dev = torch.device("cuda", ctx.device)
         self._arr = (_AdamwTensor * max(len(self.params), 1))()
-        self._state = []
+        self._state, self._items = [], []
         with torch.cuda.stream(ctx.stream):
             for j, p in enumerate(self.params):
                 if not (p.is_cuda and p.is_contiguous() and p.dtype in (torch.float32, torch.bfloat16)):
@@ -940,15 +947,17 @@ class AdamW:
                 a = self._arr[j]
                 a.d_p, a.n, a.p_type = p.data_ptr(), n, _TYPES[p.dtype]
                 a.d_m, a.d_v, a.d_scale = s[0].data_ptr(), s[1].data_ptr(), s[2].data_ptr() if blocks else None
+                self._items.append((a, p, n))
+        self._views = tuple([s[k].view(p.shape) for s, p in zip(self._state, self.params)] for k in (0, 1)) if state_bits == 32 else None
 
     def step(self, grads: Sequence[torch.Tensor], lr: Optional[float] = None, sync: bool = True):
         """One step with a gradient (any of the three types) for every parameter."""
         if len(grads) != len(self.params):
             raise SppError("one gradient per parameter is needed")
-        for j, (p, g) in enumerate(zip(self.params, grads)):
-            if not (g.is_cuda and g.is_contiguous() and g.numel() == p.numel()):
-                raise SppError(f"gradient {j} must be a contiguous tensor on the GPU of its parameter's size")
-            self._arr[j].d_p, self._arr[j].d_g, self._arr[j].g_type = p.data_ptr(), g.data_ptr(), _type(g.dtype, f"gradient {j}")
+        for (a, p, n), g in zip(self._items, grads):
+            if not (g.is_cuda and g.is_contiguous() and g.numel() == n and g.dtype in _TYPES):
+                raise SppError("a gradient must be a contiguous float32, float16 or bfloat16 tensor on the GPU of its parameter's size")
+            a.d_p, a.d_g, a.g_type = p.data_ptr(), g.data_ptr(), _TYPES[g.dtype]
         h = _AdamwHyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.weight_decay)
         _check(load_library().spp_adamw_step(self.ctx._h, self._arr, len(self.params), self.state_bits, C.byref(h), self.t + 1,
                                              SPP_SYNC if sync else 0))
@@ -963,7 +972,7 @@ class AdamW:
         if self.state_bits == 32:
             if sync:
                 self.ctx.sync()
-            return [s[0].view(p.shape) for s, p in zip(self._state, self.params)], [s[1].view(p.shape) for s, p in zip(self._state, self.params)]
+            return list(self._views[0]), list(self._views[1])
         m = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
         v = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
         pm, pv = self._moments(m, v)

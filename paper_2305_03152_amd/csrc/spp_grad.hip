@@ -1,0 +1,361 @@
+// The gradient of the layer that reads feature rows in MXFP4 by its weights, over the product's lists:
+//
+//   dW[g] = sum over the lists j of group g of dY_j^T X_j        dY_j [n_j, H] fp32, fp16 or bf16, X_j [n_j, D] in MXFP4, dW fp32
+//
+// What a code and a scale stand for is exact in bf16, as is an fp32 as the sum of three bf16 and an fp16 of two: the products of the
+// matrix instruction are exact and are added in fp32, the sums of the runs in 64 bits.
+#include "spp_mx4.h"
+
+namespace spp {
+
+// The rows of all lists, in the order of their groups, are cut into chunks, and the chunks into `splits` runs of equal length.  A
+// workgroup has one run and one tile of dW; where its run passes from a group to the next it writes down what it has as piece
+// (run + group) and starts again, and the second kernel adds up each group's pieces in the order of the rows.  No atomics: the
+// same counts give the same bits.
+//
+// Both operands have the rows as the axis that is summed over, so their tiles lie in LDS as they lie in memory and are read
+// transposed (ds_read_b64_tr_b16).  A chunk's operands are asked for two chunks ahead, into registers; X is unpacked to bf16 on
+// its way to LDS, dY cut into its pieces.
+constexpr int kGradPad = 16;         // elements behind an LDS row: the four rows that 16 lanes read at once are then 4 x 32 bytes of other banks
+
+struct GradArgs {
+    RowTable t;
+    float*   pieces;       // [splits + groups][H * D]
+    float*   dw;           // [groups][H * D]
+    int32_t  D, H, nb, rb;
+    int32_t  splits, tiles_d;
+    int32_t  chunk;        // rows of a chunk
+};
+
+// dY as bf16 numbers that add up to it exactly: one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
+// finite value becomes infinite; what is not finite is its first piece alone.
+template <class T> struct Pieces { static constexpr int n = 1; };
+template <> struct Pieces<_Float16> { static constexpr int n = 2; };
+template <> struct Pieces<float> { static constexpr int n = 3; };
+template <int P, bool Finite>
+__device__ __forceinline__ void cut(float x, __bf16 (&out)[P]) {
+    const bool finite = Finite || (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const uint32_t head = __float_as_uint(x) & 0xFFFF0000u;
+        out[p] = p == 0 && !finite ? (__bf16)x : __builtin_bit_cast(__bf16, (uint16_t)(head >> 16));
+        x = finite ? x - __uint_as_float(head) : 0.0f;
+    }
+}
+
+// Eight rows of the lane's column, four and the four sixteen rows on: of 16 lanes, lane i names row i/4 and columns 4 (i mod 4) ..,
+// and gets column i of four rows.  The wavefront's 64 lanes so read 16 rows that follow each other, 32 lanes eight: with
+// the pad behind each row these are 256 bytes of different banks.  In what order the 32 rows are summed is the same to both operands.
+template <int LD>
+__device__ __forceinline__ bf16x8 column8(const __bf16* p) {
+    typedef __attribute__((address_space(3))) i16x4* lds4;
+    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p));
+    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 16 * LD));
+    const bf16x4 x = __builtin_bit_cast(bf16x4, a), y = __builtin_bit_cast(bf16x4, b);
+    return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+}
+
+template <class T, int WH, int WD, int FH>
+struct GradShape {
+    static constexpr int P = Pieces<T>::n;
+    static constexpr int rows = P == 1 ? 64 : 32;                    // of a chunk: two buffers of it fit the LDS
+    static constexpr int threads = 64 * WH * WD;
+    static constexpr int th = 16 * FH * WH, td = 64 * WD;            // the tile of dW: a wavefront has 16 FH x 64 of it
+    static constexpr int ly = th + kGradPad, lx = td + kGradPad;     // elements of an LDS row
+    static constexpr int buffer = rows * (P * ly + lx);              // elements of a buffer
+    static constexpr int lds = 2 * buffer * 2;
+    static constexpr int ve = 16 / (int)sizeof(T);                   // elements of a 16-byte vector of dY
+    static constexpr int ahead = FH > 4 ? 1 : 2;                     // chunks in registers: the largest tile leaves room for one
+    static constexpr int ny = rows * th / ve / threads;              // vectors of dY, blocks of X per thread and chunk
+    static constexpr int nx = (rows * 2 * WD + threads - 1) / threads;
+};
+
+template <class T, int WH, int WD, int FH>
+__global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
+    typedef GradShape<T, WH, WD, FH> S;
+    constexpr int P = S::P;
+    extern __shared__ __attribute__((aligned(16))) __bf16 lds[];
+    const Lists lists(a.t, S::rows);
+    const int total = lists.total();
+    const int splits = a.splits < total ? a.splits : total;
+    const int tiles = (int)gridDim.x / a.splits;
+    // the tiles of a run, which read the same rows, share an XCD's L2
+    const int id = (int)own_piece();
+    const int tile = id % tiles, split = id / tiles;
+    if (split >= splits) return;
+    const int from = (int)((int64_t)split * total / splits), to = (int)((int64_t)(split + 1) * total / splits);
+    const int h0 = tile / a.tiles_d * S::th, d0 = tile % a.tiles_d * S::td;
+    const int wave = threadIdx.x >> 6, l = lane_id();
+    const int wh = wave / WD * (16 * FH), wd = wave % WD * 64;
+
+    u32x4 ry[S::ahead][S::ny], rx[S::ahead][S::nx];
+    uint32_t rs[S::ahead][S::nx];
+    int here[S::ahead], group[S::ahead];
+
+    auto load = [&](int u, int chunk) {
+        const int list = lists.list_of(chunk);
+        const int64_t r0 = (int64_t)(chunk - lists.first_tile(list)) * S::rows;
+        const int64_t left = lists.rows_in(list) - r0;
+        here[u] = left < S::rows ? (int)left : S::rows;
+        group[u] = a.t.group[list];
+        const int64_t ld = a.t.ld[list];
+        const T* y = static_cast<const T*>(a.t.y[list]) + r0 * ld;
+        const uint8_t* x = a.t.rows[list] + r0 * a.rb;
+        // Rows behind the last and columns behind H or D: others in their place; put() clears the rows, and those columns of dW
+        // are not written.  A vector may reach over a row's end into the next row, but not over the list's.
+        const bool wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0 && a.H % S::ve == 0;
+        if (ld < (1 << 24) && (wide || (left > S::rows && a.H >= S::ve))) {
+            uint32_t off[S::ny];
+#pragma unroll
+            for (int k = 0; k < S::ny; ++k) {
+                const int i = k * S::threads + (int)threadIdx.x;
+                int r = i / (S::th / S::ve), h = h0 + i % (S::th / S::ve) * S::ve;
+                r = r < here[u] ? r : here[u] - 1;
+                off[k] = (uint32_t)(r * (int)ld + (h < a.H ? h : 0));
+            }
+            if (wide)
+#pragma unroll
+                for (int k = 0; k < S::ny; ++k) ry[u][k] = *reinterpret_cast<const u32x4*>(y + off[k]);
+            else
+#pragma unroll
+                for (int k = 0; k < S::ny; ++k) ry[u][k] = reinterpret_cast<const Loose<u32x4>*>(y + off[k])->v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < S::ny; ++k) {
+                const int i = k * S::threads + (int)threadIdx.x;
+                int r = i / (S::th / S::ve);
+                const int h = h0 + i % (S::th / S::ve) * S::ve;
+                r = r < here[u] ? r : here[u] - 1;
+                T v[S::ve];
+#pragma unroll
+                for (int j = 0; j < S::ve; ++j) v[j] = y[r * ld + (h + j < a.H ? h + j : a.H - 1)];
+                ry[u][k] = __builtin_bit_cast(u32x4, v);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < S::nx; ++k) {
+            const int i = k * S::threads + (int)threadIdx.x;
+            int r = i / (2 * WD), b = d0 / 32 + i % (2 * WD);
+            r = r < here[u] ? r : here[u] - 1;
+            b = b < a.nb ? b : a.nb - 1;
+            const uint8_t* p = x + r * a.rb;
+            rx[u][k] = *reinterpret_cast<const u32x4*>(p + 16 * b);
+            rs[u][k] = p[16 * a.nb + b];
+        }
+    };
+    auto put = [&](int u, int buffer) {
+        __bf16* gy = lds + buffer * S::buffer;
+        __bf16* gx = gy + P * S::rows * S::ly;
+#pragma unroll
+        for (int k = 0; k < S::ny; ++k) {
+            const int i = k * S::threads + (int)threadIdx.x;
+            const int r = i / (S::th / S::ve), h = i % (S::th / S::ve) * S::ve;
+            const u32x4 raw = r < here[u] ? ry[u][k] : u32x4{0, 0, 0, 0};
+            if constexpr (P == 1) {
+                *reinterpret_cast<u32x4*>(gy + r * S::ly + h) = raw;
+            } else {
+                struct Vec { T v[S::ve]; } in = __builtin_bit_cast(Vec, raw);
+                struct Cut { __bf16 v[S::ve]; } out[P];
+                auto each = [&](auto finite) {
+#pragma unroll
+                    for (int j = 0; j < S::ve; ++j) {
+                        __bf16 c[P];
+                        cut<P, decltype(finite)::value>((float)in.v[j], c);
+#pragma unroll
+                        for (int p = 0; p < P; ++p) out[p].v[j] = c[p];
+                    }
+                };
+                float top = 0.0f;                          // infinite or NaN if any of them is
+#pragma unroll
+                for (int j = 0; j < S::ve; ++j) top += fabsf((float)in.v[j]) * 0x1p-8f;
+                if (__any((__float_as_uint(top) & 0x7F800000u) == 0x7F800000u)) each(std::false_type());
+                else each(std::true_type());
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    if constexpr (S::ve == 8) *reinterpret_cast<u32x4*>(gy + (p * S::rows + r) * S::ly + h) = __builtin_bit_cast(u32x4, out[p]);
+                    else *reinterpret_cast<u32x2*>(gy + (p * S::rows + r) * S::ly + h) = __builtin_bit_cast(u32x2, out[p]);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < S::nx; ++k) {
+            const int i = k * S::threads + (int)threadIdx.x;
+            const int r = i / (2 * WD);
+            if (S::rows * 2 * WD % S::threads && r >= S::rows) continue;
+            const float s = r < here[u] ? mx4_scale(rs[u][k]) : 0.0f;
+            u32x4 c = r < here[u] ? rx[u][k] : u32x4{0, 0, 0, 0};
+            // 16 lanes' pieces of 16 bytes, 64 bytes apart, in banks of their own: half of the lanes begin with the second
+            const int turn = WD == 2 ? (l >> 3) & 1 : (l >> 2) & 1;
+            c = turn ? u32x4{c.y, c.z, c.w, c.x} : c;
+            __bf16* to_x = gx + r * S::lx + i % (2 * WD) * 32;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 1),
+                             v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 3);
+                *reinterpret_cast<bf16x8*>(to_x + 8 * ((j + turn) & 3)) = bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+            }
+        }
+    };
+
+    f32x4 acc[FH][4];
+    auto clear = [&]() {
+#pragma unroll
+        for (int f = 0; f < FH; ++f)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    auto flush = [&](int g) {
+        // from values made anew: addresses worked out ahead of the loop would take the registers that it needs
+        const int lane = spp::here(l);
+        float* out = a.pieces + (int64_t)(split + g) * a.H * a.D;
+#pragma unroll
+        for (int f = 0; f < FH; ++f)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int h = h0 + wh + 16 * f + 4 * (lane >> 4) + i, d = d0 + wd + 16 * c + (lane & 15);
+                    if (h < a.H && d < a.D) out[(int64_t)h * a.D + d] = acc[f][c][i];
+                }
+    };
+    const int n = to - from;
+    load(0, from);
+    if (S::ahead > 1 && n > 1) load(S::ahead - 1, from + 1);
+    clear();
+    int now = group[0];
+    for (int j = 0; j < n; j += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (j + u >= n) break;
+            constexpr int mask = S::ahead - 1;
+            if (group[u & mask] != now) { flush(now); clear(); now = group[u & mask]; }
+            put(u & mask, u);
+            __syncthreads();         // the other buffer has been read by all before this one is read by any
+            if (j + u + S::ahead < n) load(u & mask, from + j + u + S::ahead);
+            const __bf16* gy = lds + u * S::buffer;
+            const __bf16* gx = gy + P * S::rows * S::ly;
+#pragma unroll
+            for (int k = 0; k < S::rows; k += 32) {
+                const int row = k + 4 * (l >> 4) + ((l & 15) >> 2), col = 4 * (l & 3);
+                bf16x8 bx[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) bx[c] = column8<S::lx>(gx + row * S::lx + col + wd + 16 * c);
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int f = 0; f < FH; ++f) {
+                        const bf16x8 ay = column8<S::ly>(gy + (p * S::rows + row) * S::ly + col + wh + 16 * f);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ay, bx[c], acc[f][c], 0, 0, 0);
+                    }
+            }
+        }
+    }
+    flush(now);
+}
+
+// The pieces of 64 elements side by side are added by a workgroup's wavefronts in turn, then the wavefronts' sums: always in the same
+// order.
+constexpr int kSumWaves = 16;
+__global__ void __launch_bounds__(64 * kSumWaves) mx4_grad_sum_kernel(GradArgs a) {
+    __shared__ double part[kSumWaves][kWave];
+    const Lists lists(a.t, a.chunk);
+    const int total = lists.total(), group = blockIdx.y, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, l = lane_id();
+    const int splits = a.splits < total ? a.splits : total;
+    const int64_t size = (int64_t)a.H * a.D;
+    // the chunks of the group: from its first list's first to its last list's last
+    const uint64_t mine = __ballot(l < a.t.n_lists && (int)a.t.group[l] == group && lists.tiles > 0);
+    int lo = 0, hi = -1;
+    if (mine) {
+        const int first = lists.first_tile(__builtin_ctzll(mine)), last = __builtin_amdgcn_readlane(lists.upto, 63 - __builtin_clzll(mine)) - 1;
+        lo = (int)((((int64_t)first + 1) * splits - 1) / total);
+        hi = (int)((((int64_t)last + 1) * splits - 1) / total);
+    }
+    for (int64_t i0 = (int64_t)blockIdx.x * kWave; i0 < size; i0 += (int64_t)gridDim.x * kWave) {
+        const int64_t i = i0 + l;
+        const float* p = a.pieces + group * size + (i < size ? i : size - 1);
+        double sum = 0.0;
+        int s = lo + wave;
+        for (; s + 7 * waves <= hi; s += 8 * waves) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p[(int64_t)(s + k * waves) * size];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[k];
+        }
+        for (; s <= hi; s += waves) sum += p[(int64_t)s * size];
+        __syncthreads();
+        part[wave][l] = sum;
+        __syncthreads();
+        if (wave == 0 && i < size) {
+            for (int k = 1; k < waves; ++k) sum += part[k][l];
+            a.dw[group * size + i] = (float)sum;
+        }
+    }
+}
+
+template <class T, int WH, int WD, int FH>
+static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
+    typedef GradShape<T, WH, WD, FH> S;
+    auto kernel = mx4_grad_kernel<T, WH, WD, FH>;
+    static LdsLimit limit;
+    a.chunk = S::rows;
+    a.tiles_d = (a.D + S::td - 1) / S::td;
+    const int64_t tiles = (int64_t)a.tiles_d * ((a.H + S::th - 1) / S::th), size = (int64_t)a.H * a.D;
+    int64_t chunks = 0;
+    for (int j = 0; j < a.t.n_lists; ++j) chunks += (a.t.n[j] + (int64_t)S::rows - 1) / S::rows;
+    // as many workgroups as run at once, and two chunks for each
+    const int fit = 163840 / S::lds, wish = 8 / (WH * WD);
+    const int64_t at_once = (int64_t)ctx->num_cu * (fit < 1 || wish < 1 ? 1 : fit < wish ? fit : wish);
+    int64_t splits = at_once / tiles;
+    if (splits > (chunks + 1) / 2) splits = (chunks + 1) / 2;
+    a.splits = (int32_t)(splits < 1 ? 1 : splits);
+    SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float)));
+    a.pieces = ctx->gradws.as<float>();
+    if (!sum_only) {
+        SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), S::lds));
+        kernel<<<(unsigned)(a.splits * tiles), S::threads, S::lds, ctx->stream>>>(a);
+        SPP_HIP(hipGetLastError());
+    }
+    const int64_t sums = (size + kWave - 1) / kWave;
+    const int waves = a.splits > 64 ? kSumWaves : a.splits > 16 ? 8 : 4;
+    mx4_grad_sum_kernel<<<dim3((unsigned)(sums < 65536 ? sums : 65536), n_groups), 64 * waves, 0, ctx->stream>>>(a);
+    SPP_HIP(hipGetLastError());
+    return SPP_OK;
+}
+// Tiles of dW: as few as 256 x 256 (128 columns of up to 64 wavefront pairs) allow, of as few wavefronts as these need.  The larger
+// the tile, the less is read from LDS per product and the less often dY and X are read.
+template <class T>
+static int grad_of(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
+    const int tiles = (a.H + 255) / 256, h = (a.H + tiles - 1) / tiles;
+    if (a.D > 128) {
+        if (h > 128) return launch_grad<T, 2, 4, 8>(ctx, a, n_groups, sum_only);
+        return h > 64 ? launch_grad<T, 2, 4, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 1, 4, 4>(ctx, a, n_groups, sum_only);
+    }
+    if (a.D > 64) {
+        if (h > 128) return h > 192 ? launch_grad<T, 4, 2, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 3, 2, 4>(ctx, a, n_groups, sum_only);
+        return h > 64 ? launch_grad<T, 2, 2, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 1, 2, 4>(ctx, a, n_groups, sum_only);
+    }
+    if (h > 128) return h > 192 ? launch_grad<T, 4, 1, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 3, 1, 4>(ctx, a, n_groups, sum_only);
+    return h > 64 ? launch_grad<T, 2, 1, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 1, 1, 4>(ctx, a, n_groups, sum_only);
+}
+
+}  // namespace spp
+
+extern "C" int spp_mx4_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H,
+                                   int32_t type, float* d_grad, uint32_t flags) {
+    using namespace spp;
+    SPP_CHECK(ctx && d_grad, SPP_E_ARG, "spp_mx4_weight_grad: null argument");
+    SPP_CHECK((uintptr_t)d_grad % 4 == 0, SPP_E_ARG, "spp_mx4_weight_grad: the gradient must be 4-byte aligned");
+    GradArgs a;
+    int64_t most = 0;
+    SPP_TRY(row_table("spp_mx4_weight_grad", lists, n_lists, n_groups, D, H, type, a.t, &most));
+    SPP_HIP(hipSetDevice(ctx->device));
+    a.dw = d_grad; a.D = D; a.H = H; a.nb = mx4_blocks(D); a.rb = mx4_bytes(D);
+    hipStream_t st = ctx->stream;
+    ScopedTimer timer(ctx, SPP_T_LAYER, st);
+    SPP_TRY(type == SPP_F32 ? grad_of<float>(ctx, a, n_groups, most == 0) : type == SPP_F16 ? grad_of<_Float16>(ctx, a, n_groups, most == 0)
+                                                                                          : grad_of<__bf16>(ctx, a, n_groups, most == 0));
+    if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(st));
+    return SPP_OK;
+}

@@ -1,29 +1,13 @@
-// The layer that reads feature rows in MXFP4, and its gradient, over up to 64 lists of rows whose lengths may be known on the
-// device only (the minibatches that a pipeline keeps in flight; rows of several kinds, each kind with a matrix of its own):
+// The layer that reads feature rows in MXFP4, over up to 64 lists of rows whose lengths may be known on the device only (the
+// minibatches that a pipeline keeps in flight; rows of several kinds, each kind with a matrix of its own):
 //
-//   product       Y_j = X_j W[g_j]^T           X_j [n_j, D] and W[g] [H, D] in MXFP4, Y_j fp32, fp16 or bf16
-//   weight grad   dW[g] = sum_j dY_j^T X_j     over the lists of group g; dY_j fp32, fp16 or bf16, dW fp32
+//   Y_j = X_j W[g_j]^T           X_j [n_j, D] and W[g] [H, D] in MXFP4, Y_j fp32, fp16 or bf16
 //
-// What a code and a scale stand for is exact in bf16, as is an fp32 as the sum of three bf16: the products of both kernels are
-// exact and are added in fp32, so the only other roundings are those of the sums and of Y.
+// Two values of the format have 6 bits as a product: the products of the matrix instruction are exact, sums are formed in fp32,
+// and Y is rounded once.
 #include "spp_mx4.h"
 
 namespace spp {
-
-// Lane j has list j: its rows, and the tiles of all lists up to it.  The count of a list may have to be fetched: one round trip.
-struct Lists {
-    int rows, upto, tiles;
-    __device__ __forceinline__ Lists(const RowTable& t, int tile_rows) {
-        const int j = lane_id();
-        rows = j < t.n_lists ? (int)rows_of(t.n[j], t.d_n[j]) : 0;
-        tiles = (int)(((int64_t)rows + tile_rows - 1) / tile_rows);
-        upto = wave_inclusive_scan(tiles);
-    }
-    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(upto, kWave - 1); }
-    __device__ __forceinline__ int list_of(int tile) const { return __builtin_amdgcn_readfirstlane(__popcll(__ballot(upto <= tile))); }
-    __device__ __forceinline__ int rows_in(int list) const { return __builtin_amdgcn_readlane(rows, list); }
-    __device__ __forceinline__ int first_tile(int list) const { return __builtin_amdgcn_readlane(upto - tiles, list); }
-};
 
 // ---- product --------------------------------------------------------------------------------------
 
@@ -442,300 +426,6 @@ __global__ void __launch_bounds__(kProdBlock) mx4_product_kernel(ProductArgs a) 
     }
 }
 
-// ---- weight gradient ------------------------------------------------------------------------------
-
-// The rows of all lists, in the order of their groups, are cut into chunks, and the chunks into `splits` runs of equal length.  A
-// workgroup has one run and one tile of dW; where its run passes from a group to the next it writes down what it has as piece
-// (run + group) and starts again, and the second kernel adds up each group's pieces in the order of the rows.  No atomics: the
-// same counts give the same bits.
-//
-// Both operands have the rows as the axis that is summed over, so their tiles lie in LDS as they lie in memory and are read
-// transposed (ds_read_b64_tr_b16).  A chunk's operands are asked for two chunks ahead, into registers; X is unpacked to bf16 on
-// its way to LDS, dY cut into its pieces.
-constexpr int kGradPad = 16;         // elements behind an LDS row: the four rows that 16 lanes read at once are then 4 x 32 bytes of other banks
-
-struct GradArgs {
-    RowTable t;
-    float*   pieces;       // [splits + groups][H * D]
-    float*   dw;           // [groups][H * D]
-    int32_t  D, H, nb, rb;
-    int32_t  splits, tiles_d;
-    int32_t  chunk;        // rows of a chunk
-};
-
-// dY as bf16 numbers that add up to it exactly: one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
-// finite value becomes infinite; what is not finite is its first piece alone.
-template <class T> struct Pieces { static constexpr int n = 1; };
-template <> struct Pieces<_Float16> { static constexpr int n = 2; };
-template <> struct Pieces<float> { static constexpr int n = 3; };
-template <int P>
-__device__ __forceinline__ void cut(float x, __bf16 (&out)[P]) {
-    const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const float head = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-        out[p] = (__bf16)(p == 0 && !finite ? x : head);
-        x = finite ? x - head : 0.0f;
-    }
-}
-
-// Eight rows of the lane's column: of 16 lanes, lane i names row i/4 and columns 4 (i mod 4) .., and gets column i of four rows.
-template <int LD>
-__device__ __forceinline__ bf16x8 column8(const __bf16* p) {
-    typedef __attribute__((address_space(3))) i16x4* lds4;
-    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p));
-    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 4 * LD));
-    const bf16x4 x = __builtin_bit_cast(bf16x4, a), y = __builtin_bit_cast(bf16x4, b);
-    return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-}
-
-template <class T, int WH, int WD>
-struct GradShape {
-    static constexpr int P = Pieces<T>::n;
-    static constexpr int rows = P == 1 ? 64 : 32;                    // of a chunk: two buffers of it fit the LDS
-    static constexpr int threads = 64 * WH * WD;
-    static constexpr int th = 64 * WH, td = 64 * WD;                 // the tile of dW: a wavefront has 64 x 64 of it
-    static constexpr int ly = th + kGradPad, lx = td + kGradPad;     // elements of an LDS row
-    static constexpr int buffer = rows * (P * ly + lx);              // elements of a buffer
-    static constexpr int lds = 2 * buffer * 2;
-    static constexpr int ve = 16 / (int)sizeof(T);                   // elements of a 16-byte vector of dY
-    static constexpr int ny = rows * th / ve / threads;              // vectors of dY, blocks of X per thread and chunk
-    static constexpr int nx = (rows * 2 * WD + threads - 1) / threads;
-};
-
-template <class T, int WH, int WD>
-__global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
-    typedef GradShape<T, WH, WD> S;
-    constexpr int P = S::P;
-    extern __shared__ __attribute__((aligned(16))) __bf16 lds[];
-    const Lists lists(a.t, S::rows);
-    const int total = lists.total();
-    const int splits = a.splits < total ? a.splits : total;
-    const int tiles = (int)gridDim.x / a.splits;
-    // the tiles of a run, which read the same rows, share an XCD's L2
-    const int id = (int)own_piece();
-    const int tile = id % tiles, split = id / tiles;
-    if (split >= splits) return;
-    const int from = (int)((int64_t)split * total / splits), to = (int)((int64_t)(split + 1) * total / splits);
-    const int h0 = tile / a.tiles_d * S::th, d0 = tile % a.tiles_d * S::td;
-    const int wave = threadIdx.x >> 6, l = lane_id();
-    const int wh = wave / WD * 64, wd = wave % WD * 64;
-
-    u32x4 ry[2][S::ny], rx[2][S::nx];
-    uint32_t rs[2][S::nx];
-    int here[2], group[2];
-
-    auto load = [&](int u, int chunk) {
-        const int list = lists.list_of(chunk);
-        const int64_t r0 = (int64_t)(chunk - lists.first_tile(list)) * S::rows;
-        const int64_t left = lists.rows_in(list) - r0;
-        here[u] = left < S::rows ? (int)left : S::rows;
-        group[u] = a.t.group[list];
-        const int64_t ld = a.t.ld[list];
-        const T* y = static_cast<const T*>(a.t.y[list]) + r0 * ld;
-        const uint8_t* x = a.t.rows[list] + r0 * a.rb;
-        // rows behind the last and columns behind H or D: others in their place; put() clears the rows, and those columns of dW
-        // are not written
-        if (((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0 && a.H % S::ve == 0) {
-#pragma unroll
-            for (int k = 0; k < S::ny; ++k) {
-                const int i = k * S::threads + (int)threadIdx.x;
-                int r = i / (S::th / S::ve), h = h0 + i % (S::th / S::ve) * S::ve;
-                r = r < here[u] ? r : here[u] - 1;
-                h = h < a.H ? h : 0;
-                ry[u][k] = *reinterpret_cast<const u32x4*>(y + r * ld + h);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < S::ny; ++k) {
-                const int i = k * S::threads + (int)threadIdx.x;
-                int r = i / (S::th / S::ve);
-                const int h = h0 + i % (S::th / S::ve) * S::ve;
-                r = r < here[u] ? r : here[u] - 1;
-                T v[S::ve];
-#pragma unroll
-                for (int j = 0; j < S::ve; ++j) v[j] = y[r * ld + (h + j < a.H ? h + j : a.H - 1)];
-                ry[u][k] = __builtin_bit_cast(u32x4, v);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < S::nx; ++k) {
-            const int i = k * S::threads + (int)threadIdx.x;
-            int r = i / (2 * WD), b = d0 / 32 + i % (2 * WD);
-            r = r < here[u] ? r : here[u] - 1;
-            b = b < a.nb ? b : a.nb - 1;
-            const uint8_t* p = x + r * a.rb;
-            rx[u][k] = *reinterpret_cast<const u32x4*>(p + 16 * b);
-            rs[u][k] = p[16 * a.nb + b];
-        }
-    };
-    auto put = [&](int u) {
-        __bf16* gy = lds + u * S::buffer;
-        __bf16* gx = gy + P * S::rows * S::ly;
-#pragma unroll
-        for (int k = 0; k < S::ny; ++k) {
-            const int i = k * S::threads + (int)threadIdx.x;
-            const int r = i / (S::th / S::ve), h = i % (S::th / S::ve) * S::ve;
-            const u32x4 raw = r < here[u] ? ry[u][k] : u32x4{0, 0, 0, 0};
-            if constexpr (P == 1) {
-                *reinterpret_cast<u32x4*>(gy + r * S::ly + h) = raw;
-            } else {
-                struct Vec { T v[S::ve]; } in = __builtin_bit_cast(Vec, raw);
-                struct Cut { __bf16 v[S::ve]; } out[P];
-#pragma unroll
-                for (int j = 0; j < S::ve; ++j) {
-                    __bf16 c[P];
-                    cut<P>((float)in.v[j], c);
-#pragma unroll
-                    for (int p = 0; p < P; ++p) out[p].v[j] = c[p];
-                }
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    if constexpr (S::ve == 8) *reinterpret_cast<u32x4*>(gy + (p * S::rows + r) * S::ly + h) = __builtin_bit_cast(u32x4, out[p]);
-                    else *reinterpret_cast<u32x2*>(gy + (p * S::rows + r) * S::ly + h) = __builtin_bit_cast(u32x2, out[p]);
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < S::nx; ++k) {
-            const int i = k * S::threads + (int)threadIdx.x;
-            const int r = i / (2 * WD);
-            if (S::rows * 2 * WD % S::threads && r >= S::rows) continue;
-            const float s = r < here[u] ? mx4_scale(rs[u][k]) : 0.0f;
-            const u32x4 c = r < here[u] ? rx[u][k] : u32x4{0, 0, 0, 0};
-            __bf16* to_x = gx + r * S::lx + i % (2 * WD) * 32;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 1),
-                             v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], s, 3);
-                *reinterpret_cast<bf16x8*>(to_x + 8 * j) = bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-            }
-        }
-    };
-
-    f32x4 acc[4][4];
-    auto clear = [&]() {
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    };
-    auto flush = [&](int g) {
-        float* out = a.pieces + (int64_t)(split + g) * a.H * a.D;
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int h = h0 + wh + 16 * f + 4 * (l >> 4) + i, d = d0 + wd + 16 * c + (l & 15);
-                    if (h < a.H && d < a.D) out[(int64_t)h * a.D + d] = acc[f][c][i];
-                }
-    };
-    const int n = to - from;
-    load(0, from);
-    if (n > 1) load(1, from + 1);
-    clear();
-    int now = group[0];
-    for (int j = 0; j < n; j += 2) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (j + u >= n) break;
-            if (group[u] != now) { flush(now); clear(); now = group[u]; }
-            put(u);
-            __syncthreads();         // the other buffer has been read by all before this one is read by any
-            if (j + u + 2 < n) load(u, from + j + u + 2);
-            const __bf16* gy = lds + u * S::buffer;
-            const __bf16* gx = gy + P * S::rows * S::ly;
-#pragma unroll
-            for (int k = 0; k < S::rows; k += 32) {
-                const int row = k + 8 * (l >> 4) + ((l & 15) >> 2), col = 4 * (l & 3);
-                bf16x8 bx[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) bx[c] = column8<S::lx>(gx + row * S::lx + col + wd + 16 * c);
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        const bf16x8 ay = column8<S::ly>(gy + (p * S::rows + row) * S::ly + col + wh + 16 * f);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ay, bx[c], acc[f][c], 0, 0, 0);
-                    }
-            }
-        }
-    }
-    flush(now);
-}
-
-// Each element's pieces are added by four lanes, then the four sums: always in the same order.
-constexpr int kSumLanes = 4;
-__global__ void __launch_bounds__(256) mx4_grad_sum_kernel(GradArgs a) {
-    const Lists lists(a.t, a.chunk);
-    const int total = lists.total(), group = blockIdx.y;
-    const int splits = a.splits < total ? a.splits : total;
-    const int64_t size = (int64_t)a.H * a.D;
-    // the chunks of the group: from its first list's first to its last list's last
-    const uint64_t mine = __ballot(lane_id() < a.t.n_lists && (int)a.t.group[lane_id()] == group && lists.tiles > 0);
-    int lo = 0, hi = -1;
-    if (mine) {
-        const int first = lists.first_tile(__builtin_ctzll(mine)), last = __builtin_amdgcn_readlane(lists.upto, 63 - __builtin_clzll(mine)) - 1;
-        lo = (int)((((int64_t)first + 1) * splits - 1) / total);
-        hi = (int)((((int64_t)last + 1) * splits - 1) / total);
-    }
-    // 16 elements side by side, the four lanes of each 16 apart
-    const int part = (lane_id() >> 4) & (kSumLanes - 1);
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), waves = (int64_t)gridDim.x * 4;
-    for (int64_t i0 = wave * 16; i0 < size; i0 += waves * 16) {
-        const int64_t i = i0 + (lane_id() & 15);
-        const float* p = a.pieces + (i < size ? i : size - 1);
-        double sum = 0.0;
-#pragma unroll 8
-        for (int s = lo + part; s <= hi; s += kSumLanes) sum += p[(int64_t)(s + group) * size];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (part == 0 && i < size) a.dw[group * size + i] = (float)sum;
-    }
-}
-
-template <class T, int WH, int WD>
-static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
-    typedef GradShape<T, WH, WD> S;
-    auto kernel = mx4_grad_kernel<T, WH, WD>;
-    a.chunk = S::rows;
-    a.tiles_d = (a.D + S::td - 1) / S::td;
-    const int64_t tiles = (int64_t)a.tiles_d * ((a.H + S::th - 1) / S::th), size = (int64_t)a.H * a.D;
-    int64_t chunks = 0;
-    for (int j = 0; j < a.t.n_lists; ++j) chunks += (a.t.n[j] + (int64_t)S::rows - 1) / S::rows;
-    const int fit = 163840 / S::lds, wish = 8 / (WH * WD);
-    const int64_t at_once = (int64_t)ctx->num_cu * (fit < 1 || wish < 1 ? 1 : fit < wish ? fit : wish);
-    int64_t splits = at_once / tiles;
-    if (splits > (chunks + 1) / 2) splits = (chunks + 1) / 2;
-    a.splits = (int32_t)(splits < 1 ? 1 : splits);
-    SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float)));
-    a.pieces = ctx->gradws.as<float>();
-    if (!sum_only) {
-        if (S::lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds));
-        kernel<<<(unsigned)(a.splits * tiles), S::threads, S::lds, ctx->stream>>>(a);
-        SPP_HIP(hipGetLastError());
-    }
-    const int64_t sums = (size + 63) / 64;
-    mx4_grad_sum_kernel<<<dim3((unsigned)(sums < 8192 ? sums : 8192), n_groups), 256, 0, ctx->stream>>>(a);
-    SPP_HIP(hipGetLastError());
-    return SPP_OK;
-}
-template <class T, int WH>
-static int grad_by_width(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
-    // as few tiles as 128 columns allow, of as few wavefronts as these need
-    const int tiles = (a.D + 127) / 128;
-    return (a.D + tiles - 1) / tiles > 64 ? launch_grad<T, WH, 2>(ctx, a, n_groups, sum_only) : launch_grad<T, WH, 1>(ctx, a, n_groups, sum_only);
-}
-template <class T>
-static int grad_of(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
-    const int tiles = (a.H + 255) / 256, wh = (a.H + 64 * tiles - 1) / (64 * tiles);
-    return wh == 1 ? grad_by_width<T, 1>(ctx, a, n_groups, sum_only) : wh == 2 ? grad_by_width<T, 2>(ctx, a, n_groups, sum_only)
-         : wh == 3 ? grad_by_width<T, 3>(ctx, a, n_groups, sum_only) : grad_by_width<T, 4>(ctx, a, n_groups, sum_only);
-}
-
 int row_table(const char* who, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H, int32_t type,
               RowTable& t, int64_t* most) {
     SPP_CHECK(n_lists >= 0 && n_lists <= kRowLists && (lists || n_lists == 0), SPP_E_ARG, "%s: %d lists (at most %d)", who, n_lists, kRowLists);
@@ -754,14 +444,15 @@ int row_table(const char* who, const spp_row_list* lists, int32_t n_lists, int32
                   "%s: list %d: rows must be 16-byte aligned, Y to its type and the count to 8 bytes", who, j);
         *most += a.n;
     }
-    for (int g = 0, k = 0; g < n_groups; ++g)               // the lists in the order of their groups
-        for (int j = 0; j < n_lists; ++j) {
-            if (lists[j].group != g) continue;
-            t.rows[k] = static_cast<const uint8_t*>(lists[j].d_rows);
-            t.y[k] = lists[j].d_y; t.d_n[k] = lists[j].n ? lists[j].d_n : nullptr; t.ld[k] = lists[j].ld;
-            t.n[k] = (int32_t)lists[j].n; t.group[k] = (uint8_t)g;
-            ++k;
-        }
+    int at[kRowLists + 1] = {};                             // the lists in the order of their groups
+    for (int j = 0; j < n_lists; ++j) ++at[lists[j].group + 1];
+    for (int g = 0; g < n_groups; ++g) at[g + 1] += at[g];
+    for (int j = 0; j < n_lists; ++j) {
+        const int k = at[lists[j].group]++;
+        t.rows[k] = static_cast<const uint8_t*>(lists[j].d_rows);
+        t.y[k] = lists[j].d_y; t.d_n[k] = lists[j].n ? lists[j].d_n : nullptr; t.ld[k] = lists[j].ld;
+        t.n[k] = (int32_t)lists[j].n; t.group[k] = (uint8_t)lists[j].group;
+    }
     t.n_lists = n_lists;
     return SPP_OK;
 }
@@ -770,7 +461,8 @@ template <class T, int TR, int RN>
 static int launch_product(spp_ctx* ctx, const ProductArgs& a) {
     const int lds = TR * a.rb;
     auto kernel = mx4_product_kernel<T, TR, RN>;
-    if (lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    static LdsLimit limit;
+    SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
     int64_t tiles = 0;
     for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)TR - 1) / TR;
     const int64_t parts = ((a.H + 63) / 64 * (TR / (16 * RN)) + kProdWaves - 1) / kProdWaves;
@@ -789,7 +481,8 @@ static int launch_rows_as(spp_ctx* ctx, ProductArgs& a) {
     a.out_lds = 16 * RN * RowsOut<T, RN>::kPitch;
     if (!Stream && row <= kRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
     const int lds = a.w_lds + (Lines ? 0 : WAVES * a.out_lds);
-    if (lds > 65536) SPP_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    static LdsLimit limit;
+    SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
     int64_t tiles = 0;
     for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)(WAVES * 16 * RN) - 1) / (WAVES * 16 * RN);
     // Workgroups per CU.  A stream of whole lines is fastest from few wavefronts (2.56M rows 128 -> 256: 221 us with one workgroup per CU,
@@ -851,23 +544,5 @@ extern "C" int spp_mx4_product(spp_ctx* ctx, const spp_row_list* lists, int32_t 
         SPP_TRY(type == SPP_F32 ? product_of<float>(ctx, a, most) : type == SPP_F16 ? product_of<_Float16>(ctx, a, most) : product_of<__bf16>(ctx, a, most));
     }
     if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(ctx->stream));
-    return SPP_OK;
-}
-
-extern "C" int spp_mx4_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H,
-                                   int32_t type, float* d_grad, uint32_t flags) {
-    using namespace spp;
-    SPP_CHECK(ctx && d_grad, SPP_E_ARG, "spp_mx4_weight_grad: null argument");
-    SPP_CHECK((uintptr_t)d_grad % 4 == 0, SPP_E_ARG, "spp_mx4_weight_grad: the gradient must be 4-byte aligned");
-    GradArgs a;
-    int64_t most = 0;
-    SPP_TRY(row_table("spp_mx4_weight_grad", lists, n_lists, n_groups, D, H, type, a.t, &most));
-    SPP_HIP(hipSetDevice(ctx->device));
-    a.dw = d_grad; a.D = D; a.H = H; a.nb = mx4_blocks(D); a.rb = mx4_bytes(D);
-    hipStream_t st = ctx->stream;
-    ScopedTimer timer(ctx, SPP_T_LAYER, st);
-    SPP_TRY(type == SPP_F32 ? grad_of<float>(ctx, a, n_groups, most == 0) : type == SPP_F16 ? grad_of<_Float16>(ctx, a, n_groups, most == 0)
-                                                                                          : grad_of<__bf16>(ctx, a, n_groups, most == 0));
-    if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(st));
     return SPP_OK;
 }

@@ -8,6 +8,8 @@
 #include "spp_common.h"
 #include "spp_device.h"
 
+#include <atomic>
+
 namespace spp {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -81,8 +83,35 @@ struct RowTable {
     uint8_t        group[kRowLists];
     int32_t        n_lists;
 };
+// Lane j has list j: its rows, and the tiles of all lists up to it.  The count of a list may have to be fetched: one round trip.
+struct Lists {
+    int rows, upto, tiles;
+    __device__ __forceinline__ Lists(const RowTable& t, int tile_rows) {
+        const int j = lane_id();
+        rows = j < t.n_lists ? (int)rows_of(t.n[j], t.d_n[j]) : 0;
+        tiles = (int)(((int64_t)rows + tile_rows - 1) / tile_rows);
+        upto = wave_inclusive_scan(tiles);
+    }
+    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(upto, kWave - 1); }
+    __device__ __forceinline__ int list_of(int tile) const { return __builtin_amdgcn_readfirstlane(__popcll(__ballot(upto <= tile))); }
+    __device__ __forceinline__ int rows_in(int list) const { return __builtin_amdgcn_readlane(rows, list); }
+    __device__ __forceinline__ int first_tile(int list) const { return __builtin_amdgcn_readlane(upto - tiles, list); }
+};
+
 // Host: the checks that the product and the gradient share; fills the table, and *most with the rows the lists can hold.
 int row_table(const char* who, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H, int32_t type,
               RowTable& t, int64_t* most);
+
+
+// More dynamic LDS than 64 KB has to be allowed to a kernel, once per device.
+struct LdsLimit {
+    std::atomic<int> most[kPoolDevices] = {};
+    int allow(const spp_ctx* ctx, const void* kernel, int lds) {
+        if (lds <= 65536 || (ctx->device < kPoolDevices && most[ctx->device].load(std::memory_order_relaxed) >= lds)) return SPP_OK;
+        SPP_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
+        if (ctx->device < kPoolDevices) most[ctx->device].store(163840, std::memory_order_relaxed);
+        return SPP_OK;
+    }
+};
 
 }  // namespace spp
