@@ -92,39 +92,75 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
     uint32_t rs[S::ahead][S::nx];
     int here[S::ahead], group[S::ahead];
 
-    auto load = [&](int u, int chunk) {
-        const int list = lists.list_of(chunk);
-        const int64_t r0 = (int64_t)(chunk - lists.first_tile(list)) * S::rows;
-        const int64_t left = lists.rows_in(list) - r0;
-        here[u] = left < S::rows ? (int)left : S::rows;
-        group[u] = a.t.group[list];
-        const int64_t ld = a.t.ld[list];
-        const T* y = static_cast<const T*>(a.t.y[list]) + r0 * ld;
-        const uint8_t* x = a.t.rows[list] + r0 * a.rb;
-        // Rows behind the last and columns behind H or D: others in their place; put() clears the rows, and those columns of dW
-        // are not written.  A vector may reach over a row's end into the next row, but not over the list's.
-        const bool wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0 && a.H % S::ve == 0;
-        if (ld < (1 << 24) && (wide || (left > S::rows && a.H >= S::ve))) {
-            uint32_t off[S::ny];
+    // Where the next chunk is; chunks are asked for in their order, so that most follow the one before in its list.
+    const T* y = nullptr;
+    const uint8_t* x = nullptr;
+    int64_t ld = 0;
+    int until = from, list_group = 0, left = 0;                      // the list's last chunk + 1, its group, its rows from the chunk on
+    bool wide = false;
+    uint32_t oy[S::ny], ox[S::nx], os[S::nx];                        // a whole chunk's vectors, blocks and scales
+#pragma unroll
+    for (int k = 0; k < S::nx; ++k) {
+        const int i = k * S::threads + (int)threadIdx.x, b = d0 / 32 + i % (2 * WD);
+        const int r = i / (2 * WD) < S::rows ? i / (2 * WD) : S::rows - 1, in = b < a.nb ? b : a.nb - 1;
+        ox[k] = (uint32_t)(r * a.rb + 16 * in);
+        os[k] = (uint32_t)(r * a.rb + 16 * a.nb + in);
+    }
+    // Behind the last chunk (more false) the last one again: a path without loads would make the compiler wait for all that are under way.
+    auto load = [&](int u, int chunk, bool more) {
+        if (more && chunk >= until) {
+            const int list = lists.list_of(chunk);
+            const int before = chunk - lists.first_tile(list);
+            until = __builtin_amdgcn_readlane(lists.upto, list);
+            left = lists.rows_in(list) - before * S::rows;
+            list_group = a.t.group[list];
+            ld = a.t.ld[list];
+            y = static_cast<const T*>(a.t.y[list]) + (int64_t)before * S::rows * ld;
+            x = a.t.rows[list] + (int64_t)before * S::rows * a.rb;
+            wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % 16 == 0 && a.H % S::ve == 0;
 #pragma unroll
             for (int k = 0; k < S::ny; ++k) {
-                const int i = k * S::threads + (int)threadIdx.x;
-                int r = i / (S::th / S::ve), h = h0 + i % (S::th / S::ve) * S::ve;
-                r = r < here[u] ? r : here[u] - 1;
-                off[k] = (uint32_t)(r * (int)ld + (h < a.H ? h : 0));
+                const int i = k * S::threads + (int)threadIdx.x, h = h0 + i % (S::th / S::ve) * S::ve;
+                oy[k] = (uint32_t)(i / (S::th / S::ve) * (int)ld + (h < a.H ? h : 0));
             }
+        } else if (more) {
+            y += S::rows * ld;
+            x += S::rows * a.rb;
+            left -= S::rows;
+        }
+        here[u] = left < S::rows ? left : S::rows;
+        group[u] = list_group;
+        // Columns behind H or D: others in their place, as those columns of dW are not written; rows behind the list's last: the last,
+        // put() clears them.  A vector may reach over a row's end into the next row, but not over the list's.
+        uint32_t py[S::ny], px[S::nx], ps[S::nx];
+#pragma unroll
+        for (int k = 0; k < S::ny; ++k) py[k] = oy[k];
+#pragma unroll
+        for (int k = 0; k < S::nx; ++k) { px[k] = ox[k]; ps[k] = os[k]; }
+        if (left < S::rows) {
+#pragma unroll
+            for (int k = 0; k < S::ny; ++k) {
+                const int i = k * S::threads + (int)threadIdx.x, r = i / (S::th / S::ve);
+                if (r >= left) py[k] -= (uint32_t)((r - left + 1) * (int)ld);
+            }
+#pragma unroll
+            for (int k = 0; k < S::nx; ++k) {
+                const int i = k * S::threads + (int)threadIdx.x, r = i / (2 * WD) < S::rows ? i / (2 * WD) : S::rows - 1;
+                if (r >= left) { px[k] -= (uint32_t)((r - left + 1) * a.rb); ps[k] -= (uint32_t)((r - left + 1) * a.rb); }
+            }
+        }
+        if (ld < (1 << 24) && (wide || (left > S::rows && a.H >= S::ve))) {
             if (wide)
 #pragma unroll
-                for (int k = 0; k < S::ny; ++k) ry[u][k] = *reinterpret_cast<const u32x4*>(y + off[k]);
+                for (int k = 0; k < S::ny; ++k) ry[u][k] = *reinterpret_cast<const u32x4*>(y + py[k]);
             else
 #pragma unroll
-                for (int k = 0; k < S::ny; ++k) ry[u][k] = reinterpret_cast<const Loose<u32x4>*>(y + off[k])->v;
+                for (int k = 0; k < S::ny; ++k) ry[u][k] = reinterpret_cast<const Loose<u32x4>*>(y + py[k])->v;
         } else {
 #pragma unroll
             for (int k = 0; k < S::ny; ++k) {
-                const int i = k * S::threads + (int)threadIdx.x;
+                const int i = k * S::threads + (int)threadIdx.x, h = h0 + i % (S::th / S::ve) * S::ve;
                 int r = i / (S::th / S::ve);
-                const int h = h0 + i % (S::th / S::ve) * S::ve;
                 r = r < here[u] ? r : here[u] - 1;
                 T v[S::ve];
 #pragma unroll
@@ -134,13 +170,8 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
         }
 #pragma unroll
         for (int k = 0; k < S::nx; ++k) {
-            const int i = k * S::threads + (int)threadIdx.x;
-            int r = i / (2 * WD), b = d0 / 32 + i % (2 * WD);
-            r = r < here[u] ? r : here[u] - 1;
-            b = b < a.nb ? b : a.nb - 1;
-            const uint8_t* p = x + r * a.rb;
-            rx[u][k] = *reinterpret_cast<const u32x4*>(p + 16 * b);
-            rs[u][k] = p[16 * a.nb + b];
+            rx[u][k] = *reinterpret_cast<const u32x4*>(x + px[k]);
+            rs[u][k] = x[ps[k]];
         }
     };
     auto put = [&](int u, int buffer) {
@@ -165,10 +196,20 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
                         for (int p = 0; p < P; ++p) out[p].v[j] = c[p];
                     }
                 };
-                float top = 0.0f;                          // infinite or NaN if any of them is
+                bool odd;                                  // infinite or NaN
+                if constexpr (S::ve == 8) {
+                    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+                    u16x2 top = __builtin_bit_cast(u16x2, raw.x & 0x7FFF7FFFu);
 #pragma unroll
-                for (int j = 0; j < S::ve; ++j) top += fabsf((float)in.v[j]) * 0x1p-8f;
-                if (__any((__float_as_uint(top) & 0x7F800000u) == 0x7F800000u)) each(std::false_type());
+                    for (int j = 1; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, raw[j] & 0x7FFF7FFFu));
+                    odd = top[0] >= 0x7C00u || top[1] >= 0x7C00u;
+                } else {
+                    uint32_t top = raw.x & 0x7FFFFFFFu;
+#pragma unroll
+                    for (int j = 1; j < 4; ++j) top = top > (raw[j] & 0x7FFFFFFFu) ? top : raw[j] & 0x7FFFFFFFu;
+                    odd = top >= 0x7F800000u;
+                }
+                if (__any(odd)) each(std::false_type());
                 else each(std::true_type());
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
@@ -219,8 +260,8 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
                 }
     };
     const int n = to - from;
-    load(0, from);
-    if (S::ahead > 1 && n > 1) load(S::ahead - 1, from + 1);
+    load(0, from, true);
+    if (S::ahead > 1) load(S::ahead - 1, from + 1, n > 1);
     clear();
     int now = group[0];
     for (int j = 0; j < n; j += 2) {
@@ -230,8 +271,8 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
             constexpr int mask = S::ahead - 1;
             if (group[u & mask] != now) { flush(now); clear(); now = group[u & mask]; }
             put(u & mask, u);
+            load(u & mask, from + j + u + S::ahead, j + u + S::ahead < n);
             __syncthreads();         // the other buffer has been read by all before this one is read by any
-            if (j + u + S::ahead < n) load(u & mask, from + j + u + S::ahead);
             const __bf16* gy = lds + u * S::buffer;
             const __bf16* gx = gy + P * S::rows * S::ly;
 #pragma unroll
