@@ -485,14 +485,15 @@ static int launch_rows_as(spp_ctx* ctx, ProductArgs& a) {
     SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
     int64_t tiles = 0;
     for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)(WAVES * 16 * RN) - 1) / (WAVES * 16 * RN);
-    // Workgroups per CU.  A stream of whole lines is fastest from few wavefronts (2.56M rows 128 -> 256: 221 us with one workgroup per CU,
-    // 245 to 250 with two to eight) once each has enough to do; with less, or two steps of columns and more to wait for (800k
-    // rows 256 -> 256: 102, 86, 92 us with one, two, three), more are better.  Rows of other lengths take unequal times: many
-    // workgroups even them out where there are many more tiles (2.56M rows 100 -> 172: 236 us with four per CU, 197 with
-    // sixteen; 300k rows in fp32 42 and 49).
+    // Workgroups per CU.  Many tiles are fastest with a workgroup each (2.56M rows 128 -> 256: 264 us, 285 with one workgroup per CU
+    // that goes over its tiles, 298 to 302 with two to sixteen; 800k rows 256 -> 256: 110 and 117); some with one per CU (300k
+    // rows 32.3 us, 34 to 35 with more); few with what runs at once (100k rows 13.9 us, 15.1 with one, 16 with four).
+    // Rows of other lengths take unequal times: many workgroups even them out where there are many more tiles (2.56M rows
+    // 100 -> 172: 289 us with four per CU, 238 with 32; 300k rows in fp32 42 and 49).
     a.fill = 2 * ctx->num_cu;
     const int64_t want = tiles >= a.fill ? tiles : tiles * ht < a.fill ? tiles * ht : a.fill;
-    const int per_cu = Stream ? 2 : Lines ? (KS > 1 ? 2 : tiles >= 8 * ctx->num_cu ? 1 : 3) : tiles >= 64 * ctx->num_cu ? 16 : 4;
+    const int64_t load = tiles / ctx->num_cu;
+    const int per_cu = Stream ? 2 : Lines ? (load >= 16 ? 128 : load >= 8 ? 1 : 3) : load >= 64 ? 32 : 4;
     const int64_t most = (int64_t)ctx->num_cu * per_cu;
     kernel<<<(unsigned)(want < most ? want : most), 64 * WAVES, lds, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
@@ -506,7 +507,7 @@ static int launch_rows(spp_ctx* ctx, ProductArgs& a) {
     for (int j = 0; j < a.t.n_lists; ++j) lines = lines && ((uintptr_t)a.t.y[j] | (uint64_t)(a.t.ld[j] * (int64_t)sizeof(T))) % 128 == 0;
     if (ht * 64 * a.ls <= kHeldW)
         return lines ? launch_rows_as<T, KS, 2, 4, false, true>(ctx, a) : launch_rows_as<T, KS, 1, 4, false, false>(ctx, a);
-    return lines ? launch_rows_as<T, KS, 2, 8, true, true>(ctx, a) : launch_rows_as<T, KS, KS >= 4 ? 1 : 2, 8, true, false>(ctx, a);
+    return lines ? launch_rows_as<T, KS, 2, KS <= 3 ? 4 : 8, true, true>(ctx, a) : launch_rows_as<T, KS, KS >= 4 ? 1 : 2, 8, true, false>(ctx, a);
 }
 constexpr int kFewRows = 64;
 template <class T>
