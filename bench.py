@@ -244,6 +244,67 @@ def host_threads():
     return max(1, min(16, n))
 
 
+def layer_phase(args, cfg, spp, S, torch, dev, ctx, w, p):
+    """Feature rows in 4 bits and the layer that reads them: groups of minibatches sampled, gathered (packed rows from the shard,
+    the cache and pinned host memory), multiplied with the layer's weights, their gradient taken (of half the squared outputs),
+    one AdamW step, the weights quantised again; the pieces timed by events over args.steps groups."""
+    g, G, Tk, lo, hi, nrem = w["g"], w["G"], w["Tk"], w["lo"], w["hi"], w["nrem"]
+    H, n, rb = args.hidden, args.group, spp.mx4_row_bytes(cfg.D)
+    local = spp.mx4_quantize(ctx, S.feature_block(cfg, lo, hi, dev))
+    remote = torch.empty((nrem, rb), dtype=torch.uint8).pin_memory()
+    for a in range(0, nrem, 1 << 19):
+        b = min(nrem, a + (1 << 19))
+        remote[a:b].copy_(spp.mx4_quantize(ctx, S.feature_rows(cfg, S.remote_ids(cfg, a, b, dev))))
+    cache = spp.build_vip_cache(ctx, p, lo, hi, cfg.K, cfg.alpha, remote, rb, 1)
+    batches = [b for b in S.epoch_batches(cfg, Tk, 0) if b.numel() == min(cfg.B, Tk.numel())]
+    bufs = [spp.MFGBuffers(dev, cfg.B, cfg.fanouts, cfg.N) for _ in range(n)]
+
+    def sample(step):
+        items = [(batches[(step * n + i) % len(batches)], step * n + i, bufs[i]) for i in range(n)]
+        spp.sample_mfg_multi(ctx, G, items, cfg.fanouts, cfg.seed_sampler, sync=False)
+
+    sample(0)
+    ctx.sync()
+    cap = int(1.25 * max(int(b.n_final_device) for b in bufs)) + 1
+    rows = [torch.empty((cap, rb), dtype=torch.uint8, device=dev) for _ in range(n)]
+    y = [torch.empty((cap, H), dtype=torch.bfloat16, device=dev) for _ in range(n)]
+    wanted = [(b.node_ids, cap, b.n_final_device, r) for b, r in zip(bufs, rows)]
+    lists = spp.RowLists([(r, cap, b.n_final_device, v) for b, r, v in zip(bufs, rows, y)])
+    weight = torch.randn(H, cfg.D, device=dev) * cfg.D ** -0.5
+    opt = spp.AdamW(ctx, [weight], state_bits=args.state_bits, lr=1e-3)
+    packed = spp.mx4_quantize(ctx, weight)
+    grad = torch.empty((1, H, cfg.D), dtype=torch.float32, device=dev)
+
+    def step(k):
+        sample(k)
+        spp.gather_features_multi(ctx, cache, local, cfg.N, lo, hi, remote, wanted, sync=False)
+        spp.mx4_product_multi(ctx, lists, packed, cfg.D, sync=False)
+        spp.mx4_weight_grad(ctx, lists, H, cfg.D, out=grad, sync=False)
+        opt.step([grad[0]], sync=False)
+        spp.mx4_quantize(ctx, weight, out=packed, sync=False)
+
+    for k in range(max(1, args.warmup)):
+        step(k)
+    ctx.sync()
+    ctx.timing(True)
+    t0 = time.perf_counter()
+    for k in range(args.steps):
+        step(k + 1)
+    ctx.sync()
+    wall = time.perf_counter() - t0
+    ms, cnt = ctx.times()
+    ctx.timing(False)
+    st = spp.gather_last_stats(ctx)
+    counts = [int(b.n_final_device) for b in bufs]
+    names = {"sample": 9, "gather_hit": 10, "gather_miss": 11, "classify": 12, "quantize_weights": 13, "product_and_gradient": 14, "adamw": 15}
+    print(json.dumps({"phase": "layer", "workload": cfg.name, "N": g.N, "M": g.M, "hidden": H, "minibatches_per_group": n,
+                      "row_bytes": rb, "row_bytes_unpacked": cfg.D * cfg.elem_bytes, "groups": args.steps,
+                      "minibatches_per_s": args.steps * n / wall, "ms_per_group": wall / args.steps * 1e3,
+                      "ms_per_group_by_piece": {k: ms[i] / args.steps for k, i in names.items()},
+                      "rows_of_last_group": sum(counts), "rows_cut_off": sum(max(0, c - cap) for c in counts),
+                      "last_gather": st, "state_bits": args.state_bits}), flush=True)
+
+
 def setup_workload(args, cfg, spp, S, torch, dev, ctx, rows=True, remote_on_device=False):
     """Inputs of one workload, resident before anything is timed."""
     lo, hi = cfg.bounds()
@@ -687,7 +748,7 @@ def main():
                     help="budget of each of the two oracle legs over minibatches (one thread, all threads); 0 = no CPU legs")
     ap.add_argument("--cpu-setup", default="on", choices=["on", "off"],
                     help="also time the oracle's VIP propagation and cache ranking once (one thread; about a minute on large)")
-    ap.add_argument("--phase", default="all", choices=["all", "vip", "alpha-sweep", "beta-sweep", "policy-sweep", "general", "calibrate"],
+    ap.add_argument("--phase", default="all", choices=["all", "vip", "alpha-sweep", "beta-sweep", "policy-sweep", "general", "layer", "calibrate"],
                     help="all: the benchmark line; vip: set-up and VIP propagation only (for profiling that kernel); "
                          "alpha-sweep: hit rate and host-miss bytes per batch over alpha in {0,.05,.1,.2,.5}, VIP-ranked "
                          "against degree-ranked cache (the experiment shape of Fig. 2 / Fig. 7), e.g. with --config skew; "
@@ -698,8 +759,12 @@ def main():
                          "beta-sweep: local rows read from host memory over the device-resident share beta of the "
                          "partition's rows, VIP order against id order (the experiment shape of the figure on local "
                          "storage on CPU versus GPU); "
+                         "layer: feature rows in 4 bits from sampling and gather through a layer of --hidden outputs, its gradient, "
+                         "an AdamW step and the weights' quantisation, timed by piece over --steps groups of --group minibatches; "
                          "calibrate: the library's plain streaming kernels over 1 GiB (read-only, copy, write-only): the "
                          "known-size kernels that scale the FETCH_SIZE / WRITE_SIZE counters of rocprofv3 --pmc")
+    ap.add_argument("--hidden", type=int, default=256, help="outputs of the layer of --phase layer")
+    ap.add_argument("--state-bits", type=int, default=32, choices=[8, 32], help="AdamW's moments in --phase layer")
     ap.add_argument("--sweep-batches", type=int, default=8)
     ap.add_argument("--sweep-epochs", type=int, default=4)
     args = ap.parse_args()
@@ -748,6 +813,8 @@ def main():
             policy_sweep(args, cfg, spp, S, torch, ctx, G, g, Tk, p, lo, hi)
         elif args.phase == "general":
             general_phase(args, cfg, spp, S, torch, ctx, G, g, Tk, p)
+        elif args.phase == "layer":
+            layer_phase(args, cfg, spp, S, torch, dev, ctx, w, p)
         return
 
     K, W = args.steps, args.warmup
