@@ -385,13 +385,13 @@ int  spp_mx4_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64
  *                                                              written (a group without rows: zeros)
  *     X and W are the values that the packed rows stand for; sums are formed in fp32 and rounded once to Y's type.  The
  *     gradient is that of the product by W's values; the rows are data and have none.  It adds in an order that the lists'
- *     lengths alone decide, so a call repeated gives the same bits; it keeps at most 64 MiB plus one matrix per group and
- *     one more of device memory with the context.
+ *     lengths alone decide, so a call repeated gives the same bits; it keeps some 64 MiB, or one matrix if that is more, and
+ *     one matrix per group of device memory with the context.
  *     d_rows 16-byte aligned; Y aligned to its type, ld >= H elements from a row to the next (16-byte aligned rows take
  *     the wide path).  Rows from *d_n on are neither read nor written, whatever they hold.  H is 1 .. SPP_MAX_HIDDEN. */
 typedef struct {
     const void*    d_rows;   /* [n, spp_mx4_row_bytes(D)] */
-    int64_t        n;        /* rows, or an upper bound when d_n is given; at most 2^31 - 1 */
+    int64_t        n;        /* rows, or an upper bound when d_n is given; at most 2^31 - 1, 2^35 over all lists */
     const int64_t* d_n;      /* device int64 count, or NULL */
     void*          d_y;      /* [n, H], row stride ld */
     int64_t        ld;

@@ -444,6 +444,7 @@ int row_table(const char* who, const spp_row_list* lists, int32_t n_lists, int32
                   "%s: list %d: rows must be 16-byte aligned, Y to its type and the count to 8 bytes", who, j);
         *most += a.n;
     }
+    SPP_CHECK(*most <= (int64_t)1 << 35, SPP_E_ARG, "%s: the lists' n add up to %lld (at most 2^35)", who, (long long)*most);
     int at[kRowLists + 1] = {};                             // the lists in the order of their groups
     for (int j = 0; j < n_lists; ++j) ++at[lists[j].group + 1];
     for (int g = 0; g < n_groups; ++g) at[g + 1] += at[g];

@@ -271,3 +271,81 @@ def test_a_training_step_of_the_layer_on_gathered_rows(ctx):
     ctx.sync()
     # features off by at most a sixth or so and weights in 4 bits: what is left is their rounding, far below the start
     assert losses[-1] < 0.1 * losses[0], (losses[0], losses[-1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D,H,pad,offset", [(300, 32, 255, 0, 0), (130, 64, 513, 0, 0), (300, 64, 500, 0, 0), (12800, 32, 300, 0, 0), (12801, 32, 301, 0, 1),
+                                              (700, 200, 1001, 0, 0), (700, 200, 1001, 3, 5), (300, 700, 500, 0, 3), (300, 500, 999, 1, 1), (5000, 40, 64, 64, 0),
+                                              (5000, 40, 64, 1, 0), (70, 96, 2, 0, 0), (4000, 128, 1, 0, 0), (33000, 128, 256, 0, 0), (270000, 32, 64, 0, 0),
+                                              (1100000, 32, 5, 0, 0)])
+def test_rows_of_y_of_any_length_and_address(ctx, dtype, n, D, H, pad, offset):
+    """Rows that are lines, rows that are put together (whole, or 64 columns at a time, their columns dealt out or not), rows
+    with gaps; nothing between or behind them is touched."""
+    rng = np.random.default_rng(n + 3 * D + 7 * H + pad)
+    rows, w = _rows(rng, n, D), _rows(rng, H, D)
+    buf = torch.full((offset + n * (H + pad) + 64,), 7.0, dtype=dtype, device=DEV)
+    y = torch.as_strided(buf, (n, H), (H + pad, 1), offset)
+    spp.mx4_product(ctx, torch.from_numpy(rows).to(DEV), torch.from_numpy(w).to(DEV), D, out=y)
+    pick = np.unique(np.concatenate([np.arange(min(n, 400)), np.arange(max(0, n - 300), n), rng.integers(0, n, 600)]))
+    want, size = _product(rows[pick], w, D)
+    _close(y[torch.from_numpy(pick).to(DEV)], want, size, D, dtype)
+    full = torch.from_numpy(R.values(rows, D)).to(DEV).float() @ torch.from_numpy(R.values(w, D)).to(DEV).float().T
+    assert torch.allclose(y.float(), full, rtol=2.0 ** -7, atol=1e-4 * float(full.abs().max()))       # every row is where it belongs
+    keep = torch.ones(buf.numel(), dtype=torch.bool, device=DEV)
+    keep.as_strided((n, H), (H + pad, 1), offset).fill_(False)
+    assert (buf[keep] == 7).all()
+
+
+@pytest.mark.parametrize("D,H,n", [(100, 256, 500), (33, 47, 100), (700, 300, 200), (1000, 70, 300), (128, 64, 3), (160, 1024, 400)])
+def test_what_lies_behind_the_scales_does_not_matter(ctx, D, H, n):
+    rng = np.random.default_rng(D + H)
+    rows, w = _rows(rng, n, D), _rows(rng, H, D)
+    want, size = _product(rows, w, D)
+    nb = -(-D // 32)
+    rows[:, 17 * nb:] = 255
+    w[:, 17 * nb:] = 255
+    y = spp.mx4_product(ctx, torch.from_numpy(rows).to(DEV), torch.from_numpy(w).to(DEV), D, dtype=torch.float32)
+    _close(y, want, size, D, torch.float32)
+    g = spp.mx4_weight_grad(ctx, [(torch.from_numpy(rows).to(DEV), n, None, y)], H, D)[0]
+    x, v = R.values(rows, D), y.double().cpu().numpy()
+    _close(g, v.T @ x, np.abs(v).T @ np.abs(x), 3 * n, torch.float32)
+
+
+def test_no_lists_and_empty_lists(ctx):
+    D, H = 64, 32
+    w = spp.mx4_quantize(ctx, torch.randn(H, D, device=DEV))
+    spp.mx4_product_multi(ctx, [], w, D)
+    g = spp.mx4_weight_grad(ctx, [], H, D, groups=3, out=torch.full((3, H, D), 5.0, device=DEV))
+    assert int(g.count_nonzero()) == 0
+    none = torch.zeros(0, spp.mx4_row_bytes(D), dtype=torch.uint8, device=DEV)
+    y = torch.zeros(0, H, device=DEV)
+    spp.mx4_product_multi(ctx, [(none, 0, None, y)] * 3, w, D)
+    g = spp.mx4_weight_grad(ctx, [(none, 0, None, y)] * 3, H, D, out=torch.full((1, H, D), 5.0, device=DEV))
+    assert int(g.count_nonzero()) == 0
+    some = torch.zeros(9, spp.mx4_row_bytes(D), dtype=torch.uint8, device=DEV)
+    out = torch.full((9, H), 3.0, device=DEV)
+    zero = torch.zeros(1, dtype=torch.int64, device=DEV)
+    spp.mx4_product_multi(ctx, [(some, 9, zero, out)], w, D)
+    assert (out == 3).all()
+
+
+def test_on_a_stream_that_is_not_the_current_one():
+    """The context's stream does the work and owns what the calls allocate; the caller orders the streams."""
+    side = torch.cuda.Stream()
+    c = spp.Context(0, side)
+    x = torch.randn(5000, 128, device=DEV)
+    wf = torch.randn(256, 128, device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    rows, w = spp.mx4_quantize(c, x, sync=False), spp.mx4_quantize(c, wf, sync=False)
+    y = spp.mx4_product(c, rows, w, 128, sync=False)
+    g = spp.mx4_weight_grad(c, [(rows, 5000, None, y)], 256, 128, sync=False)
+    opt = spp.AdamW(c, [wf], state_bits=8)
+    opt.step([g[0]], sync=False)
+    m, v = opt.state(sync=False)
+    back = spp.mx4_dequantize(c, rows, 128, sync=False)
+    torch.cuda.current_stream().wait_stream(side)
+    want = back.double() @ torch.from_numpy(R.values(w.cpu().numpy(), 128)).to(DEV).T
+    assert (y.double() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 1e-3
+    assert torch.allclose(g[0].double(), y.double().T @ back.double(), rtol=1e-4, atol=1e-2)
+    assert torch.isfinite(m[0]).all() and float(m[0].abs().max()) > 0
+    c.close()
