@@ -295,11 +295,12 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
     flush(now);
 }
 
-// The pieces of 64 elements side by side are added by a workgroup's wavefronts in turn, then the wavefronts' sums: always in the same
-// order.
+// The pieces of 256 elements side by side, four a lane, are added by a workgroup's wavefronts in turn, then the wavefronts' sums:
+// always in the same order.
 constexpr int kSumWaves = 16;
+typedef double f64x4 __attribute__((ext_vector_type(4)));
 __global__ void __launch_bounds__(64 * kSumWaves) mx4_grad_sum_kernel(GradArgs a) {
-    __shared__ double part[kSumWaves][kWave];
+    __shared__ f64x4 part[kSumWaves][kWave];
     const Lists lists(a.t, a.chunk);
     const int total = lists.total(), group = blockIdx.y, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, l = lane_id();
     const int splits = a.splits < total ? a.splits : total;
@@ -312,26 +313,45 @@ __global__ void __launch_bounds__(64 * kSumWaves) mx4_grad_sum_kernel(GradArgs a
         lo = (int)((((int64_t)first + 1) * splits - 1) / total);
         hi = (int)((((int64_t)last + 1) * splits - 1) / total);
     }
-    for (int64_t i0 = (int64_t)blockIdx.x * kWave; i0 < size; i0 += (int64_t)gridDim.x * kWave) {
-        const int64_t i = i0 + l;
-        const float* p = a.pieces + group * size + (i < size ? i : size - 1);
-        double sum = 0.0;
-        int s = lo + wave;
-        for (; s + 7 * waves <= hi; s += 8 * waves) {
-            float v[8];
+    const int64_t i = ((int64_t)blockIdx.x * kWave + l) * 4;
+    // a vector at the matrix' end begins earlier: its last elements are the matrix' last
+    const int64_t at = size < 4 ? 0 : i + 4 <= size ? i : size - 4;
+    const float* p = a.pieces + group * size + at;
+    f64x4 sum = {0.0, 0.0, 0.0, 0.0};
+    auto add = [&](f32x4 v) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = p[(int64_t)(s + k * waves) * size];
+        for (int k = 0; k < 4; ++k) sum[k] += (double)v[k];
+    };
+    auto take = [&](int s) {
+        const float* from = p + (int64_t)s * size;
+        if (size >= 4) return reinterpret_cast<const Loose<f32x4>*>(from)->v;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < (int)size; ++k) v[k] = from[k];
+        return v;
+    };
+    int s = lo + wave;
+    for (; s + 7 * waves <= hi; s += 8 * waves) {
+        f32x4 v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += v[k];
-        }
-        for (; s <= hi; s += waves) sum += p[(int64_t)s * size];
-        __syncthreads();
-        part[wave][l] = sum;
-        __syncthreads();
-        if (wave == 0 && i < size) {
-            for (int k = 1; k < waves; ++k) sum += part[k][l];
-            a.dw[group * size + i] = (float)sum;
-        }
+        for (int k = 0; k < 8; ++k) v[k] = take(s + k * waves);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) add(v[k]);
+    }
+    for (; s + 3 * waves <= hi; s += 4 * waves) {
+        f32x4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = take(s + k * waves);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add(v[k]);
+    }
+    for (; s <= hi; s += waves) add(take(s));
+    part[wave][l] = sum;
+    __syncthreads();
+    if (wave == 0) {
+        for (int k = 1; k < waves; ++k) sum += part[k][l];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (at + k >= i && at + k < size) a.dw[group * size + at + k] = (float)sum[k];
     }
 }
 
@@ -358,9 +378,9 @@ static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
         kernel<<<(unsigned)(a.splits * tiles), S::threads, S::lds, ctx->stream>>>(a);
         SPP_HIP(hipGetLastError());
     }
-    const int64_t sums = (size + kWave - 1) / kWave;
-    const int waves = a.splits > 64 ? kSumWaves : a.splits > 16 ? 8 : 4;
-    mx4_grad_sum_kernel<<<dim3((unsigned)(sums < 65536 ? sums : 65536), n_groups), 64 * waves, 0, ctx->stream>>>(a);
+    const int64_t sums = (size + 4 * kWave - 1) / (4 * kWave);       // at most 2^20: SPP_MAX_HIDDEN rows of SPP_MX4_MAX_COLS
+    const int each = a.splits / n_groups + 1, waves = each > 64 ? kSumWaves : each > 16 ? 8 : 4;
+    mx4_grad_sum_kernel<<<dim3((unsigned)sums, n_groups), 64 * waves, 0, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
