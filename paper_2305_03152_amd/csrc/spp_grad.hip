@@ -25,6 +25,7 @@ struct GradArgs {
     int32_t  D, H, nb, rb;
     int32_t  splits, tiles_d;
     int32_t  chunk;        // rows of a chunk
+    int32_t  direct;       // one run and one group: its sums are dW
 };
 
 // dY as bf16 numbers that add up to it exactly: one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
@@ -82,8 +83,9 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
     // the tiles of a run, which read the same rows, share an XCD's L2
     const int id = (int)own_piece();
     const int tile = id % tiles, split = id / tiles;
-    if (split >= splits) return;
-    const int from = (int)((int64_t)split * total / splits), to = (int)((int64_t)(split + 1) * total / splits);
+    if (split >= splits && !(a.direct && split == 0)) return;
+    // (total 0: no chunk, and dW is zeros)
+    const int from = total ? (int)((int64_t)split * total / splits) : 0, to = total ? (int)((int64_t)(split + 1) * total / splits) : 0;
     const int h0 = tile / a.tiles_d * S::th, d0 = tile % a.tiles_d * S::td;
     const int wave = threadIdx.x >> 6, l = lane_id();
     const int wh = wave / WD * (16 * FH), wd = wave % WD * 64;
@@ -248,7 +250,7 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
     auto flush = [&](int g) {
         // from values made anew: addresses worked out ahead of the loop would take the registers that it needs
         const int lane = spp::here(l);
-        float* out = a.pieces + (int64_t)(split + g) * a.H * a.D;
+        float* out = a.direct ? a.dw : a.pieces + (int64_t)(split + g) * a.H * a.D;
 #pragma unroll
         for (int f = 0; f < FH; ++f)
 #pragma unroll
@@ -260,10 +262,13 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
                 }
     };
     const int n = to - from;
-    load(0, from, true);
-    if (S::ahead > 1) load(S::ahead - 1, from + 1, n > 1);
     clear();
-    int now = group[0];
+    int now = 0;
+    if (n > 0) {
+        load(0, from, true);
+        if (S::ahead > 1) load(S::ahead - 1, from + 1, n > 1);
+        now = group[0];
+    }
     for (int j = 0; j < n; j += 2) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -355,6 +360,7 @@ __global__ void __launch_bounds__(64 * kSumWaves) mx4_grad_sum_kernel(GradArgs a
     }
 }
 
+constexpr int kFewGradRows = 128;
 template <class T, int WH, int WD, int FH>
 static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
     typedef GradShape<T, WH, WD, FH> S;
@@ -370,25 +376,32 @@ static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
     const int64_t at_once = (int64_t)ctx->num_cu * (fit < 1 || wish < 1 ? 1 : fit < wish ? fit : wish);
     int64_t splits = at_once / tiles;
     if (splits > (chunks + 1) / 2) splits = (chunks + 1) / 2;
+    if (chunks * S::rows <= kFewGradRows) splits = 1;
     a.splits = (int32_t)(splits < 1 ? 1 : splits);
-    SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float)));
+    a.direct = !sum_only && a.splits == 1 && n_groups == 1;
+    if (!a.direct) SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float)));
     a.pieces = ctx->gradws.as<float>();
     if (!sum_only) {
         SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), S::lds));
         kernel<<<(unsigned)(a.splits * tiles), S::threads, S::lds, ctx->stream>>>(a);
         SPP_HIP(hipGetLastError());
     }
+    if (a.direct) return SPP_OK;
     const int64_t sums = (size + 4 * kWave - 1) / (4 * kWave);       // at most 2^20: SPP_MAX_HIDDEN rows of SPP_MX4_MAX_COLS
     const int each = a.splits / n_groups + 1, waves = each > 64 ? kSumWaves : each > 16 ? 8 : 4;
     mx4_grad_sum_kernel<<<dim3((unsigned)sums, n_groups), 64 * waves, 0, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
-// Tiles of dW: as few as 256 x 256 (128 columns of up to 64 wavefront pairs) allow, of as few wavefronts as these need.  The larger
-// the tile, the less is read from LDS per product and the less often dY and X are read.
+// Tiles of dW: as few as 256 x 256 (of 128 columns: 256 x 128) allow, of as few wavefronts as these need.  The larger the tile, the
+// less is read from LDS per product and the less often dY and X are read.  kFewGradRows rows and less take tiles of 128 x 128 and one
+// run, so that more CUs have something to write and no pieces need adding (100 rows of 768 with 1024 gradients in bf16 10 us,
+// 21 with large tiles and two launches; 1000 rows 32 and 25).
 template <class T>
-static int grad_of(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
+static int grad_of(spp_ctx* ctx, GradArgs& a, int n_groups, int64_t most) {
     const int tiles = (a.H + 255) / 256, h = (a.H + tiles - 1) / tiles;
+    const bool sum_only = most == 0;
+    if (most <= kFewGradRows && a.D > 64 && h > 64) return launch_grad<T, 2, 2, 4>(ctx, a, n_groups, sum_only);
     if (a.D > 128) {
         if (h > 128) return launch_grad<T, 2, 4, 8>(ctx, a, n_groups, sum_only);
         return h > 64 ? launch_grad<T, 2, 4, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 1, 4, 4>(ctx, a, n_groups, sum_only);
@@ -415,8 +428,8 @@ extern "C" int spp_mx4_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int3
     a.dw = d_grad; a.D = D; a.H = H; a.nb = mx4_blocks(D); a.rb = mx4_bytes(D);
     hipStream_t st = ctx->stream;
     ScopedTimer timer(ctx, SPP_T_LAYER, st);
-    SPP_TRY(type == SPP_F32 ? grad_of<float>(ctx, a, n_groups, most == 0) : type == SPP_F16 ? grad_of<_Float16>(ctx, a, n_groups, most == 0)
-                                                                                          : grad_of<__bf16>(ctx, a, n_groups, most == 0));
+    SPP_TRY(type == SPP_F32 ? grad_of<float>(ctx, a, n_groups, most) : type == SPP_F16 ? grad_of<_Float16>(ctx, a, n_groups, most)
+                                                                                          : grad_of<__bf16>(ctx, a, n_groups, most));
     if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(st));
     return SPP_OK;
 }
