@@ -252,12 +252,36 @@ __global__ void __launch_bounds__(kAdamBlock) adamw_load_kernel(AdamTable t) {
     }
 }
 __global__ void __launch_bounds__(kAdamBlock) adamw_values_kernel(AdamTable t) {
+    constexpr int R = kAdamPer / 4;
     const uint32_t chunk = blockIdx.x, j = chunk_owner(t, chunk);
     const int64_t n = t.n[j], at = (int64_t)(chunk - t.first[j]) * kAdamChunk;
     const bool wide = t.kind[j] & 16;
+    if (wide && n - at >= kAdamChunk) {                     // all codes asked for before any is worked on
+        const uint32_t* pm = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.m[j]) + at) + threadIdx.x;
+        const uint32_t* pv = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.v[j]) + at) + threadIdx.x;
+        const float* ps = t.scale[j] + 2 * (at / kAdamShared + (threadIdx.x >> 6));
+        uint32_t cm[R], cv[R];
+        float sm[R], sv[R];
 #pragma unroll
-    for (int round = 0; round < kAdamPer / 4; ++round) {
-        const int64_t i = at + (round * kAdamBlock + (int)threadIdx.x) * 4;
+        for (int r = 0; r < R; ++r) {
+            cm[r] = pm[r * kAdamBlock];
+            cv[r] = pv[r * kAdamBlock];
+            sm[r] = ps[2 * r * (kAdamBlock / kWave)];
+            sv[r] = ps[2 * r * (kAdamBlock / kWave) + 1];
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t i = at + (r * kAdamBlock + (int)threadIdx.x) * 4;
+            float m[4], v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { m[k] = value_m((cm[r] >> (8 * k)) & 255u, sm[r]); v[k] = value_v((cv[r] >> (8 * k)) & 255u, sv[r]); }
+            store4<float>(t.p[j], i, 4, true, m);
+            store4<float>(const_cast<void*>(t.g[j]), i, 4, true, v);
+        }
+        return;
+    }
+    for (int r = 0; r < R; ++r) {
+        const int64_t i = at + (r * kAdamBlock + (int)threadIdx.x) * 4;
         if (i >= n) break;
         const int have = n - i >= 4 ? 4 : (int)(n - i);
         float m[4], v[4];
