@@ -12,7 +12,10 @@
 // zero, and their updates would be m / eps.  For the same reason a v that is not zero keeps at least the smallest code.  The
 // update itself uses the moments before they are rounded to 8 bits.
 //
-// All of it is element by element and bound by HBM: 28 bytes per fp32 parameter and gradient with moments in 32 bits, 16 in 8.
+// All of it is element by element.  With moments in 32 bits it is bound by HBM: 128M fp32 parameters and bf16 gradients, 26 bytes each,
+// 618 us, 5.4 TB/s.  In 8 bits, 14 bytes each, 327 us, 5.5 TB/s: as much by its arithmetic (some 80 instructions an element, a root
+// and a quotient rounded correctly among them).  Chunks in the order of the workgroups: with a contiguous part per XCD, as
+// streams that are only written like it, 650 and 390 us.
 #include "spp_mx4.h"
 
 #include <math.h>

@@ -16,6 +16,10 @@ namespace spp {
 // Both operands have the rows as the axis that is summed over, so their tiles lie in LDS as they lie in memory and are read
 // transposed (ds_read_b64_tr_b16).  A chunk's operands are asked for two chunks ahead, into registers; X is unpacked to bf16 on
 // its way to LDS, dY cut into its pieces.
+//
+// Bound by HBM where dW is one tile: 2.56M rows of 128 with 256 gradients in bf16 270 us, 5.5 TB/s; fp16 433, fp32 (half the rows) 331, by
+// the cutting and its two and three products.  For larger dW by the turns that writing a chunk to LDS and multiplying it take:
+// 390k rows of 768 with 1024 in bf16 587 us, 1020 TFLOP/s.
 constexpr int kGradPad = 16;         // elements behind an LDS row: the four rows that 16 lanes read at once are then 4 x 32 bytes of other banks
 
 struct GradArgs {

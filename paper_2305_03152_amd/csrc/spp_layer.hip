@@ -15,7 +15,7 @@ struct ProductArgs {
     RowTable       t;
     const uint8_t* w;
     int32_t        D, H, nb, rb;
-    int32_t        ls;           // bytes of a row of W in LDS: an odd number of 16, so that 16 rows lie in banks of their own
+    int32_t        ls;           // bytes of a row of W in LDS: an odd number of 16, so that a lane group's 16 rows lie in banks of their own
     uint32_t       magic;        // ceil(2^32 / (rb / 16))
     int32_t        fill;         // workgroups that few rows are dealt out to
     int32_t        w_lds;        // bytes of W in LDS; behind them, per wavefront, room for rows of Y on their way:
@@ -59,7 +59,8 @@ __device__ __forceinline__ void put_whole(T* y, int64_t ld, const f32x4 (&acc)[4
 }
 
 // A wavefront's 16 RN rows of Y on their way to memory where they do not begin with a line each.  They are put together in LDS and
-// written by whole 16-byte pieces, side by side; the ends of a row or a run, less than a piece, by element.
+// written by whole 16-byte pieces, side by side; the ends of a row or a run, less than a piece, by element.  Stored as they come, 2.56M
+// rows 100 -> 172 in bf16 took 432 us, so 237 (4.5 TB/s).
 //   run    the rows follow each other without a gap and fit: all of them are put together as one run of bytes
 //   lines  64 columns of every row at a time, each byte where it lies in its 128-byte line: what they fill of lines goes out, the
 //          begun line stays for the next 64
@@ -196,7 +197,11 @@ struct RowsOut {
 // The ordinary form, for D up to 768.  A wavefront holds its 16 RN rows of X in registers, all columns of them, and goes over the
 // columns of Y 64 at a time; W comes from LDS, where a workgroup's wavefronts share it.  If all of W fits it stays there
 // (Stream false), else 64 of its rows at a time, the next ones asked for while these are used.  X is read once and Y, which is most
-// of what moves, written once.
+// of what moves, written once, past the L2, which reads of the next rows would otherwise share with it (2.56M rows 128 -> 256 301 us
+// with plain stores, 250 so, both from a cached X).  Bound by HBM for narrow rows: 2.56M rows 128 -> 256 in bf16 264 us, 5.6 TB/s;
+// 400k rows 256 -> 1024 157 us, 5.7 TB/s; for wide ones by the wavefronts' waits for each other at every 64 columns: 390k
+// rows 768 -> 1024 250 us, 2.4 PFLOP/s.  Two rows of 16 per wavefront: one reads W from LDS twice as often, four (768 -> 1024) leave a
+// wavefront per SIMD.  Eight wavefronts share a stream of W, four where rows are short (256 -> 1024 167 and 157 us, 768 -> 1024 250 and 279).
 template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
 __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t ws[];
@@ -353,8 +358,9 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     }
 }
 
-// The form for wider rows, and for calls of few rows, whose W is better read once by those who need it: a workgroup takes a tile of
-// TR rows into LDS and its wavefronts take 16 RN of them by 64 columns of Y at a time, W straight from memory.
+// The form for wider rows, of which a wavefront's registers would not hold enough: a workgroup takes a tile of TR rows into LDS and its
+// wavefronts take 16 RN of them by 64 columns of Y at a time, W straight from memory.  300k rows 800 -> 256 in bf16: 158 us, 1.7 TB/s;
+// bound by the way of W's blocks from the L2, a step of 128 columns at a time.
 template <class T, int TR, int RN>
 __global__ void __launch_bounds__(kProdBlock) mx4_product_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t xs[];
@@ -472,7 +478,7 @@ static int launch_product(spp_ctx* ctx, const ProductArgs& a) {
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
-constexpr int kHeldW = 65536;            // LDS for a W that stays
+constexpr int kHeldW = 65536;            // LDS for a W that stays: two workgroups fit a CU
 constexpr int kRowOut = 768;             // bytes of Y's rows that go out in one run
 template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
 static int launch_rows_as(spp_ctx* ctx, ProductArgs& a) {
@@ -510,10 +516,8 @@ static int launch_rows(spp_ctx* ctx, ProductArgs& a) {
         return lines ? launch_rows_as<T, KS, 2, 4, false, true>(ctx, a) : launch_rows_as<T, KS, 1, 4, false, false>(ctx, a);
     return lines ? launch_rows_as<T, KS, 2, KS <= 3 ? 4 : 8, true, true>(ctx, a) : launch_rows_as<T, KS, KS >= 4 ? 1 : 2, 8, true, false>(ctx, a);
 }
-constexpr int kFewRows = 64;
 template <class T>
-static int product_of(spp_ctx* ctx, ProductArgs& a, int64_t most) {
-    if (most <= kFewRows) return launch_product<T, 64, 1>(ctx, a);
+static int product_of(spp_ctx* ctx, ProductArgs& a) {
     const int rv = a.rb / 16;
     a.ls = 16 * (rv | 1);
     a.magic = (uint32_t)((0x100000000ull + rv - 1) / rv);
@@ -543,7 +547,7 @@ extern "C" int spp_mx4_product(spp_ctx* ctx, const spp_row_list* lists, int32_t 
         a.D = D; a.H = H; a.nb = mx4_blocks(D); a.rb = mx4_bytes(D);
         SPP_HIP(hipSetDevice(ctx->device));
         ScopedTimer timer(ctx, SPP_T_LAYER, ctx->stream);
-        SPP_TRY(type == SPP_F32 ? product_of<float>(ctx, a, most) : type == SPP_F16 ? product_of<_Float16>(ctx, a, most) : product_of<__bf16>(ctx, a, most));
+        SPP_TRY(type == SPP_F32 ? product_of<float>(ctx, a) : type == SPP_F16 ? product_of<_Float16>(ctx, a) : product_of<__bf16>(ctx, a));
     }
     if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(ctx->stream));
     return SPP_OK;

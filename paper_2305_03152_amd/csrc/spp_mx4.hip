@@ -5,7 +5,8 @@
 //
 // Both directions move each byte once and are bound by HBM.  A lane has 8 columns, so four lanes share a block and find its
 // largest value with two exchanges between neighbours; the lanes of a wavefront read and write side by side.  The conversion
-// instruction takes the scale and rounds as the format asks.
+// instruction takes the scale and rounds as the format asks.  800k rows of 768 fp16: 273 us, and 274 back to bf16, 5.7 TB/s each; 2M rows of
+// 100 in fp32 166 and 169, in fp16, 200-byte rows, 107 and 79.
 #include "spp_mx4.h"
 
 namespace spp {
