@@ -200,8 +200,9 @@ struct RowsOut {
 // of what moves, written once, past the L2, which reads of the next rows would otherwise share with it (2.56M rows 128 -> 256 301 us
 // with plain stores, 250 so, both from a cached X).  Bound by HBM for narrow rows: 2.56M rows 128 -> 256 in bf16 264 us, 5.6 TB/s;
 // 400k rows 256 -> 1024 157 us, 5.7 TB/s; for wide ones by the wavefronts' waits for each other at every 64 columns: 390k
-// rows 768 -> 1024 250 us, 2.4 PFLOP/s.  Two rows of 16 per wavefront: one reads W from LDS twice as often, four (768 -> 1024) leave a
-// wavefront per SIMD.  Eight wavefronts share a stream of W, four where rows are short (256 -> 1024 167 and 157 us, 768 -> 1024 250 and 279).
+// rows 768 -> 1024 225 to 230 us, 2.7 PFLOP/s.  Two rows of 16 per wavefront, three where kManyRows says so: one reads W from LDS twice as
+// often, four (768 -> 1024) leave a wavefront per SIMD.  Eight wavefronts share a stream of W, four where rows are short (256 -> 1024
+// 167 and 157 us, 768 -> 1024 with two rows of 16 250 and 279).
 template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
 __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t ws[];
@@ -479,6 +480,11 @@ static int launch_product(spp_ctx* ctx, const ProductArgs& a) {
     return SPP_OK;
 }
 constexpr int kHeldW = 65536;            // LDS for a W that stays: two workgroups fit a CU
+// Rows per CU from which wide rows with a result of 16 bits go 48 to a wavefront instead of 32: W is read from LDS two thirds as
+// often, but tiles are larger and the last round of them emptier.  768 -> 1024, 32 and 48: 100k rows 75 and 92 us, 200k 149 both, 300k
+// 209 and 200, 390k 247 and 230, 800k 533 and 489; 500 -> 1024: 100k 58 and 71, 200k 111 both, 390k 191 and 176, 800k 410 and 387.
+// (150k rows, a round less: 110 and 100, not taken.)  In fp32 the stores bound both: 390k rows 355 and 362.
+constexpr int kManyRows = 2 * 8 * 48;
 constexpr int kRowOut = 768;             // bytes of Y's rows that go out in one run
 template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
 static int launch_rows_as(spp_ctx* ctx, ProductArgs& a) {
@@ -514,6 +520,11 @@ static int launch_rows(spp_ctx* ctx, ProductArgs& a) {
     for (int j = 0; j < a.t.n_lists; ++j) lines = lines && ((uintptr_t)a.t.y[j] | (uint64_t)(a.t.ld[j] * (int64_t)sizeof(T))) % 128 == 0;
     if (ht * 64 * a.ls <= kHeldW)
         return lines ? launch_rows_as<T, KS, 2, 4, false, true>(ctx, a) : launch_rows_as<T, KS, 1, 4, false, false>(ctx, a);
+    if constexpr (KS >= 4 && sizeof(T) == 2) {
+        int64_t rows = 0;
+        for (int j = 0; j < a.t.n_lists; ++j) rows += a.t.n[j];
+        if (lines && rows >= kManyRows * ctx->num_cu) return launch_rows_as<T, KS, 3, 8, true, true>(ctx, a);
+    }
     return lines ? launch_rows_as<T, KS, 2, KS <= 3 ? 4 : 8, true, true>(ctx, a) : launch_rows_as<T, KS, KS >= 4 ? 1 : 2, 8, true, false>(ctx, a);
 }
 template <class T>

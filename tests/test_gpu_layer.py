@@ -349,3 +349,38 @@ def test_on_a_stream_that_is_not_the_current_one():
     assert torch.allclose(g[0].double(), y.double().T @ back.double(), rtol=1e-4, atol=1e-2)
     assert torch.isfinite(m[0]).all() and float(m[0].abs().max()) > 0
     c.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,H,ld", [(385, 320, 320), (512, 300, 320), (640, 255, 256), (768, 192, 192), (700, 260, 384)])
+def test_many_wide_rows_in_lists_of_any_length(ctx, dtype, D, H, ld):
+    """Enough wide rows that a wavefront takes more of them at a time: lists that end inside its rows, inside a workgroup's and with
+    them, one whose count is on the device and below its room, two groups; nothing between or behind the rows is touched."""
+    rng = np.random.default_rng(D + H)
+    sizes = [(0, 0), (1, 1), (47, 47), (48, 48), (49, 49), (383, 383), (384, 384), (385, 385), (100, 0), (70000, 61234), (200001, 200001)]
+    pool = _rows(rng, 4099, D)
+    w = _rows(rng, 2 * H, D).reshape(2, H, -1)
+    items, plain = [], []
+    for j, (cap, n) in enumerate(sizes):
+        rows = pool[rng.integers(0, len(pool), cap)]
+        rows[n:] = 255
+        buf = torch.full((cap * ld + 64,), 7.0, dtype=dtype, device=DEV)
+        y = torch.as_strided(buf, (cap, H), (ld, 1))
+        count = torch.tensor([n], dtype=torch.int64, device=DEV) if cap != n or j % 2 else None
+        items.append((torch.from_numpy(rows).to(DEV), cap, count, y, j % 2))
+        plain.append((rows, n, buf))
+    spp.mx4_product_multi(ctx, spp.RowLists(items), torch.from_numpy(w).to(DEV), D)
+    wv = torch.from_numpy(R.values(w.reshape(2 * H, -1), D)).to(DEV).float().view(2, H, D)
+    for (rows, n, buf), it in zip(plain, items):
+        if n:
+            pick = np.unique(np.concatenate([np.arange(min(n, 400)), np.arange(max(0, n - 400), n), rng.integers(0, n, 400)]))
+            want, size = _product(rows[pick], w[it[4]], D)
+            _close(it[3][torch.from_numpy(pick).to(DEV)], want, size, D, dtype)
+            for at in range(0, n, 50000):
+                part = rows[at:min(n, at + 50000)]
+                full = torch.from_numpy(R.values(part, D)).to(DEV).float() @ wv[it[4]].T
+                assert torch.allclose(it[3][at:at + len(part)].float(), full, rtol=2.0 ** -7, atol=1e-4 * float(full.abs().max()))
+        keep = torch.ones(buf.numel(), dtype=torch.bool, device=DEV)
+        if n:
+            keep.as_strided((n, H), (ld, 1)).fill_(False)
+        assert (buf[keep] == 7).all()
