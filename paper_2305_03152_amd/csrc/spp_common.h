@@ -62,6 +62,44 @@ struct DevBuf {
     template <class T> T* as() const { return reinterpret_cast<T*>(ptr); }
 };
 
+// One whose address recorded work (a HIP graph) may hold: a replay writes to the block it was recorded with, however often the
+// buffer has grown since.  A block that a recording has used is therefore kept until the buffer is released, and while the stream
+// records nothing is freed (that would wait for the device).  Allocating is not an operation of the stream: it is done in the thread's
+// relaxed mode, so that a recording of any mode may begin with the call that needs the block.
+struct RecordedBuf : DevBuf {
+    bool               recorded = false;     // a recording has used the block
+    std::vector<void*> outgrown;
+    int reserve(size_t need, hipStream_t stream) {
+        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+        SPP_HIP(hipStreamIsCapturing(stream, &status));
+        const bool recording = status != hipStreamCaptureStatusNone;
+        if (need > bytes) {
+            if (ptr && (recorded || recording)) {
+                try { outgrown.push_back(ptr); } catch (...) {
+                    set_error("out of host memory");
+                    return SPP_E_OOM;
+                }
+                ptr = nullptr;
+                bytes = 0;
+            }
+            recorded = false;
+            hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+            if (recording) SPP_HIP(hipThreadExchangeStreamCaptureMode(&mode));
+            const int rc = DevBuf::reserve(need);
+            if (recording) SPP_HIP(hipThreadExchangeStreamCaptureMode(&mode));
+            SPP_TRY(rc);
+        }
+        recorded = recorded || recording;
+        return SPP_OK;
+    }
+    void release() {
+        DevBuf::release();
+        for (void* p : outgrown) (void)hipFree(p);
+        outgrown.clear();
+        recorded = false;
+    }
+};
+
 constexpr int kNumTimers = SPP_T_COUNT;
 constexpr int kTotalsWords = 16;
 constexpr int kTotalMax = 16384;         // grid_total (spp_vip.hip): most workgroups,
@@ -153,7 +191,7 @@ struct spp_ctx {
     int         dedup_lds_set = 0;      // the LDS dedup kernel of the sampler has been allowed its 76 KB
     int         x_lds_set = 0;          // the two kernels of the chunked layout have been allowed theirs
     int         push_lds_set = 0;       // dynamic LDS of the binned push kernels
-    spp::DevBuf gradws;                 // weight gradient: what each run of rows adds to it
+    spp::RecordedBuf gradws;            // weight gradient: what each run of rows adds to it
     int         vip_hops = 0;           // hops of the last propagation; negative: with given probabilities (always pushed)
     // timing: while enabled every timed piece of device work gets its own pair of events
     int         timing = 0;

@@ -383,7 +383,7 @@ static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
     if (chunks * S::rows <= kFewGradRows) splits = 1;
     a.splits = (int32_t)(splits < 1 ? 1 : splits);
     a.direct = !sum_only && a.splits == 1 && n_groups == 1;
-    if (!a.direct) SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float)));
+    if (!a.direct) SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float), ctx->stream));
     a.pieces = ctx->gradws.as<float>();
     if (!sum_only) {
         SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), S::lds));
