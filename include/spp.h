@@ -409,6 +409,7 @@ int  spp_mx4_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int32_t n_list
  *       p' = (1 - lr wd) p - lr/(1-b1^t) * m' / (sqrt(v') / sqrt(1-b2^t) + eps)          t = 1 at the first step
  *     computed in fp32.  An element whose v' would not be finite (its gradient is not, or its square is not) keeps p, m and v;
  *     such elements are counted (spp_ctx_totals, out[9]).  p: SPP_F32 or SPP_BF16 (rounded to nearest, ties to even); g any type.
+ *     A step is not recorded into a HIP graph, whose replays would repeat the one t: SPP_E_ARG while the stream records.
  *     state_bits 32: d_m and d_v are fp32[n], zero before the first step.
  *     state_bits 8:  d_m and d_v are uint8[n], d_scale fp32[2 * ceil(n / SPP_ADAMW_BLOCK)], all zero before the first step.
  *       Each run of SPP_ADAMW_BLOCK elements has two scales, for m and for sqrt(v), such that the largest of the run is the

@@ -951,7 +951,7 @@ class AdamW:
         self._views = tuple([s[k].view(p.shape) for s, p in zip(self._state, self.params)] for k in (0, 1)) if state_bits == 32 else None
 
     def step(self, grads: Sequence[torch.Tensor], lr: Optional[float] = None, sync: bool = True):
-        """One step with a gradient (any of the three types) for every parameter."""
+        """One step with a gradient (any of the three types) for every parameter; not while the stream records a graph."""
         if len(grads) != len(self.params):
             raise SppError("one gradient per parameter is needed")
         for (a, p, n), g in zip(self._items, grads):

@@ -353,13 +353,18 @@ extern "C" int spp_adamw_step(spp_ctx* ctx, const spp_adamw_tensor* tensors, int
                   hyper->weight_decay >= 0.0,
               SPP_E_ARG, "spp_adamw_step: lr %g, eps %g, weight decay %g", hyper->lr, hyper->eps, hyper->weight_decay);
     SPP_CHECK(t >= 1, SPP_E_ARG, "spp_adamw_step: step %lld (the first is 1)", (long long)t);
+    SPP_HIP(hipSetDevice(ctx->device));
+    // the bias corrections of step t and the learning rate are arguments of the kernel: replays would repeat step t
+    hipStreamCaptureStatus recording = hipStreamCaptureStatusNone;
+    SPP_HIP(hipStreamIsCapturing(ctx->stream, &recording));
+    SPP_CHECK(recording == hipStreamCaptureStatusNone, SPP_E_ARG, "spp_adamw_step: the stream records a graph, whose replays would repeat step %lld",
+              (long long)t);
     AdamHyper h;
     h.b1 = (float)b1; h.c1 = (float)(1.0 - b1); h.b2 = (float)b2; h.c2 = (float)(1.0 - b2);
     h.rs = (float)(1.0 / sqrt(1.0 - pow(b2, (double)t)));
     h.eps = (float)hyper->eps;
     h.decay = (float)(1.0 - hyper->lr * hyper->weight_decay);
     h.step = (float)(hyper->lr / (1.0 - pow(b1, (double)t)));
-    SPP_HIP(hipSetDevice(ctx->device));
     ScopedTimer timer(ctx, SPP_T_ADAMW, ctx->stream);
     int64_t* skipped = ctx->totals + 9;
     SPP_TRY(adam_launches(tensors, n_tensors, state_bits, [&](const AdamTable& table, unsigned chunks) {

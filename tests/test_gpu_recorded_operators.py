@@ -77,3 +77,30 @@ def test_gradient_recorded_as_a_context_s_first_calls(mode):
             assert torch.equal(b, spp.mx4_weight_grad(c, large, 1024, 768))                  # the context's eager calls go on
         c.close()
         ref.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_is_not_recorded(bits):
+    """Replays of a recorded step would repeat its bias corrections: refused, nothing is recorded, and steps go on as before."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        c = spp.Context(0, side)
+        g = torch.randn(1000, device=DEV)
+        p, q = torch.ones(1000, device=DEV), torch.ones(1000, device=DEV)
+        opt, ref = spp.AdamW(c, [p], state_bits=bits, lr=1e-2), spp.AdamW(c, [q], state_bits=bits, lr=1e-2)
+        opt.step([g])
+        ref.step([g])
+        graph, extra = torch.cuda.CUDAGraph(), torch.zeros(1, device=DEV)
+        with torch.cuda.graph(graph, stream=side):
+            extra.add_(1)
+            with pytest.raises(spp.SppError, match="repeat step 2"):
+                opt.step([g], sync=False)
+        assert opt.t == 1
+        for k in range(3):
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(p, q) and float(extra) == k + 1
+            opt.step([g])
+            ref.step([g])
+        assert torch.equal(p, q) and opt.t == 4
+        c.close()
