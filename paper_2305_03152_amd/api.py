@@ -950,6 +950,12 @@ class AdamW:
                 self._items.append((a, p, n))
         self._views = tuple([s[k].view(p.shape) for s, p in zip(self._state, self.params)] for k in (0, 1)) if state_bits == 32 else None
 
+    @staticmethod
+    def _same(a, p, n):
+        """A parameter may have been given other memory (.data, set_, resize_): of its size and type, or the state does not fit."""
+        if p.numel() != n or not p.is_contiguous() or _TYPES.get(p.dtype) != a.p_type or not p.is_cuda:
+            raise SppError("a parameter is no longer a contiguous tensor of the size and type that it had")
+
     def step(self, grads: Sequence[torch.Tensor], lr: Optional[float] = None, sync: bool = True):
         """One step with a gradient (any of the three types) for every parameter; not while the stream records a graph."""
         if len(grads) != len(self.params):
@@ -957,6 +963,7 @@ class AdamW:
         for (a, p, n), g in zip(self._items, grads):
             if not (g.is_cuda and g.is_contiguous() and g.numel() == n and g.dtype in _TYPES):
                 raise SppError("a gradient must be a contiguous float32, float16 or bfloat16 tensor on the GPU of its parameter's size")
+            self._same(a, p, n)
             a.d_p, a.d_g, a.g_type = p.data_ptr(), g.data_ptr(), _TYPES[g.dtype]
         h = _AdamwHyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.weight_decay)
         _check(load_library().spp_adamw_step(self.ctx._h, self._arr, len(self.params), self.state_bits, C.byref(h), self.t + 1,
@@ -973,6 +980,8 @@ class AdamW:
             if sync:
                 self.ctx.sync()
             return list(self._views[0]), list(self._views[1])
+        for item in self._items:
+            self._same(*item)
         m = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
         v = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
         pm, pv = self._moments(m, v)
@@ -986,6 +995,8 @@ class AdamW:
         for j, (p, a, b) in enumerate(zip(self.params, m, v)):
             if _dev(a, torch.float32, f"m {j}").numel() != p.numel() or _dev(b, torch.float32, f"v {j}").numel() != p.numel():
                 raise SppError(f"moments {j} must be of their parameter's size")
+        for item in self._items:
+            self._same(*item)
         if self.state_bits == 32:
             with torch.cuda.stream(self.ctx.stream):
                 for s, a, b in zip(self._state, m, v):
