@@ -755,7 +755,7 @@ def _new(ctx: Context, shape, dtype) -> torch.Tensor:
 
 
 def _matrix(t: torch.Tensor, cols: Optional[int], name: str) -> torch.Tensor:
-    if not (t.is_cuda and t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
+    if not (t.is_cuda and t.dim() == 2 and (t.numel() == 0 or (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1]))):
         raise SppError(f"{name} must be a 2-D tensor on the GPU whose rows are contiguous")
     if cols is not None and t.shape[1] != cols:
         raise SppError(f"{name} must have {cols} columns, not {t.shape[1]}")
