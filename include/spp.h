@@ -385,7 +385,7 @@ int  spp_mx4_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64
  *                                                              written (a group without rows: zeros)
  *     X and W are the values that the packed rows stand for; sums are formed in fp32 and rounded once to Y's type.  The
  *     gradient is that of the product by W's values; the rows are data and have none.  It adds in an order that the lists'
- *     lengths alone decide, so a call repeated gives the same bits; it keeps some 64 MiB, or one matrix if that is more, and
+ *     counts, D, H, the type and the GPU's number of CUs decide, so the same rows give the same bits, whatever the buffers' n; it keeps some 64 MiB, or one matrix if that is more, and
  *     one matrix per group of device memory with the context.  A call may be recorded into a HIP graph: what it keeps for that stays
  *     where it is, also when later calls need more, until the context is destroyed.  The context has to outlive the graph, and
  *     replays are ordered with the context's other calls, whose memory they share.

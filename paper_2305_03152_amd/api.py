@@ -904,7 +904,7 @@ def mx4_weight_grad(ctx: Context, lists, H: int, D: int, groups: int = 1, out: O
                     sync: bool = True) -> torch.Tensor:
     """float32 [groups, H, D]: for every group the sum of Y_j^T X_j over its lists, Y_j being the product's gradient.
 
-    Zeros for a group without rows.  The same lengths give the same bits.
+    Zeros for a group without rows.  The same rows give the same bits, whatever room the lists' buffers have.
     """
     lists = lists if isinstance(lists, RowLists) else RowLists(lists)
     lists._fit(D, H, groups)

@@ -10,8 +10,9 @@ namespace spp {
 
 // The rows of all lists, in the order of their groups, are cut into chunks, and the chunks into `splits` runs of equal length.  A
 // workgroup has one run and one tile of dW; where its run passes from a group to the next it writes down what it has as piece
-// (run + group) and starts again, and the second kernel adds up each group's pieces in the order of the rows.  No atomics: the
-// same counts give the same bits.
+// (run + group) and starts again, and the second kernel adds up each group's pieces in the order of the rows.  No atomics, and how
+// many runs there are follows from the chunks that the lists have, not from those that their buffers could hold: on GPUs of as
+// many CUs the same counts give the same bits.
 //
 // Both operands have the rows as the axis that is summed over, so their tiles lie in LDS as they lie in memory and are read
 // transposed (ds_read_b64_tr_b16).  A chunk's operands are asked for two chunks ahead, into registers; X is unpacked to bf16 on
@@ -27,10 +28,20 @@ struct GradArgs {
     float*   pieces;       // [splits + groups][H * D]
     float*   dw;           // [groups][H * D]
     int32_t  D, H, nb, rb;
-    int32_t  splits, tiles_d;
+    int32_t  splits, tiles_d;        // runs that the grid and the pieces have room for
+    int32_t  most;         // runs at most, by the matrix's shape
     int32_t  chunk;        // rows of a chunk
     int32_t  direct;       // one run and one group: its sums are dW
 };
+
+constexpr int kFewGradRows = 128;
+// The runs of so many chunks: two chunks for each, but one run for a few rows.  Never more for fewer chunks: the host counts with
+// what the lists can hold and the kernels with what they have.
+__host__ __device__ __forceinline__ int grad_runs(int64_t chunks, int rows, int most) {
+    if (chunks * rows <= kFewGradRows) return 1;
+    const int64_t half = (chunks + 1) / 2;
+    return half < most ? (int)half : most;
+}
 
 // dY as bf16 numbers that add up to it exactly: one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
 // finite value becomes infinite; what is not finite is its first piece alone.
@@ -62,7 +73,7 @@ __device__ __forceinline__ bf16x8 column8(const __bf16* p) {
 
 template <class T, int WH, int WD, int FH>
 struct GradShape {
-    static constexpr int P = Pieces<T>::n;
+    static constexpr int P = Pieces<T>::n, wh = WH, wd = WD, fh = FH;
     static constexpr int rows = P == 1 ? 64 : 32;                    // of a chunk: two buffers of it fit the LDS
     static constexpr int threads = 64 * WH * WD;
     static constexpr int th = 16 * FH * WH, td = 64 * WD;            // the tile of dW: a wavefront has 16 FH x 64 of it
@@ -82,14 +93,13 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
     extern __shared__ __attribute__((aligned(16))) __bf16 lds[];
     const Lists lists(a.t, S::rows);
     const int total = lists.total();
-    const int splits = a.splits < total ? a.splits : total;
+    const int splits = grad_runs(total, S::rows, a.most);
     const int tiles = (int)gridDim.x / a.splits;
     // the tiles of a run, which read the same rows, share an XCD's L2
     const int id = (int)own_piece();
     const int tile = id % tiles, split = id / tiles;
-    if (split >= splits && !(a.direct && split == 0)) return;
-    // (total 0: no chunk, and dW is zeros)
-    const int from = total ? (int)((int64_t)split * total / splits) : 0, to = total ? (int)((int64_t)(split + 1) * total / splits) : 0;
+    if (split >= splits || (total == 0 && !a.direct)) return;          // (no chunk: dW is zeros)
+    const int from = (int)((int64_t)split * total / splits), to = (int)((int64_t)(split + 1) * total / splits);
     const int h0 = tile / a.tiles_d * S::th, d0 = tile % a.tiles_d * S::td;
     const int wave = threadIdx.x >> 6, l = lane_id();
     const int wh = wave / WD * (16 * FH), wd = wave % WD * 64;
@@ -307,12 +317,17 @@ __global__ void __launch_bounds__(64 * WH * WD) mx4_grad_kernel(GradArgs a) {
 // The pieces of 256 elements side by side, four a lane, are added by a workgroup's wavefronts in turn, then the wavefronts' sums:
 // always in the same order.
 constexpr int kSumWaves = 16;
+// The wavefronts that share a group's pieces, by the runs there are; those that a grid with room for more runs has beyond them add nothing.
+__host__ __device__ __forceinline__ int grad_sum_waves(int runs, int groups) {
+    const int each = runs / groups + 1;
+    return each > 64 ? kSumWaves : each > 16 ? 8 : 4;
+}
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 __global__ void __launch_bounds__(64 * kSumWaves) mx4_grad_sum_kernel(GradArgs a) {
     __shared__ f64x4 part[kSumWaves][kWave];
     const Lists lists(a.t, a.chunk);
-    const int total = lists.total(), group = blockIdx.y, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, l = lane_id();
-    const int splits = a.splits < total ? a.splits : total;
+    const int total = lists.total(), group = blockIdx.y, wave = threadIdx.x >> 6, l = lane_id();
+    const int splits = grad_runs(total, a.chunk, a.most), waves = grad_sum_waves(splits, (int)gridDim.y);
     const int64_t size = (int64_t)a.H * a.D;
     // the chunks of the group: from its first list's first to its last list's last
     const uint64_t mine = __ballot(l < a.t.n_lists && (int)a.t.group[l] == group && lists.tiles > 0);
@@ -320,7 +335,7 @@ __global__ void __launch_bounds__(64 * kSumWaves) mx4_grad_sum_kernel(GradArgs a
     if (mine) {
         const int first = lists.first_tile(__builtin_ctzll(mine)), last = __builtin_amdgcn_readlane(lists.upto, 63 - __builtin_clzll(mine)) - 1;
         lo = (int)((((int64_t)first + 1) * splits - 1) / total);
-        hi = (int)((((int64_t)last + 1) * splits - 1) / total);
+        hi = wave < waves ? (int)((((int64_t)last + 1) * splits - 1) / total) : -1;
     }
     const int64_t i = ((int64_t)blockIdx.x * kWave + l) * 4;
     // a vector at the matrix' end begins earlier: its last elements are the matrix' last
@@ -364,24 +379,18 @@ __global__ void __launch_bounds__(64 * kSumWaves) mx4_grad_sum_kernel(GradArgs a
     }
 }
 
-constexpr int kFewGradRows = 128;
-template <class T, int WH, int WD, int FH>
+template <class S>
+static int64_t grad_tiles(const GradArgs& a) { return (int64_t)((a.D + S::td - 1) / S::td) * ((a.H + S::th - 1) / S::th); }
+template <class T, class S>
 static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
-    typedef GradShape<T, WH, WD, FH> S;
-    auto kernel = mx4_grad_kernel<T, WH, WD, FH>;
+    auto kernel = mx4_grad_kernel<T, S::wh, S::wd, S::fh>;
     static LdsLimit limit;
     a.chunk = S::rows;
     a.tiles_d = (a.D + S::td - 1) / S::td;
-    const int64_t tiles = (int64_t)a.tiles_d * ((a.H + S::th - 1) / S::th), size = (int64_t)a.H * a.D;
+    const int64_t tiles = grad_tiles<S>(a), size = (int64_t)a.H * a.D;
     int64_t chunks = 0;
     for (int j = 0; j < a.t.n_lists; ++j) chunks += (a.t.n[j] + (int64_t)S::rows - 1) / S::rows;
-    // as many workgroups as run at once, and two chunks for each
-    const int fit = 163840 / S::lds, wish = 8 / (WH * WD);
-    const int64_t at_once = (int64_t)ctx->num_cu * (fit < 1 || wish < 1 ? 1 : fit < wish ? fit : wish);
-    int64_t splits = at_once / tiles;
-    if (splits > (chunks + 1) / 2) splits = (chunks + 1) / 2;
-    if (chunks * S::rows <= kFewGradRows) splits = 1;
-    a.splits = (int32_t)(splits < 1 ? 1 : splits);
+    a.splits = grad_runs(chunks, S::rows, a.most);
     a.direct = !sum_only && a.splits == 1 && n_groups == 1;
     if (!a.direct) SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float), ctx->stream));
     a.pieces = ctx->gradws.as<float>();
@@ -392,30 +401,42 @@ static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
     }
     if (a.direct) return SPP_OK;
     const int64_t sums = (size + 4 * kWave - 1) / (4 * kWave);       // at most 2^20: SPP_MAX_HIDDEN rows of SPP_MX4_MAX_COLS
-    const int each = a.splits / n_groups + 1, waves = each > 64 ? kSumWaves : each > 16 ? 8 : 4;
-    mx4_grad_sum_kernel<<<dim3((unsigned)sums, n_groups), 64 * waves, 0, ctx->stream>>>(a);
+    mx4_grad_sum_kernel<<<dim3((unsigned)sums, n_groups), 64 * grad_sum_waves(a.splits, n_groups), 0, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
 // Tiles of dW: as few as 256 x 256 (of 128 columns: 256 x 128) allow, of as few wavefronts as these need.  The larger the tile, the
-// less is read from LDS per product and the less often dY and X are read.  kFewGradRows rows and less take tiles of 128 x 128 and one
-// run, so that more CUs have something to write and no pieces need adding (100 rows of 768 with 1024 gradients in bf16 10 us,
-// 21 with large tiles and two launches; 1000 rows 32 and 25).
-template <class T>
-static int grad_of(spp_ctx* ctx, GradArgs& a, int n_groups, int64_t most) {
+// less is read from LDS per product and the less often dY and X are read.
+template <class T, class Use>
+static int grad_shape(const GradArgs& a, Use use) {
     const int tiles = (a.H + 255) / 256, h = (a.H + tiles - 1) / tiles;
-    const bool sum_only = most == 0;
-    if (most <= kFewGradRows && a.D > 64 && h > 64) return launch_grad<T, 2, 2, 4>(ctx, a, n_groups, sum_only);
     if (a.D > 128) {
-        if (h > 128) return launch_grad<T, 2, 4, 8>(ctx, a, n_groups, sum_only);
-        return h > 64 ? launch_grad<T, 2, 4, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 1, 4, 4>(ctx, a, n_groups, sum_only);
+        if (h > 128) return use(GradShape<T, 2, 4, 8>());
+        return h > 64 ? use(GradShape<T, 2, 4, 4>()) : use(GradShape<T, 1, 4, 4>());
     }
     if (a.D > 64) {
-        if (h > 128) return h > 192 ? launch_grad<T, 4, 2, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 3, 2, 4>(ctx, a, n_groups, sum_only);
-        return h > 64 ? launch_grad<T, 2, 2, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 1, 2, 4>(ctx, a, n_groups, sum_only);
+        if (h > 128) return h > 192 ? use(GradShape<T, 4, 2, 4>()) : use(GradShape<T, 3, 2, 4>());
+        return h > 64 ? use(GradShape<T, 2, 2, 4>()) : use(GradShape<T, 1, 2, 4>());
     }
-    if (h > 128) return h > 192 ? launch_grad<T, 4, 1, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 3, 1, 4>(ctx, a, n_groups, sum_only);
-    return h > 64 ? launch_grad<T, 2, 1, 4>(ctx, a, n_groups, sum_only) : launch_grad<T, 1, 1, 4>(ctx, a, n_groups, sum_only);
+    if (h > 128) return h > 192 ? use(GradShape<T, 4, 1, 4>()) : use(GradShape<T, 3, 1, 4>());
+    return h > 64 ? use(GradShape<T, 2, 1, 4>()) : use(GradShape<T, 1, 1, 4>());
+}
+// kFewGradRows rows and less take tiles of 128 x 128 and, in one list, one run, so that more CUs have something to write and no pieces
+// need adding (100 rows of 768 with 1024 gradients in bf16 10 us, 21 with large tiles and two launches; 1000 rows 32 and 25).
+// The runs are those of the ordinary tiles: a tile's size does not change the order in which an element's rows are added.
+template <class T>
+static int grad_of(spp_ctx* ctx, GradArgs& a, int n_groups, int64_t most) {
+    const bool sum_only = most == 0;
+    a.most = grad_shape<T>(a, [&](auto shape) {
+        typedef decltype(shape) S;
+        // as many workgroups as run at once
+        const int fit = 163840 / S::lds, wish = 8 / (S::wh * S::wd);
+        const int64_t at_once = (int64_t)ctx->num_cu * (fit < 1 || wish < 1 ? 1 : fit < wish ? fit : wish), runs = at_once / grad_tiles<S>(a);
+        return (int)(runs < 1 ? 1 : runs);
+    });
+    auto launch = [&](auto shape) { return launch_grad<T, decltype(shape)>(ctx, a, n_groups, sum_only); };
+    const int tiles = (a.H + 255) / 256, h = (a.H + tiles - 1) / tiles;
+    return most <= kFewGradRows && a.D > 64 && h > 64 ? launch(GradShape<T, 2, 2, 4>()) : grad_shape<T>(a, launch);
 }
 
 }  // namespace spp
