@@ -407,15 +407,17 @@ int  spp_mx4_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int32_t n_list
 /* (7) One AdamW step over any number of tensors (contiguous, n elements each), moments in 32 or 8 bits:
  *       m' = b1 m + (1-b1) g      v' = b2 v + (1-b2) g^2
  *       p' = (1 - lr wd) p - lr/(1-b1^t) * m' / (sqrt(v') / sqrt(1-b2^t) + eps)          t = 1 at the first step
- *     computed in fp32.  An element whose v' would not be finite (its gradient is not, or its square is not) keeps p, m and v;
- *     such elements are counted (spp_ctx_totals, out[9]).  p: SPP_F32 or SPP_BF16 (rounded to nearest, ties to even); g any type.
+ *     computed in fp32.  An element whose v' would not be finite (its gradient is not, or its square is not) keeps p, m and v (in 8
+ *     bits its moments are held again under the run's new scale); such elements are counted (spp_ctx_totals, out[9]).  p: SPP_F32 or SPP_BF16 (rounded to nearest, ties to even); g any type.
  *     A step is not recorded into a HIP graph, whose replays would repeat the one t: SPP_E_ARG while the stream records.
  *     state_bits 32: d_m and d_v are fp32[n], zero before the first step.
  *     state_bits 8:  d_m and d_v are uint8[n], d_scale fp32[2 * ceil(n / SPP_ADAMW_BLOCK)], all zero before the first step.
  *       Each run of SPP_ADAMW_BLOCK elements has two scales, for m and for sqrt(v), such that the largest of the run is the
  *       largest code; a code c of sqrt(v) stands for scale * 2^(c/16 - 15) * (1 + (c mod 16)/16), 0 for 0; of m likewise with
- *       (c & 127), 8 in the place of 16, and the sign in bit 7.  Rounded to the nearest code, ties to even; a v above zero keeps at
- *       least code 1.  The step itself uses the moments before this rounding.
+ *       (c & 127), 8 in the place of 16, and the sign in bit 7.  Rounded to the nearest code, ties to even, code 0 taken as
+ *       scale * 2^-15 for that: |m| up to scale * 2^-15 * 1.0625, half way from there to code 1, is held as 0.  A v above zero
+ *       keeps at least code 1.  Runs whose largest |m| is below 2^-100 hold zeros for m.  The step itself uses the moments before
+ *       this rounding.
  *     spp_adamw_load sets the 8-bit moments from fp32 arrays (host arrays of device pointers; what is not finite, or a negative v,
  *     counts as 0); spp_adamw_values gives the values that they stand for.  Both ignore d_p, d_g and their types. */
 typedef struct {

@@ -125,6 +125,8 @@ __device__ __forceinline__ Moment moment_scale(float largest, float most) {
     // below this 1 / scale would not be finite: the block counts as zeros
     return largest >= kLeastScale ? Moment{most / largest, largest * (1.0f / most)} : Moment{0.0f, 0.0f};
 }
+// The nearest code, ties to the even one: the float's bits without the last DROP, whose first code, 0, would be 2^-15.  Rounding goes by
+// that value also where the code then reads as 0.
 template <int DROP, int BASE, int TOP>
 __device__ __forceinline__ uint32_t small_float(float q) {
     const uint32_t u = __float_as_uint(q);
