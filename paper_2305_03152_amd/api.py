@@ -947,26 +947,38 @@ class AdamW:
                 a = self._arr[j]
                 a.d_p, a.n, a.p_type = p.data_ptr(), n, _TYPES[p.dtype]
                 a.d_m, a.d_v, a.d_scale = s[0].data_ptr(), s[1].data_ptr(), s[2].data_ptr() if blocks else None
-                self._items.append((a, p, n))
+                # and the type of its last gradient; what step() asks of it every time, looked up once
+                self._items.append([a, p, n, p.dtype, p.data_ptr(), None, p.data_ptr, p.numel, p.is_contiguous])
+        self._hyper = _AdamwHyper()
+        self._args = C.cast(self._arr, C.POINTER(_AdamwTensor)), C.pointer(self._hyper)
         self._views = tuple([s[k].view(p.shape) for s, p in zip(self._state, self.params)] for k in (0, 1)) if state_bits == 32 else None
 
     @staticmethod
-    def _same(a, p, n):
+    def _same(p, n, dtype):
         """A parameter may have been given other memory (.data, set_, resize_): of its size and type, or the state does not fit."""
-        if p.numel() != n or not p.is_contiguous() or _TYPES.get(p.dtype) != a.p_type or not p.is_cuda:
+        if p.numel() != n or not p.is_contiguous() or p.dtype is not dtype or not p.is_cuda:
             raise SppError("a parameter is no longer a contiguous tensor of the size and type that it had")
 
     def step(self, grads: Sequence[torch.Tensor], lr: Optional[float] = None, sync: bool = True):
         """One step with a gradient (any of the three types) for every parameter; not while the stream records a graph."""
         if len(grads) != len(self.params):
             raise SppError("one gradient per parameter is needed")
-        for (a, p, n), g in zip(self._items, grads):
-            if not (g.is_cuda and g.is_contiguous() and g.numel() == n and g.dtype in _TYPES):
+        # a small model's step is bound by this loop: what seldom changes is written to the call's arguments when it does
+        for item, g in zip(self._items, grads):
+            a, p, n, dtype, ptr, gtype, address, numel, contiguous = item
+            given = g.dtype
+            if g.numel() != n or not (g.is_cuda and g.is_contiguous()) or given is not gtype and given not in _TYPES:
                 raise SppError("a gradient must be a contiguous float32, float16 or bfloat16 tensor on the GPU of its parameter's size")
-            self._same(a, p, n)
-            a.d_p, a.d_g, a.g_type = p.data_ptr(), g.data_ptr(), _TYPES[g.dtype]
-        h = _AdamwHyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.weight_decay)
-        _check(load_library().spp_adamw_step(self.ctx._h, self._arr, len(self.params), self.state_bits, C.byref(h), self.t + 1,
+            if address() != ptr or numel() != n or p.dtype is not dtype or not contiguous():
+                self._same(p, n, dtype)
+                item[4] = a.d_p = address()
+            if given is not gtype:
+                item[5], a.g_type = given, _TYPES[given]
+            a.d_g = g.data_ptr()
+        h = self._hyper
+        h.lr, h.eps, h.weight_decay = self.lr if lr is None else lr, self.eps, self.weight_decay
+        h.beta1, h.beta2 = self.betas
+        _check(load_library().spp_adamw_step(self.ctx._h, self._args[0], len(self._items), self.state_bits, self._args[1], self.t + 1,
                                              SPP_SYNC if sync else 0))
         self.t += 1
 
@@ -980,8 +992,8 @@ class AdamW:
             if sync:
                 self.ctx.sync()
             return list(self._views[0]), list(self._views[1])
-        for item in self._items:
-            self._same(*item)
+        for _, p, n, dtype, *_ in self._items:
+            self._same(p, n, dtype)
         m = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
         v = [_new(self.ctx, p.shape, torch.float32) for p in self.params]
         pm, pv = self._moments(m, v)
@@ -995,8 +1007,8 @@ class AdamW:
         for j, (p, a, b) in enumerate(zip(self.params, m, v)):
             if _dev(a, torch.float32, f"m {j}").numel() != p.numel() or _dev(b, torch.float32, f"v {j}").numel() != p.numel():
                 raise SppError(f"moments {j} must be of their parameter's size")
-        for item in self._items:
-            self._same(*item)
+        for _, p, n, dtype, *_ in self._items:
+            self._same(p, n, dtype)
         if self.state_bits == 32:
             with torch.cuda.stream(self.ctx.stream):
                 for s, a, b in zip(self._state, m, v):
