@@ -90,27 +90,13 @@ __device__ __forceinline__ void store_codes(void* base, int64_t i, int have, boo
             if (k < have) p[k] = (uint8_t)c[k];
 }
 
-// The root of v, rounded correctly: of the instruction's result r, off by less than a step, and its neighbours the one with
-// (r - step) r < v <= (r + step) r.  Below 2^-96 the products would leave the normal range: scaled by 2^32 there.
-__device__ __forceinline__ float root_of(float v) {
-    const bool tiny = v < 0x1p-96f;
-    const float x = tiny ? v * 0x1p32f : v;
-    float r = __builtin_amdgcn_sqrtf(x);
-    const float below = __uint_as_float(__float_as_uint(r) - 1), above = __uint_as_float(__float_as_uint(r) + 1);
-    const float down = __builtin_fmaf(-below, r, x), up = __builtin_fmaf(-above, r, x);
-    r = down <= 0.0f ? below : r;
-    r = up > 0.0f ? above : r;
-    r = tiny ? r * 0x1p-16f : r;
-    return v == 0.0f ? 0.0f : r;
-}
-
 // False: the element stays as it was.  root: of the v that it then has.
 __device__ __forceinline__ bool adam_element(const AdamHyper& h, float g, float& p, float& m, float& v, float& root) {
     const float m1 = m * h.b1 + g * h.c1;
     const float v1 = v * h.b2 + (g * g) * h.c2;
     const bool finite = (__float_as_uint(v1) & 0x7F800000u) != 0x7F800000u;
     v = finite ? v1 : v;
-    root = root_of(v);
+    root = sqrtf(v);
     const float den = root * h.rs + h.eps;
     const float p1 = p * h.decay - (m1 / den) * h.step;
     p = finite ? p1 : p;
@@ -251,7 +237,7 @@ __global__ void __launch_bounds__(kAdamBlock) adamw_load_kernel(AdamTable t) {
         for (int k = 0; k < 4; ++k) {                       // what no step can have left there counts as zero
             if ((__float_as_uint(m[k]) & 0x7F800000u) == 0x7F800000u) m[k] = 0.0f;
             if (!(v[k] >= 0.0f) || (__float_as_uint(v[k]) & 0x7F800000u) == 0x7F800000u) v[k] = 0.0f;
-            v[k] = root_of(v[k]);
+            v[k] = sqrtf(v[k]);
         }
         put_moments(t, j, i, have, wide, m, v);
     }
