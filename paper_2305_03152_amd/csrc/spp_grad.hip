@@ -2,8 +2,9 @@
 //
 //   dW[g] = sum over the lists j of group g of dY_j^T X_j        dY_j [n_j, H] fp32, fp16 or bf16, X_j [n_j, D] in MXFP4, dW fp32
 //
-// What a code and a scale stand for is exact in bf16, as is an fp32 as the sum of three bf16 and an fp16 of two: the products of the
-// matrix instruction are exact and are added in fp32, the sums of the runs in 64 bits.
+// What a code and a scale stand for is exact in bf16, as is an fp16 as the sum of two bf16 and an fp32 of at least 2^-110 as that of three:
+// the products of the matrix instruction are exact and are added in fp32, the sums of the runs in 64 bits.  Of a smaller fp32 the bits
+// below 2^-133, the smallest bf16, are lost: off by less than 2^-133 each, whatever X.
 #include "spp_mx4.h"
 
 namespace spp {
@@ -43,7 +44,7 @@ __host__ __device__ __forceinline__ int grad_runs(int64_t chunks, int rows, int 
     return half < most ? (int)half : most;
 }
 
-// dY as bf16 numbers that add up to it exactly: one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
+// dY as bf16 numbers that add up to it exactly (above): one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
 // finite value becomes infinite; what is not finite is its first piece alone.
 template <class T> struct Pieces { static constexpr int n = 1; };
 template <> struct Pieces<_Float16> { static constexpr int n = 2; };
