@@ -41,3 +41,35 @@ def test_an_x_beyond_fp32_is_infinite(ctx):
     y = torch.tensor([[1e-10], [1.0]], device=DEV)
     g = spp.mx4_weight_grad(ctx, [(torch.from_numpy(rows).to(DEV), 2, None, y)], 1, 32)[0, 0].cpu()
     assert torch.isinf(g[1::2]).all() and torch.isfinite(g[0::2]).all()
+
+
+# every shape of tile: D up to 64, 128 and more, H up to 64, 128, 192 and 256 of a tile; few rows and many; lists over several groups
+SHAPES = [(D, H) for D in (33, 64, 65, 128, 160, 700) for H in (7, 64, 65, 128, 129, 192, 193, 256, 300)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D,H", SHAPES)
+def test_whole_numbers_are_added_exactly(ctx, dtype, D, H):
+    """X of whole numbers up to 12, dY up to 4: sums below 2^24 are exact in any order, so that a chunk or a run lost, doubled or
+    counted to another group shows.  Many rows in lists of uneven lengths, some counted on the device, behind them NaN."""
+    rng = np.random.default_rng(D * 1000 + H)
+    groups, nb = 3, -(-D // 32)
+    want = torch.zeros(groups, H, D, dtype=torch.float64)
+    items = []
+    for j, n in enumerate([0, 1, 63, 64, 65, 7001, 2, 9000, 129, 0, 8191, 1000]):
+        rows = np.zeros((n + 40, R.row_bytes(D)), np.uint8)
+        rows[:, :16 * nb] = rng.integers(0, 256, (n + 40, 16 * nb))
+        rows[:, 16 * nb:17 * nb] = 128
+        rows[n:, 16 * nb:17 * nb] = 255
+        y = torch.full((n + 40, H), float("nan"), dtype=dtype, device=DEV)
+        y[:n] = torch.from_numpy(rng.integers(-4, 5, (n, H))).to(DEV, dtype)
+        g = (5 * j) % groups if j != 6 else 2
+        want[g] += y[:n].double().cpu().T @ torch.from_numpy(R.values(rows[:n], D))
+        on_device = j % 2 == 0
+        items.append((torch.from_numpy(rows).to(DEV), n + 40 if on_device else n, torch.tensor([n], device=DEV) if on_device else None, y, g))
+    assert float(want.abs().max()) < 2 ** 24
+    assert torch.equal(spp.mx4_weight_grad(ctx, items, H, D, groups=groups).double().cpu(), want)
+    for n in (1, 63, 128, 129, 5000):                            # one list: straight into dW, or in runs
+        x, y = items[5][0][:n], items[5][3][:n]
+        one = y.double().cpu().T @ torch.from_numpy(R.values(x.cpu().numpy(), D))
+        assert torch.equal(spp.mx4_weight_grad(ctx, [(x, n, None, y)], H, D)[0].double().cpu(), one), n
