@@ -17,10 +17,12 @@ namespace spp {
 
 void set_error(const char* fmt, ...);
 
+// A failure is reported once: the runtime forgets it, or the check behind the next launch would find it again.
 #define SPP_HIP(call)                                                                       \
     do {                                                                                    \
         hipError_t e__ = (call);                                                            \
         if (e__ != hipSuccess) {                                                            \
+            (void)hipGetLastError();                                                        \
             spp::set_error("%s failed: %s (%s:%d)", #call, hipGetErrorString(e__), __FILE__, \
                            __LINE__);                                                       \
             return (e__ == hipErrorOutOfMemory) ? SPP_E_OOM : SPP_E_HIP;                    \

@@ -29,10 +29,12 @@ static MemoryPool* pool_of(int device) {         // never destroyed: handles may
 hipError_t device_malloc(void** out, size_t bytes) {
     hipError_t e = hipMalloc(out, bytes);
     int device = 0;
-    if (e != hipErrorOutOfMemory || hipGetDevice(&device) != hipSuccess) return e;
-    pool_trim(device);
-    (void)hipGetLastError();
-    return hipMalloc(out, bytes);        // also where there was nothing to give: another thread may just have emptied the pool
+    if (e == hipErrorOutOfMemory && hipGetDevice(&device) == hipSuccess) {
+        pool_trim(device);
+        e = hipMalloc(out, bytes);       // also where there was nothing to give: another thread may just have emptied the pool
+    }
+    if (e != hipSuccess) (void)hipGetLastError();            // told by what is returned, not to the next launch's check as well
+    return e;
 }
 
 hipError_t pool_take(int device, void** out, size_t bytes) {
