@@ -19,9 +19,10 @@ namespace spp {
 // transposed (ds_read_b64_tr_b16).  A chunk's operands are asked for two chunks ahead, into registers; X is unpacked to bf16 on
 // its way to LDS, dY cut into its pieces.
 //
-// Bound by HBM where dW is one tile: 2.56M rows of 128 with 256 gradients in bf16 270 us, 5.5 TB/s; fp16 433, fp32 (half the rows) 331, by
-// the cutting and its two and three products.  For larger dW by the turns that writing a chunk to LDS and multiplying it take:
-// 390k rows of 768 with 1024 in bf16 587 us, 1020 TFLOP/s.
+// Bound by HBM where dW is one tile: 2.56M rows of 128 with 256 gradients in bf16 270 us, 5.5 TB/s; fp16 430 to 445, fp32 (half the rows) 330
+// to 345, by the cutting and its two and three products.  For larger dW by the turns that writing a chunk to LDS and multiplying it take:
+// 390k rows of 768 with 1024 in bf16 580 to 610 us, 980 to 1030 TFLOP/s.  Few chunks a run leave little to overlap: 45k rows of 128 with
+// 256 in bf16 27 us, 60k of 100 with 172 in eight groups in fp32 39 (their pieces, written and read again: 18 MB beside 72 of operands).
 constexpr int kGradPad = 16;         // elements behind an LDS row: the four rows that 16 lanes read at once are then 4 x 32 bytes of other banks
 
 struct GradArgs {
@@ -423,7 +424,10 @@ static int grad_shape(const GradArgs& a, Use use) {
     return h > 64 ? use(GradShape<T, 2, 1, 4>()) : use(GradShape<T, 1, 1, 4>());
 }
 // kFewGradRows rows and less take tiles of 128 x 128 and, in one list, one run, so that more CUs have something to write and no pieces
-// need adding (100 rows of 768 with 1024 gradients in bf16 10 us, 21 with large tiles and two launches; 1000 rows 32 and 25).
+// need adding.  Large tiles and two launches against this, us: 128 x 256 in bf16 100 rows 15 and 10.5, 256 15 and 12, 512 15 and
+// 16; in fp32 100 rows 16 and 13.5, 160 15 both, 256 15.5 and 20; 768 x 1024 in bf16 128 rows 15 and 10, 512 27 and 17, 1000 30 and 26; in
+// fp32 128 rows 28 and 14, 384 30 and 27, 512 31 and 33.  (So large matrices and 16 bits would gain up to 384 rows and more; the limit
+// is where no shape or type loses.)
 // The runs are those of the ordinary tiles: a tile's size does not change the order in which an element's rows are added.
 template <class T>
 static int grad_of(spp_ctx* ctx, GradArgs& a, int n_groups, int64_t most) {

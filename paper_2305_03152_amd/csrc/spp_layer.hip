@@ -60,7 +60,8 @@ __device__ __forceinline__ void put_whole(T* y, int64_t ld, const f32x4 (&acc)[4
 
 // A wavefront's 16 RN rows of Y on their way to memory where they do not begin with a line each.  They are put together in LDS and
 // written by whole 16-byte pieces, side by side; the ends of a row or a run, less than a piece, by element.  Stored as they come, 2.56M
-// rows 100 -> 172 in bf16 took 432 us, so 237 (4.5 TB/s).
+// rows 100 -> 172 in bf16 took 432 us, so 230 to 237 (4.5 TB/s).  Where W is a stream rows go out by lines, and the narrower their LDS writes
+// have to be the longer it takes: 400k rows 256 -> 1001 313 us, -> 1002 263, -> 1004 242, -> 1008 225, -> 1024, stored as they come, 154.
 //   run    the rows follow each other without a gap and fit: all of them are put together as one run of bytes
 //   lines  64 columns of every row at a time, each byte where it lies in its 128-byte line: what they fill of lines goes out, the
 //          begun line stays for the next 64
@@ -360,8 +361,9 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
 }
 
 // The form for wider rows, of which a wavefront's registers would not hold enough: a workgroup takes a tile of TR rows into LDS and its
-// wavefronts take 16 RN of them by 64 columns of Y at a time, W straight from memory.  300k rows 800 -> 256 in bf16: 158 us, 1.7 TB/s;
-// bound by the way of W's blocks from the L2, a step of 128 columns at a time.
+// wavefronts take 16 RN of them by 64 columns of Y at a time, W straight from memory.  300k rows 800 -> 256 in bf16: 158 us, 1.7 TB/s,
+// 1024 -> 256 205, 800 -> 1024 463; 50k rows 4096 -> 256 188.  Bound by the way of W's blocks from the L2, a step of 128 columns at a
+// time: every wavefront fetches them itself, and nothing is asked for ahead.
 template <class T, int TR, int RN>
 __global__ void __launch_bounds__(kProdBlock) mx4_product_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t xs[];
@@ -499,8 +501,12 @@ static int launch_rows_as(spp_ctx* ctx, ProductArgs& a) {
     int64_t tiles = 0;
     for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)(WAVES * 16 * RN) - 1) / (WAVES * 16 * RN);
     // Workgroups per CU.  Many tiles are fastest with a workgroup each (2.56M rows 128 -> 256: 264 us, 285 with one workgroup per CU
-    // that goes over its tiles, 298 to 302 with two to sixteen; 800k rows 256 -> 256: 110 and 117); some with one per CU (300k
-    // rows 32.3 us, 34 to 35 with more); few with what runs at once (100k rows 13.9 us, 15.1 with one, 16 with four).
+    // that goes over its tiles, 298 to 302 with two to sixteen); some with one per CU; few with what runs at once.  With 1, 2, 3, 8 and 128
+    // per CU, 128 -> 256: 200k rows 23.4, 22.5, 24.1, 26.1, 26.2 us; 270k 30.3, 31.4, 33.6, 31.6, 32.6; 500k 47.9, 47.4, 47.7, 48.3, 48.7;
+    // 540k 53.3, 55.2, 57.3, 55.6, 53.7; 800k 73.7, 74.5, 76.0, 77.3, 74.1.  Of other shapes: 256 -> 256 200k 29.4, 26.2, 27.5, 30.6, 30.5;
+    // 400k 49.6, 44.1, 47.8, 47.1, 49.7; 800k 110, 108, 111, 104, 104; 32 -> 64 200k 12.3, 8.7, 8.3, 10.8, 10.7; 400k 19.6, 14.1, 12.6, 15.3,
+    // 17.2; 800k 33.4, 23.2, 21.8, 24.3, 30.3.  (The limits, 262k and 524k rows, are those of 128 -> 256, and within a few per cent there;
+    // narrow rows would be up to a third faster with three throughout.)
     // Rows of other lengths take unequal times: many workgroups even them out where there are many more tiles (2.56M rows
     // 100 -> 172: 289 us with four per CU, 238 with 32; 300k rows in fp32 42 and 49).
     a.fill = 2 * ctx->num_cu;
