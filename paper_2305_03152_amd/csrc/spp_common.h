@@ -184,10 +184,10 @@ struct spp_ctx {
                                         // what a vip propagation adds up over its launches with and a flag, all zero between calls
     int         vip_state_clean = 1;    // they are
     // vip workspaces
-    spp::DevBuf y0, y1, tot, acc, frontier;
+    spp::RecordedBuf y0, y1, tot, acc, frontier;
     spp::DevBuf sortws, rankws;         // set-up: counts of a radix sort, keys and histograms of a ranking (bounded, see kKeptSortBytes)
-    spp::DevBuf xvals;                  // dense hops over the chunked layout: y[source] of every entry
-    spp::DevBuf bins;                   // general propagation: per row block the (row, weight) entries of a hop, and the fill counts
+    spp::RecordedBuf xvals;             // dense hops over the chunked layout: y[source] of every entry
+    spp::RecordedBuf bins;              // general propagation: per row block the (row, weight) entries of a hop, and the fill counts
     int         bin_lds_set = 0, sum_lds_set = 0, prepare_lds_set = 0;   // dynamic LDS its kernels have been allowed
     int         tile_lds_set = 0;       // dynamic LDS bytes the dense-hop kernel has been allowed on this device
     int         dedup_lds_set = 0;      // the LDS dedup kernel of the sampler has been allowed its 76 KB

@@ -1846,12 +1846,12 @@ extern "C" int spp_vip_propagate_general(spp_ctx* ctx, const spp_graph* g, const
     SPP_HIP(hipSetDevice(ctx->device));
     hipStream_t st = ctx->stream;
     const int64_t N = g->N;
-    SPP_TRY(ctx->y0.reserve((size_t)N * sizeof(float)));
-    SPP_TRY(ctx->y1.reserve((size_t)N * sizeof(float)));
-    SPP_TRY(ctx->tot.reserve((size_t)N * sizeof(double)));
-    SPP_TRY(ctx->acc.reserve((size_t)N * sizeof(double)));
+    SPP_TRY(ctx->y0.reserve((size_t)N * sizeof(float), ctx->stream));
+    SPP_TRY(ctx->y1.reserve((size_t)N * sizeof(float), ctx->stream));
+    SPP_TRY(ctx->tot.reserve((size_t)N * sizeof(double), ctx->stream));
+    SPP_TRY(ctx->acc.reserve((size_t)N * sizeof(double), ctx->stream));
     const int64_t lcap = frontier_list_capacity(N, g->M);
-    SPP_TRY(ctx->frontier.reserve((size_t)(lcap + 2) * sizeof(int32_t) + (4 + SPP_MAX_L + 2) * sizeof(unsigned long long)));
+    SPP_TRY(ctx->frontier.reserve((size_t)(lcap + 2) * sizeof(int32_t) + (4 + SPP_MAX_L + 2) * sizeof(unsigned long long), ctx->stream));
     unsigned long long* slots;
     int *d_bad, left_clean;
     SPP_TRY(vip_state(ctx, &slots, &d_bad, &left_clean));
@@ -1885,10 +1885,10 @@ extern "C" int spp_vip_propagate_general(spp_ctx* ctx, const spp_graph* g, const
     const size_t sum_lds = binned ? sizeof(double) << g->tile_rbits : 0;
     if (binned) {
         parts = tile_parts(ctx->num_cu, g->nrb, g->M);
-        SPP_TRY(ctx->acc.reserve((size_t)parts * (size_t)part_stride * sizeof(double)));
+        SPP_TRY(ctx->acc.reserve((size_t)parts * (size_t)part_stride * sizeof(double), ctx->stream));
         acc = ctx->acc.as<double>();
         const int64_t room = g->M > 8 ? g->M : 8;        // entries, or as many weights, rounded up, and rows
-        SPP_TRY(ctx->bins.reserve(((size_t)room + (size_t)g->nrb + 1) * sizeof(uint2)));
+        SPP_TRY(ctx->bins.reserve(((size_t)room + (size_t)g->nrb + 1) * sizeof(uint2), ctx->stream));
         bins = ctx->bins.as<uint2>();
         cursor = reinterpret_cast<uint32_t*>(bins + room);
         if (ctx->bin_lds_set < (int)fill_lds) {
@@ -1965,10 +1965,10 @@ extern "C" int spp_vip_propagate(spp_ctx* ctx, const spp_graph* g, const int32_t
     SPP_HIP(hipSetDevice(ctx->device));
     hipStream_t st = ctx->stream;
     const int64_t N = g->N;
-    SPP_TRY(ctx->y0.reserve((size_t)(N + 4) * sizeof(float)));       // dense hops read y as whole vectors of four
-    SPP_TRY(ctx->y1.reserve((size_t)(N + 4) * sizeof(float)));
+    SPP_TRY(ctx->y0.reserve((size_t)(N + 4) * sizeof(float), ctx->stream));       // dense hops read y as whole vectors of four
+    SPP_TRY(ctx->y1.reserve((size_t)(N + 4) * sizeof(float), ctx->stream));
     static_assert(2 * SPP_MAX_L + 1 <= 64, "fits the mirror");
-    SPP_TRY(ctx->tot.reserve((size_t)N * sizeof(double)));
+    SPP_TRY(ctx->tot.reserve((size_t)N * sizeof(double), ctx->stream));
     int parts = tile_parts(ctx->num_cu, g->nrb, g->M);
     // the chunked layout: with a row block per CU or more, one workgroup takes a whole block and
     // finishes its vertices itself (no partial sums leave the chip)
@@ -1977,7 +1977,7 @@ extern "C" int spp_vip_propagate(spp_ctx* ctx, const spp_graph* g, const int32_t
     {
         const size_t tile_bytes = (size_t)parts * (size_t)part_stride * sizeof(double);
         const size_t push_bytes = (size_t)(N + 1) * sizeof(double);
-        SPP_TRY(ctx->acc.reserve(tile_bytes > push_bytes ? tile_bytes : push_bytes));
+        SPP_TRY(ctx->acc.reserve(tile_bytes > push_bytes ? tile_bytes : push_bytes, ctx->stream));
     }
     // The push goes through bins where the chunked layout's value memory holds the entries (8 bytes for at most
     // M / kPushShare edges), the counts and the offsets, and a workgroup per row block fills the chip: graphs of
@@ -2014,7 +2014,7 @@ extern "C" int spp_vip_propagate(spp_ctx* ctx, const spp_graph* g, const int32_t
                                         hipFuncAttributeMaxDynamicSharedMemorySize, (int)bin_finish_lds));
             ctx->push_lds_set = (int)bin_lds;
         }
-        SPP_TRY(ctx->xvals.reserve((size_t)(g->x_entries > 0 ? g->x_entries : 4) * sizeof(float)));
+        SPP_TRY(ctx->xvals.reserve((size_t)(g->x_entries > 0 ? g->x_entries : 4) * sizeof(float), ctx->stream));
     }
     // A workgroup per 256 vertices, up to eight per CU (the finishing pass takes four vertices per thread and round: its
     // workgroups see no more than a round's vertices in kSegments segments, or ceil of their share).
@@ -2026,7 +2026,7 @@ extern "C" int spp_vip_propagate(spp_ctx* ctx, const spp_graph* g, const int32_t
     const int64_t seg_all = vgrid * per_group(N) > tgrid * per_group(nT) ? vgrid * per_group(N) : tgrid * per_group(nT);
     int64_t lcap = binned ? frontier_list_capacity(N, g->M) : seg_all + 2 * kSegments;
     lcap += lcap & 1;
-    SPP_TRY(ctx->frontier.reserve((size_t)lcap * sizeof(int32_t) + (1 + SPP_MAX_L + 2) * sizeof(unsigned long long)));
+    SPP_TRY(ctx->frontier.reserve((size_t)lcap * sizeof(int32_t) + (1 + SPP_MAX_L + 2) * sizeof(unsigned long long), ctx->stream));
     unsigned long long* slots;
     int *d_bad, left_clean;
     SPP_TRY(vip_state(ctx, &slots, &d_bad, &left_clean));

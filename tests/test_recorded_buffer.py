@@ -98,3 +98,15 @@ def program(tmp_path_factory):
 def test_blocks_that_a_recording_may_hold(program, case):
     r = subprocess.run([program, case], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+def test_what_recorded_calls_write_to_is_such_a_buffer(tmp_path):
+    """The workspaces of the calls that may be recorded: propagations and the weight gradient."""
+    src = tmp_path / "members.cpp"
+    src.write_text('#include "spp_common.h"\n#include <type_traits>\n' + "".join(
+        "static_assert(std::is_same<decltype(spp_ctx::%s), spp::RecordedBuf>::value, \"%s\");\n" % (m, m)
+        for m in ("y0", "y1", "tot", "acc", "frontier", "xvals", "bins", "gradws")))
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    r = subprocess.run(["g++", "-std=c++17", "-fsyntax-only", "-D__HIP_PLATFORM_AMD__=1", "-I", os.path.join(rocm, "include"), "-I", CSRC, str(src)],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
