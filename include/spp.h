@@ -8,8 +8,9 @@
  *                         (Sec. 2.3; steps (i)-(iii) of the random process of Sec. 3.1)
  *   spp_gather_features   cache-aware feature gather: local shard / replica cache / remote
  *                         rows on a miss (Secs. 4.1-4.3; stages 5-10 of Appendix D)
- *   spp_mx4_*, spp_adamw_*  feature rows in 4 bits, the layer that reads them, its weight gradient and the
- *                         optimiser's step: what a training loop does next with the gathered rows
+ *   spp_mx4_*, spp_fp8_*, spp_adamw_*  feature rows in 4 bits, the layer that reads them, its weight gradient; hidden
+ *                         rows in 8 bits, the layers that read them, gated or not, their gradients; the optimiser's
+ *                         step: what a training loop does next with the gathered rows
  *
  * Conventions
  *   G        directed graph in CSR on the device: rowptr int64[N+1], col int32[M].  Row v,
@@ -46,8 +47,8 @@ extern "C" {
 #define SPP_MAX_GATHER_LISTS 64 /* most id lists in one spp_gather_features_multi call */
 #define SPP_MAX_SAMPLE_BATCHES 64 /* most minibatches in one spp_sample_mfg_multi call */
 #define SPP_STATIC_GATHER_MAX_ROWS 131072 /* most ids in one spp_gather_features_static call */
-#define SPP_MAX_ROW_LISTS 64   /* most lists, and most weight matrices, in one spp_mx4_product or spp_mx4_weight_grad call */
-#define SPP_MX4_MAX_COLS 4096  /* most columns of a row in MXFP4 */
+#define SPP_MAX_ROW_LISTS 64   /* most lists, and most weight matrices, in one call of the operators on rows */
+#define SPP_MX4_MAX_COLS 4096  /* most columns of a row in 4 or 8 bits */
 #define SPP_MAX_HIDDEN 65536   /* most columns of a product */
 #define SPP_ADAMW_BLOCK 256    /* elements whose 8-bit moments share a scale */
 #define SPP_ADAMW_MAX_ELEMENTS 17179869184 /* most elements of one tensor of spp_adamw_step: 2^34 */
@@ -355,10 +356,13 @@ typedef struct {
 int  spp_access_count(spp_ctx* ctx, const spp_id_list* lists, int32_t n_lists, int64_t N, float* d_count,
                       uint32_t flags);
 
-/* Operators on gathered rows: feature rows in 4 bits, the layer that reads them, its gradient and the optimiser's step.
+/* Operators on gathered and hidden rows: feature rows in 4 bits, hidden rows in 8, the layers that read them, their gradients and
+ * the optimiser's step.
  *
  * Element types of the arrays below. */
 enum { SPP_F32 = 0, SPP_F16 = 1, SPP_BF16 = 2 };
+/* Activations of the gated layer: g / (1 + exp(-g)); g times the normal distribution function of g; 1 / (1 + exp(-g)). */
+enum { SPP_SILU = 0, SPP_GELU = 1, SPP_SIGMOID = 2 };
 
 /* (5) Rows in MXFP4.  A row of D columns (1 .. SPP_MX4_MAX_COLS) is nb = ceil(D/32) blocks of 32 columns, the last one filled up
  *     with zeros.  With a = max |x| of a block and e = max(floor(log2 a) - 2, -127) its columns are held as the nearest of
@@ -439,6 +443,41 @@ int  spp_adamw_load(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_ten
 int  spp_adamw_values(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_tensors, float* const* d_m, float* const* d_v,
                       uint32_t flags);
 
+/* (8) Hidden rows in 8 bits: what a layer's backward pass needs of its input, kept from the forward pass, and what the layers of (9)
+ *     read.  A row of D columns (1 .. SPP_MX4_MAX_COLS) is nb = ceil(D/128) blocks of 128 columns.  With a = the largest finite |x| of
+ *     a block, e = the smallest integer with a <= 448 * 2^e, at least -117 and at most 119: its columns are held as the nearest E4M3
+ *     (sign, 4, 3; the largest is 448) to x / 2^e, ties to even, NaN and infinities as NaN; its scale is the byte e + 127 (E8M0).  (Only
+ *     a column above 448 * 2^119 does not fit: it is held as that.)  Every value of a row is 0 or a normal fp32 and bf16.
+ *     Bytes of a row: ceil(D/16)*16 codes, those behind column D zeros, then nb scale bytes, then zeros up to spp_fp8_row_bytes(D),
+ *     a multiple of 16 (272 for 256 columns).  A row is one piece of bytes, for the gather, the cache and the local store too.
+ *     Arguments as of spp_mx4_quantize and spp_mx4_dequantize; rows of other origin may have any scale byte, 255 is NaN. */
+int64_t spp_fp8_row_bytes(int32_t D);
+int  spp_fp8_quantize(spp_ctx* ctx, const void* d_x, int32_t type, int64_t n, const int64_t* d_n, int32_t D, int64_t ld,
+                      void* d_rows, uint32_t flags);
+int  spp_fp8_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64_t* d_n, int32_t D, void* d_x, int32_t type,
+                        int64_t ld, uint32_t flags);
+
+/* (9) The layers that read such rows, over lists as in (6) (d_rows: rows in 8 bits, [n, spp_fp8_row_bytes(D)]):
+ *       product      Y_j[i,:] = sum_d X_j[i,d] W[g_j][:,d]           d_weights: n_groups matrices of H rows in 8 bits
+ *       gated        Y_j = act(G_j) * U_j                            d_weights: n_groups times H rows Wg, then H rows Wu;
+ *                    G_j = X_j Wg[g_j]^T, U_j = X_j Wu[g_j]^T        H at most SPP_MAX_HIDDEN / 2
+ *       gated grad   dP_j = [dY_j * U_j * act'(G_j) | dY_j * act(G_j)]
+ *                    lists: d_y is dY_j, read; grads: the same rows, n, d_n and groups, d_y is dP_j [n, 2H], written, ld >= 2H.  G and U
+ *                    are formed again from the rows, as in the forward pass.  dP must not overlap dY.
+ *       weight grad  dW[g] = sum over the lists j of group g of dY_j^T X_j, as spp_mx4_weight_grad in everything else.  With grads and
+ *                    2H for H it gives the gradients of Wg and Wu, one behind the other.
+ *     X and W are the values that the rows stand for; sums and activations are formed in fp32 and rounded once to Y's type.  The gradient
+ *     of the rows of a layer is the product of dY (dP) in 8 bits by the transposed weights (of Wg and Wu, one behind the other).
+ *     Rows from *d_n on are neither read nor written, nor what lies between rows of Y; recording as in (6). */
+int  spp_fp8_product(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
+                     int32_t D, int32_t H, int32_t type, uint32_t flags);
+int  spp_fp8_gated(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
+                   int32_t D, int32_t H, int32_t type, int32_t activation, uint32_t flags);
+int  spp_fp8_gated_grad(spp_ctx* ctx, const spp_row_list* lists, const spp_row_list* grads, int32_t n_lists, const void* d_weights,
+                        int32_t n_groups, int32_t D, int32_t H, int32_t type, int32_t activation, uint32_t flags);
+int  spp_fp8_weight_grad(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, int32_t n_groups, int32_t D, int32_t H,
+                         int32_t type, float* d_grad, uint32_t flags);
+
 /* Device-time accounting.  After spp_ctx_timing(ctx, 1) every call brackets its pieces of device
  * work with events on the stream they run on (vip total and per hop, the whole sampling of a
  * batch, gather classify / hit copy / miss copy).  spp_ctx_times waits for the context's streams,
@@ -446,7 +485,7 @@ int  spp_adamw_values(spp_ctx* ctx, const spp_adamw_tensor* tensors, int32_t n_t
  * since the last call, and starts a new accumulation.  spp_ctx_timing(ctx, 0) stops recording. */
 enum { SPP_T_VIP_TOTAL = 0, SPP_T_VIP_HOP_FIRST = 1 /* .. +L-1 */, SPP_T_SAMPLE = 9,
        SPP_T_GATHER_HIT = 10, SPP_T_GATHER_MISS = 11, SPP_T_GATHER_CLASSIFY = 12,
-       SPP_T_MX4 = 13 /* quantise, dequantise */, SPP_T_LAYER = 14 /* product, weight gradient */, SPP_T_ADAMW = 15, SPP_T_COUNT = 16 };
+       SPP_T_MX4 = 13 /* quantise, dequantise, in 4 or 8 bits */, SPP_T_LAYER = 14 /* products, gated layers, gradients */, SPP_T_ADAMW = 15, SPP_T_COUNT = 16 };
 int  spp_ctx_timing(spp_ctx* ctx, int enable);
 int  spp_ctx_times(spp_ctx* ctx, float* sum_ms /* [SPP_T_COUNT] */, int64_t* count /* [SPP_T_COUNT] */);
 /*     The same with the shortest and the median piece per index (0 where there was none); any of the

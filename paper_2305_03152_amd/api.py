@@ -39,6 +39,7 @@ SPP_MX4_MAX_COLS = 4096
 SPP_MAX_HIDDEN = 65536
 SPP_ADAMW_BLOCK = 256
 SPP_F32, SPP_F16, SPP_BF16 = 0, 1, 2
+SPP_SILU, SPP_GELU, SPP_SIGMOID = 0, 1, 2
 
 EXPORTS = [
     "spp_last_error", "spp_ctx_create", "spp_ctx_destroy", "spp_ctx_sync", "spp_graph_create",
@@ -50,6 +51,7 @@ EXPORTS = [
     "spp_stream_rates", "spp_gather_features_static",
     "spp_mx4_row_bytes", "spp_mx4_quantize", "spp_mx4_dequantize", "spp_mx4_product", "spp_mx4_weight_grad",
     "spp_adamw_step", "spp_adamw_load", "spp_adamw_values",
+    "spp_fp8_row_bytes", "spp_fp8_quantize", "spp_fp8_dequantize", "spp_fp8_product", "spp_fp8_gated", "spp_fp8_gated_grad", "spp_fp8_weight_grad",
 ]
 
 
@@ -182,6 +184,16 @@ def load_library():
                                     C.c_int32, C.c_uint32]
     lib.spp_mx4_weight_grad.argtypes = [C.c_void_p, C.POINTER(_RowList), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                         C.c_void_p, C.c_uint32]
+    lib.spp_fp8_row_bytes.argtypes = [C.c_int32]
+    lib.spp_fp8_row_bytes.restype = C.c_int64
+    lib.spp_fp8_quantize.argtypes = lib.spp_mx4_quantize.argtypes
+    lib.spp_fp8_dequantize.argtypes = lib.spp_mx4_dequantize.argtypes
+    lib.spp_fp8_product.argtypes = lib.spp_mx4_product.argtypes
+    lib.spp_fp8_gated.argtypes = [C.c_void_p, C.POINTER(_RowList), C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                  C.c_int32, C.c_uint32]
+    lib.spp_fp8_gated_grad.argtypes = [C.c_void_p, C.POINTER(_RowList), C.POINTER(_RowList), C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
+                                       C.c_int32, C.c_int32, C.c_int32, C.c_uint32]
+    lib.spp_fp8_weight_grad.argtypes = lib.spp_mx4_weight_grad.argtypes
     lib.spp_adamw_step.argtypes = [C.c_void_p, C.POINTER(_AdamwTensor), C.c_int32, C.c_int32, C.POINTER(_AdamwHyper), C.c_int64,
                                    C.c_uint32]
     lib.spp_adamw_load.argtypes = [C.c_void_p, C.POINTER(_AdamwTensor), C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
@@ -766,8 +778,8 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _packed(t: torch.Tensor, D: int, name: str) -> torch.Tensor:
-    rb = mx4_row_bytes(D)
+def _packed(t: torch.Tensor, D: int, name: str, row_bytes=None) -> torch.Tensor:
+    rb = (row_bytes or mx4_row_bytes)(D)
     if not (t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.dim() >= 2 and t.shape[-1] == rb):
         raise SppError(f"{name} must be a contiguous uint8 tensor on the GPU with rows of {rb} bytes")
     return t
@@ -791,29 +803,21 @@ def mx4_row_bytes(D: int) -> int:
     return int(rb)
 
 
-def mx4_quantize(ctx: Context, x: torch.Tensor, out: Optional[torch.Tensor] = None, n_device: Optional[torch.Tensor] = None,
-                 sync: bool = True) -> torch.Tensor:
-    """Rows [n, D] (float32, float16 or bfloat16, rows may be apart) in MXFP4: uint8 [n, mx4_row_bytes(D)].
-
-    The result is one piece of bytes per row: a row store of the gather, the cache and the local store like any other.
-    With n_device (one int64 on the GPU) only that many rows are read and written.
-    """
+def _quantize(ctx, x, out, n_device, sync, row_bytes, entry):
     _matrix(x, None, "x")
     ty = _type(x.dtype, "x")
     n, D = x.shape
-    rb = mx4_row_bytes(D)
+    rb = row_bytes(D)
     if out is None:
         out = _new(ctx, (n, rb), torch.uint8)
-    elif _packed(out, D, "out").dim() != 2 or out.shape[0] < n:
+    elif _packed(out, D, "out", row_bytes).dim() != 2 or out.shape[0] < n:
         raise SppError("out is too small")
-    _check(load_library().spp_mx4_quantize(ctx._h, x.data_ptr(), ty, n, _count(n_device), D, _ld(x), out.data_ptr(), SPP_SYNC if sync else 0))
+    _check(getattr(load_library(), entry)(ctx._h, x.data_ptr(), ty, n, _count(n_device), D, _ld(x), out.data_ptr(), SPP_SYNC if sync else 0))
     return out
 
 
-def mx4_dequantize(ctx: Context, rows: torch.Tensor, D: int, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
-                   n_device: Optional[torch.Tensor] = None, sync: bool = True) -> torch.Tensor:
-    """The values [n, D] that packed rows stand for, as `dtype` (or the type of `out`)."""
-    if _packed(rows, D, "rows").dim() != 2:
+def _dequantize(ctx, rows, D, dtype, out, n_device, sync, row_bytes, entry):
+    if _packed(rows, D, "rows", row_bytes).dim() != 2:
         raise SppError("rows must be a 2-D tensor")
     n = rows.shape[0]
     if out is None:
@@ -821,9 +825,25 @@ def mx4_dequantize(ctx: Context, rows: torch.Tensor, D: int, dtype: torch.dtype 
         out = _new(ctx, (n, D), dtype)
     elif _matrix(out, D, "out").shape[0] < n:
         raise SppError("out is too small")
-    _check(load_library().spp_mx4_dequantize(ctx._h, rows.data_ptr(), n, _count(n_device), D, out.data_ptr(), _type(out.dtype, "out"), _ld(out),
-                                             SPP_SYNC if sync else 0))
+    _check(getattr(load_library(), entry)(ctx._h, rows.data_ptr(), n, _count(n_device), D, out.data_ptr(), _type(out.dtype, "out"), _ld(out),
+                                          SPP_SYNC if sync else 0))
     return out
+
+
+def mx4_quantize(ctx: Context, x: torch.Tensor, out: Optional[torch.Tensor] = None, n_device: Optional[torch.Tensor] = None,
+                 sync: bool = True) -> torch.Tensor:
+    """Rows [n, D] (float32, float16 or bfloat16, rows may be apart) in MXFP4: uint8 [n, mx4_row_bytes(D)].
+
+    The result is one piece of bytes per row: a row store of the gather, the cache and the local store like any other.
+    With n_device (one int64 on the GPU) only that many rows are read and written.
+    """
+    return _quantize(ctx, x, out, n_device, sync, mx4_row_bytes, "spp_mx4_quantize")
+
+
+def mx4_dequantize(ctx: Context, rows: torch.Tensor, D: int, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                   n_device: Optional[torch.Tensor] = None, sync: bool = True) -> torch.Tensor:
+    """The values [n, D] that packed rows stand for, as `dtype` (or the type of `out`)."""
+    return _dequantize(ctx, rows, D, dtype, out, n_device, sync, mx4_row_bytes, "spp_mx4_dequantize")
 
 
 class RowLists:
@@ -861,8 +881,8 @@ class RowLists:
             a.ld, a.group = _ld(y), group
             self.groups = max(self.groups, group + 1)
 
-    def _fit(self, D: int, H: int, groups: int):
-        if self.lists and (self.row_bytes != mx4_row_bytes(D) or self.H != H):
+    def _fit(self, D: int, H: int, groups: int, row_bytes=None):
+        if self.lists and (self.row_bytes != (row_bytes or mx4_row_bytes)(D) or self.H != H):
             raise SppError(f"the lists are not of {D} columns and {H} outputs")
         if self.groups > groups:
             raise SppError(f"a list names group {self.groups - 1} of {groups}")
@@ -913,6 +933,151 @@ def mx4_weight_grad(ctx: Context, lists, H: int, D: int, groups: int = 1, out: O
     elif _dev(out, torch.float32, "out").numel() != groups * H * D:
         raise SppError("out must hold groups * H * D values")
     _check(load_library().spp_mx4_weight_grad(ctx._h, lists._arr, len(lists.lists), groups, D, H, _TYPES[lists.dtype or torch.float32],
+                                              out.data_ptr(), SPP_SYNC if sync else 0))
+    return out
+
+
+@functools.lru_cache(maxsize=None)
+def fp8_row_bytes(D: int) -> int:
+    """Bytes of a row of D columns in 8 bits: a code per column and a scale byte per 128, each rounded up to a multiple of 16."""
+    rb = load_library().spp_fp8_row_bytes(int(D))
+    if rb < 0:
+        _check(int(rb))
+    return int(rb)
+
+
+def fp8_quantize(ctx: Context, x: torch.Tensor, out: Optional[torch.Tensor] = None, n_device: Optional[torch.Tensor] = None,
+                 sync: bool = True) -> torch.Tensor:
+    """Rows [n, D] (float32, float16 or bfloat16, rows may be apart) in 8 bits: uint8 [n, fp8_row_bytes(D)].
+
+    E4M3 with a power of two as scale for every 128 columns of a row: a hidden layer's input, as the layer reads it and as its
+    backward pass finds it again.  NaN and infinities become NaN.  With n_device (one int64 on the GPU) only that many rows are
+    read and written.
+    """
+    return _quantize(ctx, x, out, n_device, sync, fp8_row_bytes, "spp_fp8_quantize")
+
+
+def fp8_dequantize(ctx: Context, rows: torch.Tensor, D: int, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                   n_device: Optional[torch.Tensor] = None, sync: bool = True) -> torch.Tensor:
+    """The values [n, D] that rows in 8 bits stand for, as `dtype` (or the type of `out`)."""
+    return _dequantize(ctx, rows, D, dtype, out, n_device, sync, fp8_row_bytes, "spp_fp8_dequantize")
+
+
+_ACTIVATIONS = {"silu": SPP_SILU, "gelu": SPP_GELU, "sigmoid": SPP_SIGMOID}
+
+
+def _activation(name: str) -> int:
+    if name not in _ACTIVATIONS:
+        raise SppError("activation must be 'silu', 'gelu' or 'sigmoid'")
+    return _ACTIVATIONS[name]
+
+
+def _fp8_weights(lists, weights: torch.Tensor, D: int, per: int):
+    """(lists, groups, H) of weights with `per` matrices of H rows for each group."""
+    lists = lists if isinstance(lists, RowLists) else RowLists(lists)
+    _packed(weights, D, "weights", fp8_row_bytes)
+    if weights.dim() not in (2, 3):
+        raise SppError("weights must be [rows, row bytes] or [groups, rows, row bytes]")
+    groups, rows = (1, weights.shape[0]) if weights.dim() == 2 else weights.shape[:2]
+    if rows % per:
+        raise SppError(f"weights must have the same number of rows for both factors, not {rows} in all")
+    lists._fit(D, rows // per, groups, fp8_row_bytes)
+    return lists, groups, rows // per
+
+
+def fp8_product_multi(ctx: Context, lists, weights: torch.Tensor, D: int, sync: bool = True):
+    """Y_j = X_j W[group_j]^T for every list of rows in 8 bits, in one launch; `lists` is a RowLists or what makes one.
+
+    weights: uint8 [groups, H, row bytes] or [H, row bytes], rows of D columns (fp8_quantize of a matrix [H, D]).  The gradient of a
+    layer's rows is this product too, of the outputs' gradient in 8 bits and the transposed weights (fp8_quantize of [D, H]).
+    """
+    lists, groups, H = _fp8_weights(lists, weights, D, 1)
+    if lists.lists:
+        _check(load_library().spp_fp8_product(ctx._h, lists._arr, len(lists.lists), weights.data_ptr(), groups, D, H, _TYPES[lists.dtype],
+                                              SPP_SYNC if sync else 0))
+    elif sync:
+        ctx.sync()
+
+
+def fp8_product(ctx: Context, rows: torch.Tensor, weight: torch.Tensor, D: int, n: Optional[int] = None,
+                n_device: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                sync: bool = True) -> torch.Tensor:
+    """Y [n, H] = X W^T of one list of rows in 8 bits and one weight matrix [H, row bytes]."""
+    if weight.dim() != 2:
+        raise SppError("weight must be [H, row bytes]")
+    n = int(rows.shape[0] if n is None else n)
+    if out is None:
+        _type(dtype, "dtype")
+        out = _new(ctx, (n, weight.shape[0]), dtype)
+    fp8_product_multi(ctx, [(rows, n, n_device, out)], weight, D, sync=sync)
+    return out
+
+
+def fp8_gated_multi(ctx: Context, lists, weights: torch.Tensor, D: int, activation: str = "silu", sync: bool = True):
+    """Y_j = act(X_j Wg^T) * (X_j Wu^T) for every list of rows in 8 bits, in one launch; `lists` is a RowLists or what makes one.
+
+    weights: uint8 [groups, 2H, row bytes] or [2H, row bytes], for each group the H rows of Wg and then those of Wu.  activation:
+    'silu', 'gelu' or 'sigmoid'.  Nothing else is kept for the backward pass: it needs the rows only.
+    """
+    act = _activation(activation)
+    lists, groups, H = _fp8_weights(lists, weights, D, 2)
+    if lists.lists:
+        _check(load_library().spp_fp8_gated(ctx._h, lists._arr, len(lists.lists), weights.data_ptr(), groups, D, H, _TYPES[lists.dtype], act,
+                                            SPP_SYNC if sync else 0))
+    elif sync:
+        ctx.sync()
+
+
+def fp8_gated(ctx: Context, rows: torch.Tensor, weight: torch.Tensor, D: int, activation: str = "silu", n: Optional[int] = None,
+              n_device: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+              sync: bool = True) -> torch.Tensor:
+    """Y [n, H] of one list of rows in 8 bits and one pair of matrices [2H, row bytes]."""
+    if weight.dim() != 2:
+        raise SppError("weight must be [2H, row bytes]")
+    n = int(rows.shape[0] if n is None else n)
+    if out is None:
+        _type(dtype, "dtype")
+        out = _new(ctx, (n, weight.shape[0] // 2), dtype)
+    fp8_gated_multi(ctx, [(rows, n, n_device, out)], weight, D, activation=activation, sync=sync)
+    return out
+
+
+def fp8_gated_grad(ctx: Context, lists, grads, weights: torch.Tensor, D: int, activation: str = "silu", sync: bool = True):
+    """The gradients of a gated layer's two factors: dP_j = [dY_j * U_j * act'(G_j) | dY_j * act(G_j)].
+
+    lists: the rows that the layer read, each with dY_j [n, H] as its y.  grads: the same rows, counts and groups, each with the
+    matrix [n, 2H] that dP_j is written to as its y; fp8_weight_grad of it is the gradient of the weights.  G and U are formed
+    again from the rows.  dP must not overlap dY.
+    """
+    act = _activation(activation)
+    lists, groups, H = _fp8_weights(lists, weights, D, 2)
+    grads = grads if isinstance(grads, RowLists) else RowLists(grads)
+    if len(grads.lists) != len(lists.lists):
+        raise SppError("grads must have a list for each of lists")
+    grads._fit(D, 2 * H, groups, fp8_row_bytes)
+    if lists.dtype is not grads.dtype:
+        raise SppError("grads must have the type of lists")
+    if lists.lists:
+        _check(load_library().spp_fp8_gated_grad(ctx._h, lists._arr, grads._arr, len(lists.lists), weights.data_ptr(), groups, D, H,
+                                                 _TYPES[lists.dtype], act, SPP_SYNC if sync else 0))
+    elif sync:
+        ctx.sync()
+
+
+def fp8_weight_grad(ctx: Context, lists, H: int, D: int, groups: int = 1, out: Optional[torch.Tensor] = None,
+                    sync: bool = True) -> torch.Tensor:
+    """float32 [groups, H, D]: for every group the sum of Y_j^T X_j over its lists of rows in 8 bits, Y_j being a layer's gradient.
+
+    With the grads of fp8_gated_grad and twice its H: the gradients of Wg and Wu, one behind the other.  Zeros for a group without
+    rows.  The same rows give the same bits, whatever room the lists' buffers have.
+    """
+    lists = lists if isinstance(lists, RowLists) else RowLists(lists)
+    lists._fit(D, H, groups, fp8_row_bytes)
+    if out is None:
+        out = _new(ctx, (groups, H, D), torch.float32)
+    elif _dev(out, torch.float32, "out").numel() != groups * H * D:
+        raise SppError("out must hold groups * H * D values")
+    _check(load_library().spp_fp8_weight_grad(ctx._h, lists._arr, len(lists.lists), groups, D, H, _TYPES[lists.dtype or torch.float32],
                                               out.data_ptr(), SPP_SYNC if sync else 0))
     return out
 

@@ -1,0 +1,139 @@
+// The layers that read hidden rows in 8 bits, and the backward pass of the gated one, over the lists of the product:
+//
+//   product      Y_j = X_j W[g_j]^T                                 X_j [n_j, D], W[g] [H, D] in 8 bits
+//   gated        Y_j = act(X_j Wg[g_j]^T) * (X_j Wu[g_j]^T)         W[g] = Wg, then Wu, H rows each
+//   its gradient [dY_j * u * act'(g) | dY_j * act(g)]               g and u formed again from X_j and W[g_j], as in the forward pass
+//
+// Codes are E4M3 and scales powers of two: a product has 8 bits.  Results of 16 bits are formed by the matrix instruction for 8-bit floats,
+// which takes the scales.  It adds the products of eight neighbouring columns after cutting each off at 2^-13 of the power of two of
+// the largest (measured: beside 2^16 an addend of 2^3 counts and one of 2^2 does not), everything else in fp32: normally distributed rows
+// come out 1.4e-5 off, where rounding the result to bf16 costs 1.7e-3 and to fp16 2e-4.  Results of 32 bits, which would show it, are formed by
+// the bf16 instruction, at half the rate, of values decoded in registers: a code under a scale is exact in bf16, the products are
+// exact and the sums fp32.  The activation is computed in fp32, and what is written is rounded once.
+#pragma once
+
+#include "spp_fp8.h"
+#include "spp_rows_out.h"
+
+#include <type_traits>
+
+namespace spp {
+
+enum HiddenMode { kProduct, kGated, kGatedGrad };
+
+struct HiddenArgs {
+    RowTable       t;
+    void*          dp[kRowLists];        // gradient of the gated layer: where each list's goes, [n_j, 2H]
+    int64_t        dp_ld[kRowLists];
+    const uint8_t* w;
+    int32_t        D, H, rb, cb, steps;  // steps of 128 columns
+    int32_t        act;
+};
+
+// ---- operands -------------------------------------------------------------------------------------
+
+// A lane's 32 codes of a step of 128 columns, 16 from 16 q and 16 from 64 + 16 q on, q being its quarter of the wavefront, and their
+// scale's byte.
+struct Operand {
+    u32x4 lo, hi;
+    uint32_t scale;
+};
+__device__ __forceinline__ i32x8 codes_of(const Operand& o) {
+    return i32x8{(int)o.lo.x, (int)o.lo.y, (int)o.lo.z, (int)o.lo.w, (int)o.hi.x, (int)o.hi.y, (int)o.hi.z, (int)o.hi.w};
+}
+// The values of eight of them.
+__device__ __forceinline__ bf16x8 eight_of(uint32_t a, uint32_t b, float s) {
+    const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true),
+                 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, false), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true);
+    return bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+}
+struct Decoded { bf16x8 v[4]; };
+__device__ __forceinline__ Decoded decode(const Operand& o) {
+    const float s = mx4_scale(o.scale & 255u);
+    return Decoded{{eight_of(o.lo.x, o.lo.y, s), eight_of(o.lo.z, o.lo.w, s), eight_of(o.hi.x, o.hi.y, s), eight_of(o.hi.z, o.hi.w, s)}};
+}
+// acc[c][f] += X[c] W[f]^T over a step, rows of X as rows of the result.
+template <bool Exact, int RN, int FN>
+__device__ __forceinline__ void multiply(f32x4 (&acc)[RN][FN], const Operand (&x)[RN], const Operand (&w)[FN]) {
+    if constexpr (Exact) {
+        Decoded xd[RN];
+#pragma unroll
+        for (int c = 0; c < RN; ++c) xd[c] = decode(x[c]);
+#pragma unroll
+        for (int f = 0; f < FN; ++f) {
+            const Decoded wd = decode(w[f]);
+#pragma unroll
+            for (int c = 0; c < RN; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[c][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xd[c].v[j], wd.v[j], acc[c][f], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int f = 0; f < FN; ++f)
+#pragma unroll
+            for (int c = 0; c < RN; ++c)
+                acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes_of(x[c]), codes_of(w[f]), acc[c][f], 0, 0, 0, (int)x[c].scale, 0,
+                                                                             (int)w[f].scale);
+    }
+}
+
+// ---- activations ----------------------------------------------------------------------------------
+
+// 1 / (1 + exp(-g)) and 1 / (1 + exp(g)), from exp(-|g|), which is at most 1: neither loses its small values.
+__device__ __forceinline__ void sigmoids(float g, float& s, float& r) {
+    const float t = __builtin_amdgcn_exp2f(__builtin_fabsf(g) * -1.44269504f);
+    const float p = __builtin_amdgcn_rcpf(1.0f + t), q = t * p;
+    s = g >= 0.0f ? p : q;
+    r = g >= 0.0f ? q : p;
+}
+template <int Act> __device__ __forceinline__ float activate(float g) {
+    if constexpr (Act == SPP_GELU) {
+        return g * (0.5f * erfcf(g * -0.70710678f));
+    } else {
+        float s, r;
+        sigmoids(g, s, r);
+        return Act == SPP_SILU ? g * s : s;
+    }
+}
+// act(g) and act'(g)
+template <int Act> __device__ __forceinline__ void activate_both(float g, float& f, float& d) {
+    if constexpr (Act == SPP_GELU) {
+        const float p = 0.5f * erfcf(g * -0.70710678f);
+        f = g * p;
+        d = p + g * (__builtin_amdgcn_exp2f(g * g * -0.72134752f) * 0.39894228f);
+    } else {
+        float s, r;
+        sigmoids(g, s, r);
+        f = Act == SPP_SILU ? g * s : s;
+        d = Act == SPP_SILU ? s * (1.0f + g * r) : s * r;
+    }
+}
+// The activation is the same for the whole call: a branch around a tile's worth of work.
+template <class Use> __device__ __forceinline__ void with_activation(int act, Use use) {
+    if (act == SPP_SILU) use(std::integral_constant<int, SPP_SILU>());
+    else if (act == SPP_GELU) use(std::integral_constant<int, SPP_GELU>());
+    else use(std::integral_constant<int, SPP_SIGMOID>());
+}
+
+// Columns h .. h+3 of rows y[0..3], of which `have` are there; others are zeros.
+template <class T>
+__device__ __forceinline__ void get_tile(const T* y, int64_t ld, int have, int h, int H, bool wide, f32x4 (&v)[4]) {
+    typedef typename Elem<T>::v4 V;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        V x = {(T)0.0f, (T)0.0f, (T)0.0f, (T)0.0f};
+        const T* from = y + i * ld + h;
+        if (i < have) {
+            if (wide && h + 4 <= H) x = *reinterpret_cast<const V*>(from);
+            else if (h + 4 <= H) x = reinterpret_cast<const Loose<V>*>(from)->v;
+            else
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (h + k < H) x[k] = from[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k][i] = (float)x[k];
+    }
+}
+
+}  // namespace spp
