@@ -28,12 +28,27 @@ struct HiddenArgs {
     const uint8_t* w;
     int32_t        D, H, rb, cb, steps;  // steps of 128 columns
     int32_t        act;
+    // the form that holds W in LDS
+    int32_t        ls;           // bytes of a row of W there: its codes and zeros up to whole steps, then its scales; an odd number of 16
+    uint32_t       magic;        // ceil(2^32 / (ls / 16))
+    int32_t        fill;         // workgroups that few rows are dealt out to
+    int32_t        w_lds;        // bytes of W; behind them, per wavefront, room for rows on their way:
+    int32_t        out_lds;      // bytes
 };
+
+// f(0), f(1) .. with the index as a constant.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void steps_of(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        steps_of<N, I + 1>(f);
+    }
+}
 
 // ---- operands -------------------------------------------------------------------------------------
 
-// A lane's 32 codes of a step of 128 columns, 16 from 16 q and 16 from 64 + 16 q on, q being its quarter of the wavefront, and their
-// scale's byte.
+// A lane's 32 codes of a step of 128 columns, 16 from 16 q and 16 from 64 + 16 q on, q being its quarter of the wavefront, and the
+// scales of four steps, a byte each.
 struct Operand {
     u32x4 lo, hi;
     uint32_t scale;
@@ -48,20 +63,21 @@ __device__ __forceinline__ bf16x8 eight_of(uint32_t a, uint32_t b, float s) {
     return bf16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
 }
 struct Decoded { bf16x8 v[4]; };
+template <int Byte>
 __device__ __forceinline__ Decoded decode(const Operand& o) {
-    const float s = mx4_scale(o.scale & 255u);
+    const float s = mx4_scale((o.scale >> (8 * Byte)) & 255u);
     return Decoded{{eight_of(o.lo.x, o.lo.y, s), eight_of(o.lo.z, o.lo.w, s), eight_of(o.hi.x, o.hi.y, s), eight_of(o.hi.z, o.hi.w, s)}};
 }
 // acc[c][f] += X[c] W[f]^T over a step, rows of X as rows of the result.
-template <bool Exact, int RN, int FN>
+template <bool Exact, int Byte, int RN, int FN>
 __device__ __forceinline__ void multiply(f32x4 (&acc)[RN][FN], const Operand (&x)[RN], const Operand (&w)[FN]) {
     if constexpr (Exact) {
         Decoded xd[RN];
 #pragma unroll
-        for (int c = 0; c < RN; ++c) xd[c] = decode(x[c]);
+        for (int c = 0; c < RN; ++c) xd[c] = decode<Byte>(x[c]);
 #pragma unroll
         for (int f = 0; f < FN; ++f) {
-            const Decoded wd = decode(w[f]);
+            const Decoded wd = decode<Byte>(w[f]);
 #pragma unroll
             for (int c = 0; c < RN; ++c)
 #pragma unroll
@@ -72,8 +88,8 @@ __device__ __forceinline__ void multiply(f32x4 (&acc)[RN][FN], const Operand (&x
         for (int f = 0; f < FN; ++f)
 #pragma unroll
             for (int c = 0; c < RN; ++c)
-                acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes_of(x[c]), codes_of(w[f]), acc[c][f], 0, 0, 0, (int)x[c].scale, 0,
-                                                                             (int)w[f].scale);
+                acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes_of(x[c]), codes_of(w[f]), acc[c][f], 0, 0, Byte, (int)x[c].scale,
+                                                                             Byte, (int)w[f].scale);
     }
 }
 
@@ -135,5 +151,57 @@ __device__ __forceinline__ void get_tile(const T* y, int64_t ld, int have, int h
         for (int k = 0; k < 4; ++k) v[k][i] = (float)x[k];
     }
 }
+
+// What 64 columns of the two factors become: of the gated layer Y, in `one`; of its gradient dG and dU, in `one` and `two`.
+template <int Mode>
+__device__ __forceinline__ void combine(int act, f32x4 (&one)[4], f32x4 (&two)[4], const f32x4 (&dy)[4]) {
+    if constexpr (Mode == kGated) {
+        with_activation(act, [&](auto kind) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) one[k][i] = activate<decltype(kind)::value>(one[k][i]) * two[k][i];
+        });
+    } else if constexpr (Mode == kGatedGrad) {
+        with_activation(act, [&](auto kind) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float f, d;
+                    activate_both<decltype(kind)::value>(one[k][i], f, d);
+                    one[k][i] = dy[k][i] * two[k][i] * d;
+                    two[k][i] = dy[k][i] * f;
+                }
+        });
+    }
+}
+
+// A list's matrices of results: Y, read or written, and dP.  `row`: of the list; `have`: rows that are there from it on.
+template <class T, int Mode>
+struct Results {
+    T*      y;
+    T*      p;
+    int64_t ld, pld;
+    bool    wide, pwide;
+    __device__ __forceinline__ Results(const HiddenArgs& a, int list) {
+        y = static_cast<T*>(a.t.y[list]);
+        ld = a.t.ld[list];
+        wide = ((uintptr_t)y | (uint64_t)(ld * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0;
+        if constexpr (Mode == kGatedGrad) {
+            p = static_cast<T*>(a.dp[list]);
+            pld = a.dp_ld[list];
+            pwide = ((uintptr_t)p | (uint64_t)(pld * (int64_t)sizeof(T)) | (uint64_t)(a.H * (int)sizeof(T))) % (4 * sizeof(T)) == 0;
+        }
+    }
+    __device__ __forceinline__ void get(const HiddenArgs& a, int64_t row, int have, int h, f32x4 (&v)[4]) const { get_tile<T>(y + row * ld, ld, have, h, a.H, wide, v); }
+    __device__ __forceinline__ void put(const HiddenArgs& a, int64_t row, int have, int h, const f32x4 (&v)[4]) const {
+        if constexpr (Mode == kGatedGrad) put_tile<T>(p + row * pld, pld, have, h, a.H, pwide, v);
+        else put_tile<T>(y + row * ld, ld, have, h, a.H, wide, v);
+    }
+    __device__ __forceinline__ void put_second(const HiddenArgs& a, int64_t row, int have, int h, const f32x4 (&v)[4]) const {
+        put_tile<T>(p + row * pld + a.H, pld, have, h, a.H, pwide, v);
+    }
+};
 
 }  // namespace spp

@@ -79,53 +79,239 @@ __global__ void __launch_bounds__(kTileBlock) hidden_tile_kernel(HiddenArgs a) {
             for (int c = 0; c < 2; ++c) xv[c] = operand_at(32 * wave + 16 * c + m);
 #pragma unroll
             for (int f = 0; f < 8; ++f) wv[f] = operand_at(kTileRows + 16 * f + m);
-            multiply<sizeof(T) == 4>(acc, xv, wv);
+            multiply<sizeof(T) == 4, 0>(acc, xv, wv);
         }
-        const int64_t ld = a.t.ld[list];
-        T* y = static_cast<T*>(a.t.y[list]) + r0 * ld;
-        const bool wide = ((uintptr_t)a.t.y[list] | (uint64_t)(ld * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0;
+        const Results<T, Mode> out(a, list);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const int row = 32 * wave + 16 * c + 4 * q, have = here - row;
+            const int row = 32 * wave + 16 * c + 4 * q;
             f32x4(&one)[4] = reinterpret_cast<f32x4(&)[4]>(acc[c][0]);
             f32x4(&two)[4] = reinterpret_cast<f32x4(&)[4]>(acc[c][4]);
+            f32x4 dy[4];
+            if constexpr (Mode == kGatedGrad) out.get(a, r0 + row, here - row, h0 + 4 * m, dy);
+            combine<Mode>(a.act, one, two, dy);
             if constexpr (Mode == kProduct) {
-                put_tile<T>(y + row * ld, ld, have, h0 + 4 * m, a.H, wide, one);
-                put_tile<T>(y + row * ld, ld, have, h0 + 64 + 4 * m, a.H, wide, two);
-            } else if constexpr (Mode == kGated) {
-                with_activation(a.act, [&](auto act) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) one[k][i] = activate<decltype(act)::value>(one[k][i]) * two[k][i];
-                });
-                put_tile<T>(y + row * ld, ld, have, h0 + 4 * m, a.H, wide, one);
+                out.put(a, r0 + row, here - row, h0 + 4 * m, one);
+                out.put(a, r0 + row, here - row, h0 + 64 + 4 * m, two);
             } else {
-                f32x4 dy[4];
-                get_tile<T>(y + row * ld, ld, have, h0 + 4 * m, a.H, wide, dy);
-                with_activation(a.act, [&](auto act) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float f, d;
-                            activate_both<decltype(act)::value>(one[k][i], f, d);
-                            one[k][i] = dy[k][i] * two[k][i] * d;
-                            two[k][i] = dy[k][i] * f;
-                        }
-                });
-                const int64_t pld = a.dp_ld[list];
-                T* p = static_cast<T*>(a.dp[list]) + (r0 + row) * pld;
-                const bool pwide = ((uintptr_t)a.dp[list] | (uint64_t)(pld * (int64_t)sizeof(T)) | (uint64_t)(a.H * (int)sizeof(T))) % (4 * sizeof(T)) == 0;
-                put_tile<T>(p, pld, have, h0 + 4 * m, a.H, pwide, one);
-                put_tile<T>(p + a.H, pld, have, h0 + 4 * m, a.H, pwide, two);
+                out.put(a, r0 + row, here - row, h0 + 4 * m, one);
+                if constexpr (Mode == kGatedGrad) out.put_second(a, r0 + row, here - row, h0 + 4 * m, two);
             }
         }
     }
 }
 
+// ---- W in LDS --------------------------------------------------------------------------------------
+
+// The form for weights that LDS holds.  A wavefront keeps its 16 RN rows of X in registers, all columns of them, and goes over the columns of
+// the result 64 at a time (64 of the gate's and the same 64 of the other factor); a workgroup's wavefronts share W and wait for each other only
+// where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.
+constexpr int kHeldWaves = 8, kHeldBlock = 64 * kHeldWaves;
+template <class T, int Mode, int KS, int RN, bool Lines>
+__global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    constexpr int TB = kHeldWaves * 16 * RN, MR = Mode == kProduct ? 64 : 128;       // rows of X per workgroup, rows of W per 64 columns
+    constexpr bool kAhead = KS * RN <= 4, kExact = sizeof(T) == 4;
+    const Lists lists(a.t, TB);
+    const int total = lists.total();
+    if (total == 0) return;
+    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
+    const int ht = (a.H + 63) / 64;
+    int parts = a.fill / total;                        // few rows: the columns of the result are dealt out too
+    parts = parts < 1 ? 1 : parts > ht ? ht : parts;
+    const int64_t items = (int64_t)total * parts;
+    int held_group = -1, held_from = -1;
+    struct Item { int part, list, here, group; int64_t r0; };
+    auto find = [&](int64_t item) {
+        Item it;
+        it.part = (int)(item / total);
+        const int tile = (int)(item - (int64_t)it.part * total);
+        it.list = lists.list_of(tile);
+        it.r0 = (int64_t)(tile - lists.first_tile(it.list)) * TB;
+        const int64_t left = lists.rows_in(it.list) - it.r0;
+        it.here = left < TB ? (int)left : TB;
+        it.group = a.t.group[it.list];
+        return it;
+    };
+    u32x4 ahead[KS][RN][2];
+    uint32_t ahead_scale[(KS + 3) / 4][RN];
+    auto ask_rows = [&](const Item& it) {
+        const uint8_t* x = a.t.rows[it.list] + it.r0 * a.rb;
+#pragma unroll
+        for (int c = 0; c < RN; ++c) {
+            const int row = (wave * RN + c) * 16 + m;
+            const uint8_t* p = x + (int64_t)(row < it.here ? row : it.here - 1) * a.rb;
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = 128 * s + 64 * k + 16 * q;
+                    ahead[s][c][k] = *reinterpret_cast<const u32x4*>(p + (at < a.cb ? at : 0));
+                }
+#pragma unroll
+            for (int s = 0; s < (KS + 3) / 4; ++s) ahead_scale[s][c] = *reinterpret_cast<const uint32_t*>(p + a.cb + (4 * s < a.steps ? 4 * s : 0));
+        }
+    };
+    const Share share(items);
+    if (share.at >= share.end) return;
+    Item it = find(share.at);
+    if (kAhead) ask_rows(it);
+    for (int64_t item = share.at; item < share.end; item += share.step) {
+        if (!kAhead) { it = find(item); ask_rows(it); }
+        const int t0 = (int)((int64_t)it.part * ht / parts), t1 = (int)((int64_t)(it.part + 1) * ht / parts);
+        const int list = it.list, here = it.here, group = it.group, mine = here - wave * 16 * RN;       // rows of the workgroup, of the wavefront
+        const int64_t r0 = it.r0 + wave * 16 * RN;
+        if (group != held_group || t0 != held_from) {
+            const uint8_t* w = a.w + (int64_t)group * a.H * (MR / 64) * a.rb;
+            const uint32_t lv = (uint32_t)a.ls / 16, all = (uint32_t)(t1 - t0) * MR * lv;
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < all; i += kHeldBlock) {
+                const uint32_t r = __umulhi(i, a.magic), v = i - r * lv;             // LDS row: by operand, columns 4m + f of 64 as row 16 f + m
+                int h = 64 * (t0 + (int)(r / MR)) + 4 * (int)(r & 15) + (int)(r >> 4 & 3);
+                h = h < a.H ? h : a.H - 1;
+                const uint8_t* from = w + (int64_t)(MR == 128 && (r & 64) ? a.H + h : h) * a.rb;
+                const int at = v == lv - 1 ? a.cb : 16 * (int)v;
+                const u32x4 x = *reinterpret_cast<const u32x4*>(from + (v == lv - 1 || at < a.cb ? at : 0));
+                reinterpret_cast<u32x4*>(lds)[i] = v == lv - 1 || at < a.cb ? x : u32x4{0, 0, 0, 0};
+            }
+            held_group = group; held_from = t0;
+            __syncthreads();
+        }
+        Operand x[KS][RN];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int c = 0; c < RN; ++c) {
+                const int at = 128 * s + 16 * q;
+                x[s][c].lo = at < a.cb ? ahead[s][c][0] : u32x4{0, 0, 0, 0};
+                x[s][c].hi = at + 64 < a.cb ? ahead[s][c][1] : u32x4{0, 0, 0, 0};
+                x[s][c].scale = ahead_scale[s / 4][c];
+            }
+        if (kAhead && item + share.step < share.end) { it = find(item + share.step); ask_rows(it); }
+        if (mine <= 0) continue;
+        const Results<T, Mode> res(a, list);
+        T* const y = (Mode == kGatedGrad ? res.p : res.y);
+        const int64_t ld = Mode == kGatedGrad ? res.pld : res.ld;
+        constexpr int kOuts = Mode == kGatedGrad ? 2 : 1;
+        RowsOut<T, RN> out[kOuts];
+        if constexpr (!Lines) {
+#pragma unroll
+            for (int k = 0; k < kOuts; ++k) {
+                out[k].lds = lds + a.w_lds + (wave * kOuts + k) * a.out_lds;
+                out[k].rows = mine < 16 * RN ? mine : 16 * RN;
+                out[k].step = ld * (int64_t)sizeof(T);
+                out[k].y = reinterpret_cast<char*>(y + r0 * ld + k * a.H + 64 * t0);
+                out[k].bytes = ((64 * t1 < a.H ? 64 * t1 : a.H) - 64 * t0) * (int)sizeof(T);
+                out[k].run = kOuts == 1 && out[k].bytes == out[k].step && 16 * RN * out[k].bytes + 16 <= a.out_lds;
+                out[k].begin();
+            }
+        }
+        for (int t = t0; t < t1; ++t) {
+            const uint8_t* tile_w = lds + (t - t0) * MR * a.ls;
+            const bool whole = mine >= 16 * RN && 64 * t + 64 <= a.H;
+            f32x4 dy[RN][4];
+            if constexpr (Mode == kGatedGrad) {
+#pragma unroll
+                for (int c = 0; c < RN; ++c) res.get(a, r0 + 16 * c + 4 * q, mine - 16 * c - 4 * q, 64 * t + 4 * m, dy[c]);
+            }
+            f32x4 acc[MR / 64][RN][4];
+#pragma unroll
+            for (int k = 0; k < MR / 64; ++k) {
+#pragma unroll
+                for (int c = 0; c < RN; ++c)
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) acc[k][c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+                steps_of<KS>([&](auto step) {
+                    constexpr int s = decltype(step)::value;
+                    if (s < a.steps) {
+                        Operand w[4];
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) {
+                            const uint8_t* p = tile_w + (64 * k + 16 * f + m) * a.ls;
+                            w[f].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
+                            w[f].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
+                            w[f].scale = *reinterpret_cast<const uint32_t*>(p + 128 * a.steps + 4 * (s / 4));
+                        }
+                        multiply<kExact, (s & 3)>(acc[k], x[s], w);
+                    }
+                });
+            }
+#pragma unroll
+            for (int c = 0; c < RN; ++c) combine<Mode>(a.act, acc[0][c], acc[MR / 64 - 1][c], dy[c]);
+            if constexpr (Lines) {
+#pragma unroll
+                for (int k = 0; k < kOuts; ++k)
+#pragma unroll
+                    for (int c = 0; c < RN; ++c) {
+                        T* at = y + (r0 + 16 * c + 4 * q) * ld + k * a.H;
+                        if (whole) put_whole<T>(at + 64 * t + 4 * m, ld, acc[k][c]);
+                        else put_tile<T>(at, ld, mine - 16 * c - 4 * q, 64 * t + 4 * m, a.H, true, acc[k][c]);
+                    }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kOuts; ++k) {
+                    out[k].put(t - t0, acc[k]);
+                    if (!out[k].run) out[k].flush_lines(t - t0, t == t0, t + 1 == t1);
+                    else if (t + 1 == t1) out[k].flush_run();
+                }
+            }
+        }
+    }
+}
+
+constexpr int kHeldLds = 163840;         // all of a CU's
+constexpr int kHeldRowOut = 768;         // bytes of rows that go out in one run
+template <class T, int Mode, int KS, bool Lines>
+static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
+    constexpr int RN = KS <= 2 && Lines ? 2 : 1, MR = Mode == kProduct ? 64 : 128, TB = kHeldWaves * 16 * RN, outs = Mode == kGatedGrad ? 2 : 1;
+    auto kernel = hidden_held_kernel<T, Mode, KS, RN, Lines>;
+    const int ht = (a.H + 63) / 64, row = a.H * (int)sizeof(T);
+    a.out_lds = Lines ? 0 : 16 * RN * RowsOut<T, RN>::kPitch;
+    if (!Lines && outs == 1 && row <= kHeldRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
+    const int64_t need = (int64_t)ht * MR * a.ls, most_lds = kHeldLds - (int64_t)kHeldWaves * outs * a.out_lds;
+    *done = need <= most_lds;
+    if (!*done) return SPP_OK;
+    a.w_lds = (int)need;
+    const int lds = a.w_lds + kHeldWaves * outs * a.out_lds;
+    static LdsLimit limit;
+    SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
+    int64_t tiles = 0;
+    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)TB - 1) / TB;
+    a.fill = ctx->num_cu;
+    const int fit = kHeldLds / lds, per_cu = fit < 1 ? 1 : fit > 2 ? 2 : fit;
+    const int64_t want = tiles >= a.fill ? tiles : tiles * ht < a.fill ? tiles * ht : a.fill, most = (int64_t)ctx->num_cu * per_cu;
+    kernel<<<(unsigned)(want < most ? want : most), kHeldBlock, lds, ctx->stream>>>(a);
+    SPP_HIP(hipGetLastError());
+    return SPP_OK;
+}
 template <class T, int Mode>
-static int launch_hidden(spp_ctx* ctx, const HiddenArgs& a) {
+static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
+    *done = false;
+    a.ls = 128 * a.steps + 16;
+    a.magic = (uint32_t)((0x100000000ull + a.ls / 16 - 1) / (a.ls / 16));
+    // rows that begin with a line each are stored as they come, 128 or 256 bytes of a row at a time
+    bool lines = Mode != kGatedGrad || a.H * sizeof(T) % 128 == 0;
+    for (int j = 0; j < a.t.n_lists; ++j) {
+        void* const y = Mode == kGatedGrad ? a.dp[j] : a.t.y[j];
+        const int64_t ld = Mode == kGatedGrad ? a.dp_ld[j] : a.t.ld[j];
+        lines = lines && ((uintptr_t)y | (uint64_t)(ld * (int64_t)sizeof(T))) % 128 == 0;
+    }
+    auto with = [&](auto steps) {
+        constexpr int KS = decltype(steps)::value;
+        return lines ? launch_held<T, Mode, KS, true>(ctx, a, done) : launch_held<T, Mode, KS, false>(ctx, a, done);
+    };
+    if (a.steps <= 1) return with(std::integral_constant<int, 1>());
+    if (a.steps <= 2) return with(std::integral_constant<int, 2>());
+    if (a.steps <= 4) return with(std::integral_constant<int, 4>());
+    if (a.steps <= 8) return with(std::integral_constant<int, 8>());
+    return SPP_OK;
+}
+
+template <class T, int Mode>
+static int launch_hidden(spp_ctx* ctx, HiddenArgs& a) {
+    bool done;
+    SPP_TRY((try_held<T, Mode>(ctx, a, &done)));
+    if (done) return SPP_OK;
     auto kernel = hidden_tile_kernel<T, Mode>;
     static LdsLimit limit;
     SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), 2 * kTileBuffer));
