@@ -34,6 +34,9 @@ struct HiddenArgs {
     int32_t        fill;         // workgroups that few rows are dealt out to
     int32_t        w_lds;        // bytes of W; behind them, per wavefront, room for rows on their way:
     int32_t        out_lds;      // bytes
+    // the form that holds W in registers
+    int32_t        blocks;       // workgroups that share a row's columns
+    int32_t        shares;       // and the rows of an XCD; 0: few rows, dealt out to all
 };
 
 // f(0), f(1) .. with the index as a constant.
@@ -131,41 +134,61 @@ template <class Use> __device__ __forceinline__ void with_activation(int act, Us
     else use(std::integral_constant<int, SPP_SIGMOID>());
 }
 
-// Columns h .. h+3 of rows y[0..3], of which `have` are there; others are zeros.
-template <class T>
-__device__ __forceinline__ void get_tile(const T* y, int64_t ld, int have, int h, int H, bool wide, f32x4 (&v)[4]) {
-    typedef typename Elem<T>::v4 V;
+// Columns h .. h+N-1 of rows y[0..3], of which `have` are there: read, others as zeros, and written.  `wide`: N are aligned.
+template <class T, int N>
+__device__ __forceinline__ void get_columns(const T* y, int64_t ld, int have, int h, int H, bool wide, f32x4 (&v)[N]) {
+    typedef T V __attribute__((ext_vector_type(N)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        V x = {(T)0.0f, (T)0.0f, (T)0.0f, (T)0.0f};
+        V x;
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = (T)0.0f;
         const T* from = y + i * ld + h;
         if (i < have) {
-            if (wide && h + 4 <= H) x = *reinterpret_cast<const V*>(from);
-            else if (h + 4 <= H) x = reinterpret_cast<const Loose<V>*>(from)->v;
+            if (wide && h + N <= H) x = *reinterpret_cast<const V*>(from);
+            else if (h + N <= H) x = reinterpret_cast<const Loose<V>*>(from)->v;
             else
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < N; ++k)
                     if (h + k < H) x[k] = from[k];
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k][i] = (float)x[k];
+        for (int k = 0; k < N; ++k) v[k][i] = (float)x[k];
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void put_columns(T* y, int64_t ld, int have, int h, int H, bool wide, const f32x4 (&v)[N]) {
+    typedef T V __attribute__((ext_vector_type(N)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        V x;
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = (T)v[k][i];
+        T* out = y + i * ld + h;
+        if (i >= have) continue;
+        if (wide && h + N <= H) *reinterpret_cast<V*>(out) = x;
+        else if (h + N <= H) reinterpret_cast<Loose<V>*>(out)->v = x;
+        else
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (h + k < H) out[k] = x[k];
     }
 }
 
-// What 64 columns of the two factors become: of the gated layer Y, in `one`; of its gradient dG and dU, in `one` and `two`.
-template <int Mode>
-__device__ __forceinline__ void combine(int act, f32x4 (&one)[4], f32x4 (&two)[4], const f32x4 (&dy)[4]) {
+// What columns of the two factors become: of the gated layer Y, in `one`; of its gradient dG and dU, in `one` and `two`.
+template <int Mode, int N>
+__device__ __forceinline__ void combine(int act, f32x4 (&one)[N], f32x4 (&two)[N], const f32x4 (&dy)[N]) {
     if constexpr (Mode == kGated) {
         with_activation(act, [&](auto kind) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < N; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) one[k][i] = activate<decltype(kind)::value>(one[k][i]) * two[k][i];
         });
     } else if constexpr (Mode == kGatedGrad) {
         with_activation(act, [&](auto kind) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < N; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float f, d;
@@ -194,13 +217,18 @@ struct Results {
             pwide = ((uintptr_t)p | (uint64_t)(pld * (int64_t)sizeof(T)) | (uint64_t)(a.H * (int)sizeof(T))) % (4 * sizeof(T)) == 0;
         }
     }
-    __device__ __forceinline__ void get(const HiddenArgs& a, int64_t row, int have, int h, f32x4 (&v)[4]) const { get_tile<T>(y + row * ld, ld, have, h, a.H, wide, v); }
-    __device__ __forceinline__ void put(const HiddenArgs& a, int64_t row, int have, int h, const f32x4 (&v)[4]) const {
-        if constexpr (Mode == kGatedGrad) put_tile<T>(p + row * pld, pld, have, h, a.H, pwide, v);
-        else put_tile<T>(y + row * ld, ld, have, h, a.H, wide, v);
+    template <int N>
+    __device__ __forceinline__ void get(const HiddenArgs& a, int64_t row, int have, int h, f32x4 (&v)[N]) const {
+        get_columns<T, N>(y + row * ld, ld, have, h, a.H, wide, v);
     }
-    __device__ __forceinline__ void put_second(const HiddenArgs& a, int64_t row, int have, int h, const f32x4 (&v)[4]) const {
-        put_tile<T>(p + row * pld + a.H, pld, have, h, a.H, pwide, v);
+    template <int N>
+    __device__ __forceinline__ void put(const HiddenArgs& a, int64_t row, int have, int h, const f32x4 (&v)[N]) const {
+        if constexpr (Mode == kGatedGrad) put_columns<T, N>(p + row * pld, pld, have, h, a.H, pwide, v);
+        else put_columns<T, N>(y + row * ld, ld, have, h, a.H, wide, v);
+    }
+    template <int N>
+    __device__ __forceinline__ void put_second(const HiddenArgs& a, int64_t row, int have, int h, const f32x4 (&v)[N]) const {
+        put_columns<T, N>(p + row * pld + a.H, pld, have, h, a.H, pwide, v);
     }
 };
 

@@ -307,11 +307,191 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
     return SPP_OK;
 }
 
+// ---- W in registers --------------------------------------------------------------------------------
+
+// The form for weights that LDS does not hold.  A wavefront keeps 64 rows of W in registers (32 of the gate's and the same 32 of the other
+// factor), all columns of them, and a workgroup goes over its share of the rows of X, 32 at a time, which its wavefronts read from LDS:
+// W is read once per workgroup, and per product half as much from LDS as with X in registers and W in LDS.  The workgroups that have the same
+// rows and other columns share an XCD's L2 and take the rows in the same order at the same time.
+template <class T, int Mode, int KS, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, KS > 4 ? 1 : 2) hidden_wide_kernel(HiddenArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    constexpr int RN = 2, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
+    constexpr int kVec = (TB * (8 * KS + 1) + threads - 1) / threads;
+    constexpr bool kExact = sizeof(T) == 4;
+    constexpr int kDepth = KS == 4 || (KS == 8 && (Mode != kProduct || kExact)) ? 1 : 2;         // tiles in registers, as many as there is room for
+    const Lists lists(a.t, TB);
+    const int total = lists.total();
+    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
+    // which columns, which rows
+    int block, at, end, step;
+    if (a.shares > 0) {
+        const int xcd = blockIdx.x & 7, k = (int)blockIdx.x >> 3;
+        block = k % a.blocks;
+        at = (int)((int64_t)total * xcd >> 3) + k / a.blocks;
+        end = (int)((int64_t)total * (xcd + 1) >> 3);
+        step = a.shares;
+    } else {
+        block = (int)blockIdx.x % a.blocks;
+        at = (int)blockIdx.x / a.blocks;
+        end = total;
+        step = (int)gridDim.x / a.blocks;
+    }
+    if (at >= end) return;
+    const int h0 = (block * WAVES + wave) * cols;
+    const int buffer = TB * a.ls;
+    for (int i = threadIdx.x; i < 2 * buffer / 16; i += threads) reinterpret_cast<u32x4*>(lds)[i] = u32x4{0, 0, 0, 0};
+
+    Operand w[KS][4];
+    int held_group = -1;
+    auto hold = [&](int group) {
+        const uint8_t* base = a.w + (int64_t)group * a.H * (Mode == kProduct ? 1 : 2) * a.rb;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            int h = h0 + (Mode == kProduct ? 4 * m + f : 2 * m + (f & 1));
+            h = h < a.H ? h : a.H - 1;
+            const uint8_t* p = base + (int64_t)(Mode != kProduct && f >= 2 ? a.H + h : h) * a.rb;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int lo = 128 * s + 16 * q, hi = lo + 64;
+                const u32x4 x = *reinterpret_cast<const u32x4*>(p + (lo < a.cb ? lo : 0)), y = *reinterpret_cast<const u32x4*>(p + (hi < a.cb ? hi : 0));
+                w[s][f].lo = lo < a.cb ? x : u32x4{0, 0, 0, 0};
+                w[s][f].hi = hi < a.cb ? y : u32x4{0, 0, 0, 0};
+                w[s][f].scale = *reinterpret_cast<const uint32_t*>(p + a.cb + (s < a.steps ? 4 * (s / 4) : 0));
+            }
+        }
+        held_group = group;
+    };
+
+    // X: the thread's vectors of a tile, by row and place; those of the zeros between codes and scales stay as they are
+    const int lv = a.ls / 16;                                 // vectors of a row in LDS
+    uint32_t from[kVec];
+    int row_of[kVec];                                         // or -1
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+        const uint32_t i = k * threads + threadIdx.x, r = __umulhi(i, a.magic), v = i - r * lv;
+        const bool scale = (int)v >= 8 * a.steps;
+        row_of[k] = r < TB && (scale || 16 * (int)v < a.cb) ? (int)r : -1;
+        from[k] = row_of[k] < 0 ? 0 : r * a.rb + (scale ? a.cb + 16 * (v - 8 * a.steps) : 16 * v);
+    }
+    struct Tile { int list, here, group; int64_t r0; };
+    u32x4 ahead[kDepth][kVec];
+    Tile tiles[kDepth];
+    auto find = [&](int tile) {
+        Tile t;
+        t.list = lists.list_of(tile);
+        t.r0 = (int64_t)(tile - lists.first_tile(t.list)) * TB;
+        const int64_t left = lists.rows_in(t.list) - t.r0;
+        t.here = left < TB ? (int)left : TB;
+        t.group = a.t.group[t.list];
+        return t;
+    };
+    // Behind the last tile the last one again.
+    auto ask = [&](int u, int tile) {
+        tiles[u] = find(tile < end ? tile : end - 1);
+        const uint8_t* x = a.t.rows[tiles[u].list] + tiles[u].r0 * a.rb;
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) {
+            const int over = row_of[k] - (tiles[u].here - 1);
+            ahead[u][k] = *reinterpret_cast<const u32x4*>(x + (int64_t)from[k] - (over > 0 ? over * a.rb : 0));
+        }
+    };
+    auto keep = [&](int u, uint8_t* to) {
+#pragma unroll
+        for (int k = 0; k < kVec; ++k)
+            if (row_of[k] >= 0) reinterpret_cast<u32x4*>(to)[k * threads + threadIdx.x] = ahead[u][k];
+    };
+    ask(0, at);
+    hold(tiles[0].group);
+    Tile now = tiles[0];
+    __syncthreads();
+    keep(0, lds);
+    ask(0, at + step);
+    if (kDepth > 1) ask(kDepth - 1, at + 2 * step);
+    for (int tile = at, j = 0; tile < end; tile += 2 * step, j += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (tile + u * step >= end) break;
+            __syncthreads();                                  // this tile is in LDS, and the one before has been read by all
+            if (now.group != held_group) hold(now.group);
+            const uint8_t* x = lds + u * buffer;
+            constexpr int mask = kDepth - 1;
+            const Tile next = tiles[u & mask];
+            keep(u & mask, lds + (u ^ 1) * buffer);
+            ask(u & mask, tile + (u + 1 + kDepth) * step);
+            f32x4 acc[RN][4];
+#pragma unroll
+            for (int c = 0; c < RN; ++c)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+            steps_of<KS>([&](auto index) {
+                constexpr int s = decltype(index)::value;
+                if (s < a.steps) {
+                    Operand xv[RN];
+#pragma unroll
+                    for (int c = 0; c < RN; ++c) {
+                        const uint8_t* p = x + (16 * c + m) * a.ls;
+                        xv[c].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
+                        xv[c].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
+                        xv[c].scale = *reinterpret_cast<const uint32_t*>(p + 128 * a.steps + 4 * (s / 4));
+                    }
+                    multiply<kExact, (s & 3)>(acc, xv, w[s]);
+                }
+            });
+            const Results<T, Mode> out(a, now.list);
+#pragma unroll
+            for (int c = 0; c < RN; ++c) {
+                const int64_t row = now.r0 + 16 * c + 4 * q;
+                const int have = now.here - 16 * c - 4 * q;
+                if constexpr (Mode == kProduct) {
+                    out.put(a, row, have, h0 + 4 * m, acc[c]);
+                } else {
+                    f32x4(&one)[2] = reinterpret_cast<f32x4(&)[2]>(acc[c][0]);
+                    f32x4(&two)[2] = reinterpret_cast<f32x4(&)[2]>(acc[c][2]);
+                    f32x4 dy[2];
+                    if constexpr (Mode == kGatedGrad) out.get(a, row, have, h0 + 2 * m, dy);
+                    combine<Mode>(a.act, one, two, dy);
+                    out.put(a, row, have, h0 + 2 * m, one);
+                    if constexpr (Mode == kGatedGrad) out.put_second(a, row, have, h0 + 2 * m, two);
+                }
+            }
+            now = next;
+        }
+    }
+}
+
+template <class T, int Mode, int KS, int WAVES>
+static int launch_wide(spp_ctx* ctx, HiddenArgs& a) {
+    constexpr int TB = 32, cols = WAVES * (Mode == kProduct ? 64 : 32);
+    auto kernel = hidden_wide_kernel<T, Mode, KS, WAVES>;
+    const int lds = 2 * TB * a.ls;
+    static LdsLimit limit;
+    SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
+    int64_t tiles = 0;
+    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)TB - 1) / TB;
+    a.blocks = (a.H + cols - 1) / cols;
+    const int64_t at_once = ctx->num_cu;
+    a.shares = (int)(at_once / 8 / a.blocks);
+    int64_t grid = (int64_t)a.shares * 8 * a.blocks;
+    if (a.shares == 0 || tiles < 8 * a.shares) {
+        const int64_t fill = at_once / a.blocks < 1 ? 1 : at_once / a.blocks;
+        a.shares = 0;
+        grid = (tiles < fill ? tiles : fill) * a.blocks;
+    }
+    kernel<<<(unsigned)grid, 64 * WAVES, lds, ctx->stream>>>(a);
+    SPP_HIP(hipGetLastError());
+    return SPP_OK;
+}
+
 template <class T, int Mode>
 static int launch_hidden(spp_ctx* ctx, HiddenArgs& a) {
     bool done;
     SPP_TRY((try_held<T, Mode>(ctx, a, &done)));
     if (done) return SPP_OK;
+    if (a.steps <= 2) return launch_wide<T, Mode, 2, 8>(ctx, a);
+    if (a.steps <= 4) return launch_wide<T, Mode, 4, 8>(ctx, a);
+    if (a.steps <= 6) return launch_wide<T, Mode, 6, 4>(ctx, a);
+    if (a.steps <= 8) return launch_wide<T, Mode, 8, 4>(ctx, a);
     auto kernel = hidden_tile_kernel<T, Mode>;
     static LdsLimit limit;
     SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), 2 * kTileBuffer));
