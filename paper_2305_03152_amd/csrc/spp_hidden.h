@@ -29,8 +29,6 @@ struct HiddenArgs {
     int32_t        D, H, rb, cb, steps;  // steps of 128 columns
     int32_t        act;
     // the form that holds W in LDS
-    int32_t        ls;           // bytes of a row of W there: its codes and zeros up to whole steps, then its scales; an odd number of 16
-    uint32_t       magic;        // ceil(2^32 / (ls / 16))
     int32_t        fill;         // workgroups that few rows are dealt out to
     int32_t        w_lds;        // bytes of W; behind them, per wavefront, room for rows on their way:
     int32_t        out_lds;      // bytes
@@ -38,6 +36,9 @@ struct HiddenArgs {
     int32_t        blocks;       // workgroups that share a row's columns
     int32_t        shares;       // and the rows of an XCD; 0: few rows, dealt out to all
 };
+
+// Lane j has list j's group: fetched byte by byte where it is needed, it would make the wavefront wait for all that it has under way.
+__device__ __forceinline__ int group_of_lane(const RowTable& t) { return lane_id() < t.n_lists ? t.group[lane_id()] : 0; }
 
 // f(0), f(1) .. with the index as a constant.
 template <int N, int I = 0, class F>
@@ -105,26 +106,50 @@ __device__ __forceinline__ void sigmoids(float g, float& s, float& r) {
     s = g >= 0.0f ? p : q;
     r = g >= 0.0f ? q : p;
 }
+// The normal distribution function of g, and exp(-g^2 / 2).  Below -x, x = |g|, it is exp(-x^2 / 2) R(x) with R falling from 1/2 to
+// about 0.4 / x: t P(t) with t = 1 / (1 + 0.345 x) and P of degree 8, fitted here for the least relative error over x from 0 to 14, 2.1e-8;
+// behind that the exponential is 0.  In fp32 2^-23 (3 + 0.5 x^2) off, relative (the exponential's argument), at both ends.  The library's
+// erfc takes some four times as long.
+__device__ __forceinline__ float normal(float g, float& e) {
+    const float x = __builtin_fabsf(g);
+    e = __builtin_amdgcn_exp2f(x * x * -0.72134752f);
+    const float t = __builtin_amdgcn_rcpf(__fmaf_rn(0.345f, x, 1.0f));
+    float p = -0.028387917205691338f;
+    p = __fmaf_rn(p, t, 0.14530695974826813f);
+    p = __fmaf_rn(p, t, -0.2712171971797943f);
+    p = __fmaf_rn(p, t, 0.18723931908607483f);
+    p = __fmaf_rn(p, t, -0.03762628510594368f);
+    p = __fmaf_rn(p, t, 0.11180825531482697f);
+    p = __fmaf_rn(p, t, 0.11723647266626358f);
+    p = __fmaf_rn(p, t, 0.1380210965871811f);
+    p = __fmaf_rn(p, t, 0.137619286775589f);
+    const float below = e * (t * p);
+    return g >= 0.0f ? 1.0f - below : below;
+}
 template <int Act> __device__ __forceinline__ float activate(float g) {
     if constexpr (Act == SPP_GELU) {
-        return g * (0.5f * erfcf(g * -0.70710678f));
+        float e;
+        return g * normal(g, e);
+    } else if constexpr (Act == SPP_SILU) {
+        return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));       // an infinite exponential leaves 0
     } else {
         float s, r;
         sigmoids(g, s, r);
-        return Act == SPP_SILU ? g * s : s;
+        return s;
     }
 }
 // act(g) and act'(g)
 template <int Act> __device__ __forceinline__ void activate_both(float g, float& f, float& d) {
     if constexpr (Act == SPP_GELU) {
-        const float p = 0.5f * erfcf(g * -0.70710678f);
+        float e;
+        const float p = normal(g, e);
         f = g * p;
-        d = p + g * (__builtin_amdgcn_exp2f(g * g * -0.72134752f) * 0.39894228f);
+        d = __fmaf_rn(g, e * 0.39894228f, p);
     } else {
         float s, r;
         sigmoids(g, s, r);
         f = Act == SPP_SILU ? g * s : s;
-        d = Act == SPP_SILU ? s * (1.0f + g * r) : s * r;
+        d = Act == SPP_SILU ? s * __fmaf_rn(g, r, 1.0f) : s * r;
     }
 }
 // The activation is the same for the whole call: a branch around a tile's worth of work.

@@ -1,558 +1,7 @@
-#include "spp_hidden.h"
-
-namespace spp {
-
-// A workgroup takes 128 rows of X by 128 columns: of the product, or 64 of the gate's and the same 64 of the other factor.  Steps of 128
-// columns of X and W go through LDS, the next asked for while one is multiplied.
-constexpr int kTileRows = 128, kTileBlock = 256, kTileLd = kFp8Block + 16;
-constexpr int kTileBuffer = 2 * kTileRows * kTileLd + 2 * kTileRows;       // rows of X, rows of W, their scales
-
-template <class T, int Mode>
-__global__ void __launch_bounds__(kTileBlock) hidden_tile_kernel(HiddenArgs a) {
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const Lists lists(a.t, kTileRows);
-    const int total = lists.total();
-    if (total == 0) return;
-    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
-    constexpr int cols = Mode == kProduct ? 128 : 64;
-    const int parts = (a.H + cols - 1) / cols;
-    const Share share((int64_t)total * parts);
-    for (int64_t item = share.at; item < share.end; item += share.step) {
-        const int tile = (int)(item / parts), h0 = (int)(item - (int64_t)tile * parts) * cols;
-        const int list = lists.list_of(tile);
-        const int64_t r0 = (int64_t)(tile - lists.first_tile(list)) * kTileRows;
-        const int64_t left = lists.rows_in(list) - r0;
-        const int here = left < kTileRows ? (int)left : kTileRows;
-        const uint8_t* x = a.t.rows[list] + r0 * a.rb;
-        const uint8_t* w = a.w + (int64_t)a.t.group[list] * a.H * (Mode == kProduct ? 1 : 2) * a.rb;
-        // Row r of the 128 of W: a column of the result.
-        auto w_row = [&](int r) {
-            int h = h0 + (Mode == kProduct ? r : r & 63);
-            h = h < a.H ? h : a.H - 1;
-            return w + (int64_t)(Mode == kProduct || r < 64 ? h : a.H + h) * a.rb;
-        };
-        u32x4 next[8];
-        uint8_t next_scale;
-        auto ask = [&](int s) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = k * kTileBlock + (int)threadIdx.x, r = i >> 3, at = 128 * s + 16 * (i & 7);
-                const bool in = at < a.cb;
-                next[k] = *reinterpret_cast<const u32x4*>(x + (int64_t)(r < here ? r : here - 1) * a.rb + (in ? at : 0));
-                next[4 + k] = *reinterpret_cast<const u32x4*>(w_row(r) + (in ? at : 0));
-                if (!in) next[k] = next[4 + k] = u32x4{0, 0, 0, 0};
-            }
-            const int r = (int)threadIdx.x & 127;
-            next_scale = (threadIdx.x < 128 ? x + (int64_t)(r < here ? r : here - 1) * a.rb : w_row(r))[a.cb + s];
-        };
-        // by operand: columns 4m + f of each 64 as row 16 f + m
-        auto operand = [](int r) { return (r & 64) + (r & 3) * 16 + ((r & 63) >> 2); };
-        auto keep = [&](uint8_t* to) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = k * kTileBlock + (int)threadIdx.x, r = i >> 3, at = 16 * (i & 7);
-                *reinterpret_cast<u32x4*>(to + r * kTileLd + at) = next[k];
-                *reinterpret_cast<u32x4*>(to + (kTileRows + operand(r)) * kTileLd + at) = next[4 + k];
-            }
-            const int r = (int)threadIdx.x & 127;
-            to[2 * kTileRows * kTileLd + (threadIdx.x < 128 ? r : 128 + operand(r))] = next_scale;
-        };
-        f32x4 acc[2][8];
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int f = 0; f < 8; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
-        ask(0);
-        __syncthreads();                                 // the item before has been worked off
-        for (int s = 0; s < a.steps; ++s) {
-            uint8_t* buffer = lds + (s & 1) * kTileBuffer;
-            keep(buffer);
-            if (s + 1 < a.steps) ask(s + 1);
-            __syncthreads();                             // (and the buffer of the step after next has been read by all)
-            const uint8_t* scales = buffer + 2 * kTileRows * kTileLd;
-            auto operand_at = [&](int row) {
-                const uint8_t* p = buffer + row * kTileLd + 16 * q;
-                return Operand{*reinterpret_cast<const u32x4*>(p), *reinterpret_cast<const u32x4*>(p + 64), scales[row]};
-            };
-            Operand xv[2], wv[8];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) xv[c] = operand_at(32 * wave + 16 * c + m);
-#pragma unroll
-            for (int f = 0; f < 8; ++f) wv[f] = operand_at(kTileRows + 16 * f + m);
-            multiply<sizeof(T) == 4, 0>(acc, xv, wv);
-        }
-        const Results<T, Mode> out(a, list);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int row = 32 * wave + 16 * c + 4 * q;
-            f32x4(&one)[4] = reinterpret_cast<f32x4(&)[4]>(acc[c][0]);
-            f32x4(&two)[4] = reinterpret_cast<f32x4(&)[4]>(acc[c][4]);
-            f32x4 dy[4];
-            if constexpr (Mode == kGatedGrad) out.get(a, r0 + row, here - row, h0 + 4 * m, dy);
-            combine<Mode>(a.act, one, two, dy);
-            if constexpr (Mode == kProduct) {
-                out.put(a, r0 + row, here - row, h0 + 4 * m, one);
-                out.put(a, r0 + row, here - row, h0 + 64 + 4 * m, two);
-            } else {
-                out.put(a, r0 + row, here - row, h0 + 4 * m, one);
-                if constexpr (Mode == kGatedGrad) out.put_second(a, r0 + row, here - row, h0 + 4 * m, two);
-            }
-        }
-    }
-}
-
-// ---- W in LDS --------------------------------------------------------------------------------------
-
-// The form for weights that LDS holds.  A wavefront keeps its 16 RN rows of X in registers, all columns of them, and goes over the columns of
-// the result 64 at a time (64 of the gate's and the same 64 of the other factor); a workgroup's wavefronts share W and wait for each other only
-// where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.
-constexpr int kHeldWaves = 8, kHeldBlock = 64 * kHeldWaves;
-template <class T, int Mode, int KS, int RN, bool Lines>
-__global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    constexpr int TB = kHeldWaves * 16 * RN, MR = Mode == kProduct ? 64 : 128;       // rows of X per workgroup, rows of W per 64 columns
-    constexpr bool kAhead = KS * RN <= 4, kExact = sizeof(T) == 4;
-    const Lists lists(a.t, TB);
-    const int total = lists.total();
-    if (total == 0) return;
-    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
-    const int ht = (a.H + 63) / 64;
-    int parts = a.fill / total;                        // few rows: the columns of the result are dealt out too
-    parts = parts < 1 ? 1 : parts > ht ? ht : parts;
-    const int64_t items = (int64_t)total * parts;
-    int held_group = -1, held_from = -1;
-    struct Item { int part, list, here, group; int64_t r0; };
-    auto find = [&](int64_t item) {
-        Item it;
-        it.part = (int)(item / total);
-        const int tile = (int)(item - (int64_t)it.part * total);
-        it.list = lists.list_of(tile);
-        it.r0 = (int64_t)(tile - lists.first_tile(it.list)) * TB;
-        const int64_t left = lists.rows_in(it.list) - it.r0;
-        it.here = left < TB ? (int)left : TB;
-        it.group = a.t.group[it.list];
-        return it;
-    };
-    u32x4 ahead[KS][RN][2];
-    uint32_t ahead_scale[(KS + 3) / 4][RN];
-    auto ask_rows = [&](const Item& it) {
-        const uint8_t* x = a.t.rows[it.list] + it.r0 * a.rb;
-#pragma unroll
-        for (int c = 0; c < RN; ++c) {
-            const int row = (wave * RN + c) * 16 + m;
-            const uint8_t* p = x + (int64_t)(row < it.here ? row : it.here - 1) * a.rb;
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = 128 * s + 64 * k + 16 * q;
-                    ahead[s][c][k] = *reinterpret_cast<const u32x4*>(p + (at < a.cb ? at : 0));
-                }
-#pragma unroll
-            for (int s = 0; s < (KS + 3) / 4; ++s) ahead_scale[s][c] = *reinterpret_cast<const uint32_t*>(p + a.cb + (4 * s < a.steps ? 4 * s : 0));
-        }
-    };
-    const Share share(items);
-    if (share.at >= share.end) return;
-    Item it = find(share.at);
-    if (kAhead) ask_rows(it);
-    for (int64_t item = share.at; item < share.end; item += share.step) {
-        if (!kAhead) { it = find(item); ask_rows(it); }
-        const int t0 = (int)((int64_t)it.part * ht / parts), t1 = (int)((int64_t)(it.part + 1) * ht / parts);
-        const int list = it.list, here = it.here, group = it.group, mine = here - wave * 16 * RN;       // rows of the workgroup, of the wavefront
-        const int64_t r0 = it.r0 + wave * 16 * RN;
-        if (group != held_group || t0 != held_from) {
-            const uint8_t* w = a.w + (int64_t)group * a.H * (MR / 64) * a.rb;
-            const uint32_t lv = (uint32_t)a.ls / 16, all = (uint32_t)(t1 - t0) * MR * lv;
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < all; i += kHeldBlock) {
-                const uint32_t r = __umulhi(i, a.magic), v = i - r * lv;             // LDS row: by operand, columns 4m + f of 64 as row 16 f + m
-                int h = 64 * (t0 + (int)(r / MR)) + 4 * (int)(r & 15) + (int)(r >> 4 & 3);
-                h = h < a.H ? h : a.H - 1;
-                const uint8_t* from = w + (int64_t)(MR == 128 && (r & 64) ? a.H + h : h) * a.rb;
-                const int at = v == lv - 1 ? a.cb : 16 * (int)v;
-                const u32x4 x = *reinterpret_cast<const u32x4*>(from + (v == lv - 1 || at < a.cb ? at : 0));
-                reinterpret_cast<u32x4*>(lds)[i] = v == lv - 1 || at < a.cb ? x : u32x4{0, 0, 0, 0};
-            }
-            held_group = group; held_from = t0;
-            __syncthreads();
-        }
-        Operand x[KS][RN];
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int c = 0; c < RN; ++c) {
-                const int at = 128 * s + 16 * q;
-                x[s][c].lo = at < a.cb ? ahead[s][c][0] : u32x4{0, 0, 0, 0};
-                x[s][c].hi = at + 64 < a.cb ? ahead[s][c][1] : u32x4{0, 0, 0, 0};
-                x[s][c].scale = ahead_scale[s / 4][c];
-            }
-        if (kAhead && item + share.step < share.end) { it = find(item + share.step); ask_rows(it); }
-        if (mine <= 0) continue;
-        const Results<T, Mode> res(a, list);
-        T* const y = (Mode == kGatedGrad ? res.p : res.y);
-        const int64_t ld = Mode == kGatedGrad ? res.pld : res.ld;
-        constexpr int kOuts = Mode == kGatedGrad ? 2 : 1;
-        RowsOut<T, RN> out[kOuts];
-        if constexpr (!Lines) {
-#pragma unroll
-            for (int k = 0; k < kOuts; ++k) {
-                out[k].lds = lds + a.w_lds + (wave * kOuts + k) * a.out_lds;
-                out[k].rows = mine < 16 * RN ? mine : 16 * RN;
-                out[k].step = ld * (int64_t)sizeof(T);
-                out[k].y = reinterpret_cast<char*>(y + r0 * ld + k * a.H + 64 * t0);
-                out[k].bytes = ((64 * t1 < a.H ? 64 * t1 : a.H) - 64 * t0) * (int)sizeof(T);
-                out[k].run = kOuts == 1 && out[k].bytes == out[k].step && 16 * RN * out[k].bytes + 16 <= a.out_lds;
-                out[k].begin();
-            }
-        }
-        for (int t = t0; t < t1; ++t) {
-            const uint8_t* tile_w = lds + (t - t0) * MR * a.ls;
-            const bool whole = mine >= 16 * RN && 64 * t + 64 <= a.H;
-            f32x4 dy[RN][4];
-            if constexpr (Mode == kGatedGrad) {
-#pragma unroll
-                for (int c = 0; c < RN; ++c) res.get(a, r0 + 16 * c + 4 * q, mine - 16 * c - 4 * q, 64 * t + 4 * m, dy[c]);
-            }
-            f32x4 acc[MR / 64][RN][4];
-#pragma unroll
-            for (int k = 0; k < MR / 64; ++k) {
-#pragma unroll
-                for (int c = 0; c < RN; ++c)
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) acc[k][c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
-                steps_of<KS>([&](auto step) {
-                    constexpr int s = decltype(step)::value;
-                    if (s < a.steps) {
-                        Operand w[4];
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) {
-                            const uint8_t* p = tile_w + (64 * k + 16 * f + m) * a.ls;
-                            w[f].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
-                            w[f].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
-                            w[f].scale = *reinterpret_cast<const uint32_t*>(p + 128 * a.steps + 4 * (s / 4));
-                        }
-                        multiply<kExact, (s & 3)>(acc[k], x[s], w);
-                    }
-                });
-            }
-#pragma unroll
-            for (int c = 0; c < RN; ++c) combine<Mode>(a.act, acc[0][c], acc[MR / 64 - 1][c], dy[c]);
-            if constexpr (Lines) {
-#pragma unroll
-                for (int k = 0; k < kOuts; ++k)
-#pragma unroll
-                    for (int c = 0; c < RN; ++c) {
-                        T* at = y + (r0 + 16 * c + 4 * q) * ld + k * a.H;
-                        if (whole) put_whole<T>(at + 64 * t + 4 * m, ld, acc[k][c]);
-                        else put_tile<T>(at, ld, mine - 16 * c - 4 * q, 64 * t + 4 * m, a.H, true, acc[k][c]);
-                    }
-            } else {
-#pragma unroll
-                for (int k = 0; k < kOuts; ++k) {
-                    out[k].put(t - t0, acc[k]);
-                    if (!out[k].run) out[k].flush_lines(t - t0, t == t0, t + 1 == t1);
-                    else if (t + 1 == t1) out[k].flush_run();
-                }
-            }
-        }
-    }
-}
-
-constexpr int kHeldLds = 163840;         // all of a CU's
-constexpr int kHeldRowOut = 768;         // bytes of rows that go out in one run
-template <class T, int Mode, int KS, bool Lines>
-static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
-    constexpr int RN = KS <= 2 && Lines ? 2 : 1, MR = Mode == kProduct ? 64 : 128, TB = kHeldWaves * 16 * RN, outs = Mode == kGatedGrad ? 2 : 1;
-    auto kernel = hidden_held_kernel<T, Mode, KS, RN, Lines>;
-    const int ht = (a.H + 63) / 64, row = a.H * (int)sizeof(T);
-    a.out_lds = Lines ? 0 : 16 * RN * RowsOut<T, RN>::kPitch;
-    if (!Lines && outs == 1 && row <= kHeldRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
-    const int64_t need = (int64_t)ht * MR * a.ls, most_lds = kHeldLds - (int64_t)kHeldWaves * outs * a.out_lds;
-    *done = need <= most_lds;
-    if (!*done) return SPP_OK;
-    a.w_lds = (int)need;
-    const int lds = a.w_lds + kHeldWaves * outs * a.out_lds;
-    static LdsLimit limit;
-    SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
-    int64_t tiles = 0;
-    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)TB - 1) / TB;
-    a.fill = ctx->num_cu;
-    const int fit = kHeldLds / lds, per_cu = fit < 1 ? 1 : fit > 2 ? 2 : fit;
-    const int64_t want = tiles >= a.fill ? tiles : tiles * ht < a.fill ? tiles * ht : a.fill, most = (int64_t)ctx->num_cu * per_cu;
-    kernel<<<(unsigned)(want < most ? want : most), kHeldBlock, lds, ctx->stream>>>(a);
-    SPP_HIP(hipGetLastError());
-    return SPP_OK;
-}
-template <class T, int Mode>
-static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
-    *done = false;
-    a.ls = 128 * a.steps + 16;
-    a.magic = (uint32_t)((0x100000000ull + a.ls / 16 - 1) / (a.ls / 16));
-    // rows that begin with a line each are stored as they come, 128 or 256 bytes of a row at a time
-    bool lines = Mode != kGatedGrad || a.H * sizeof(T) % 128 == 0;
-    for (int j = 0; j < a.t.n_lists; ++j) {
-        void* const y = Mode == kGatedGrad ? a.dp[j] : a.t.y[j];
-        const int64_t ld = Mode == kGatedGrad ? a.dp_ld[j] : a.t.ld[j];
-        lines = lines && ((uintptr_t)y | (uint64_t)(ld * (int64_t)sizeof(T))) % 128 == 0;
-    }
-    auto with = [&](auto steps) {
-        constexpr int KS = decltype(steps)::value;
-        return lines ? launch_held<T, Mode, KS, true>(ctx, a, done) : launch_held<T, Mode, KS, false>(ctx, a, done);
-    };
-    if (a.steps <= 1) return with(std::integral_constant<int, 1>());
-    if (a.steps <= 2) return with(std::integral_constant<int, 2>());
-    if (a.steps <= 4) return with(std::integral_constant<int, 4>());
-    if (a.steps <= 8) return with(std::integral_constant<int, 8>());
-    return SPP_OK;
-}
-
-// ---- W in registers --------------------------------------------------------------------------------
-
-// The form for weights that LDS does not hold.  A wavefront keeps 64 rows of W in registers (32 of the gate's and the same 32 of the other
-// factor), all columns of them, and a workgroup goes over its share of the rows of X, 32 at a time, which its wavefronts read from LDS:
-// W is read once per workgroup, and per product half as much from LDS as with X in registers and W in LDS.  The workgroups that have the same
-// rows and other columns share an XCD's L2 and take the rows in the same order at the same time.
-template <class T, int Mode, int KS, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, KS > 4 ? 1 : 2) hidden_wide_kernel(HiddenArgs a) {
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    constexpr int RN = 2, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
-    constexpr int kVec = (TB * (8 * KS + 1) + threads - 1) / threads;
-    constexpr bool kExact = sizeof(T) == 4;
-    constexpr int kDepth = KS == 4 || (KS == 8 && (Mode != kProduct || kExact)) ? 1 : 2;         // tiles in registers, as many as there is room for
-    const Lists lists(a.t, TB);
-    const int total = lists.total();
-    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
-    // which columns, which rows
-    int block, at, end, step;
-    if (a.shares > 0) {
-        const int xcd = blockIdx.x & 7, k = (int)blockIdx.x >> 3;
-        block = k % a.blocks;
-        at = (int)((int64_t)total * xcd >> 3) + k / a.blocks;
-        end = (int)((int64_t)total * (xcd + 1) >> 3);
-        step = a.shares;
-    } else {
-        block = (int)blockIdx.x % a.blocks;
-        at = (int)blockIdx.x / a.blocks;
-        end = total;
-        step = (int)gridDim.x / a.blocks;
-    }
-    if (at >= end) return;
-    const int h0 = (block * WAVES + wave) * cols;
-    const int buffer = TB * a.ls;
-    for (int i = threadIdx.x; i < 2 * buffer / 16; i += threads) reinterpret_cast<u32x4*>(lds)[i] = u32x4{0, 0, 0, 0};
-
-    Operand w[KS][4];
-    int held_group = -1;
-    auto hold = [&](int group) {
-        const uint8_t* base = a.w + (int64_t)group * a.H * (Mode == kProduct ? 1 : 2) * a.rb;
-#pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            int h = h0 + (Mode == kProduct ? 4 * m + f : 2 * m + (f & 1));
-            h = h < a.H ? h : a.H - 1;
-            const uint8_t* p = base + (int64_t)(Mode != kProduct && f >= 2 ? a.H + h : h) * a.rb;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int lo = 128 * s + 16 * q, hi = lo + 64;
-                const u32x4 x = *reinterpret_cast<const u32x4*>(p + (lo < a.cb ? lo : 0)), y = *reinterpret_cast<const u32x4*>(p + (hi < a.cb ? hi : 0));
-                w[s][f].lo = lo < a.cb ? x : u32x4{0, 0, 0, 0};
-                w[s][f].hi = hi < a.cb ? y : u32x4{0, 0, 0, 0};
-                w[s][f].scale = *reinterpret_cast<const uint32_t*>(p + a.cb + (s < a.steps ? 4 * (s / 4) : 0));
-            }
-        }
-        held_group = group;
-    };
-
-    // X: the thread's vectors of a tile, by row and place; those of the zeros between codes and scales stay as they are
-    const int lv = a.ls / 16;                                 // vectors of a row in LDS
-    uint32_t from[kVec];
-    int row_of[kVec];                                         // or -1
-#pragma unroll
-    for (int k = 0; k < kVec; ++k) {
-        const uint32_t i = k * threads + threadIdx.x, r = __umulhi(i, a.magic), v = i - r * lv;
-        const bool scale = (int)v >= 8 * a.steps;
-        row_of[k] = r < TB && (scale || 16 * (int)v < a.cb) ? (int)r : -1;
-        from[k] = row_of[k] < 0 ? 0 : r * a.rb + (scale ? a.cb + 16 * (v - 8 * a.steps) : 16 * v);
-    }
-    struct Tile { int list, here, group; int64_t r0; };
-    u32x4 ahead[kDepth][kVec];
-    Tile tiles[kDepth];
-    auto find = [&](int tile) {
-        Tile t;
-        t.list = lists.list_of(tile);
-        t.r0 = (int64_t)(tile - lists.first_tile(t.list)) * TB;
-        const int64_t left = lists.rows_in(t.list) - t.r0;
-        t.here = left < TB ? (int)left : TB;
-        t.group = a.t.group[t.list];
-        return t;
-    };
-    // Behind the last tile the last one again.
-    auto ask = [&](int u, int tile) {
-        tiles[u] = find(tile < end ? tile : end - 1);
-        const uint8_t* x = a.t.rows[tiles[u].list] + tiles[u].r0 * a.rb;
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) {
-            const int over = row_of[k] - (tiles[u].here - 1);
-            ahead[u][k] = *reinterpret_cast<const u32x4*>(x + (int64_t)from[k] - (over > 0 ? over * a.rb : 0));
-        }
-    };
-    auto keep = [&](int u, uint8_t* to) {
-#pragma unroll
-        for (int k = 0; k < kVec; ++k)
-            if (row_of[k] >= 0) reinterpret_cast<u32x4*>(to)[k * threads + threadIdx.x] = ahead[u][k];
-    };
-    ask(0, at);
-    hold(tiles[0].group);
-    Tile now = tiles[0];
-    __syncthreads();
-    keep(0, lds);
-    ask(0, at + step);
-    if (kDepth > 1) ask(kDepth - 1, at + 2 * step);
-    for (int tile = at, j = 0; tile < end; tile += 2 * step, j += 2) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (tile + u * step >= end) break;
-            __syncthreads();                                  // this tile is in LDS, and the one before has been read by all
-            if (now.group != held_group) hold(now.group);
-            const uint8_t* x = lds + u * buffer;
-            constexpr int mask = kDepth - 1;
-            const Tile next = tiles[u & mask];
-            keep(u & mask, lds + (u ^ 1) * buffer);
-            ask(u & mask, tile + (u + 1 + kDepth) * step);
-            f32x4 acc[RN][4];
-#pragma unroll
-            for (int c = 0; c < RN; ++c)
-#pragma unroll
-                for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
-            steps_of<KS>([&](auto index) {
-                constexpr int s = decltype(index)::value;
-                if (s < a.steps) {
-                    Operand xv[RN];
-#pragma unroll
-                    for (int c = 0; c < RN; ++c) {
-                        const uint8_t* p = x + (16 * c + m) * a.ls;
-                        xv[c].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
-                        xv[c].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
-                        xv[c].scale = *reinterpret_cast<const uint32_t*>(p + 128 * a.steps + 4 * (s / 4));
-                    }
-                    multiply<kExact, (s & 3)>(acc, xv, w[s]);
-                }
-            });
-            const Results<T, Mode> out(a, now.list);
-#pragma unroll
-            for (int c = 0; c < RN; ++c) {
-                const int64_t row = now.r0 + 16 * c + 4 * q;
-                const int have = now.here - 16 * c - 4 * q;
-                if constexpr (Mode == kProduct) {
-                    out.put(a, row, have, h0 + 4 * m, acc[c]);
-                } else {
-                    f32x4(&one)[2] = reinterpret_cast<f32x4(&)[2]>(acc[c][0]);
-                    f32x4(&two)[2] = reinterpret_cast<f32x4(&)[2]>(acc[c][2]);
-                    f32x4 dy[2];
-                    if constexpr (Mode == kGatedGrad) out.get(a, row, have, h0 + 2 * m, dy);
-                    combine<Mode>(a.act, one, two, dy);
-                    out.put(a, row, have, h0 + 2 * m, one);
-                    if constexpr (Mode == kGatedGrad) out.put_second(a, row, have, h0 + 2 * m, two);
-                }
-            }
-            now = next;
-        }
-    }
-}
-
-template <class T, int Mode, int KS, int WAVES>
-static int launch_wide(spp_ctx* ctx, HiddenArgs& a) {
-    constexpr int TB = 32, cols = WAVES * (Mode == kProduct ? 64 : 32);
-    auto kernel = hidden_wide_kernel<T, Mode, KS, WAVES>;
-    const int lds = 2 * TB * a.ls;
-    static LdsLimit limit;
-    SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
-    int64_t tiles = 0;
-    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)TB - 1) / TB;
-    a.blocks = (a.H + cols - 1) / cols;
-    const int64_t at_once = ctx->num_cu;
-    a.shares = (int)(at_once / 8 / a.blocks);
-    int64_t grid = (int64_t)a.shares * 8 * a.blocks;
-    if (a.shares == 0 || tiles < 8 * a.shares) {
-        const int64_t fill = at_once / a.blocks < 1 ? 1 : at_once / a.blocks;
-        a.shares = 0;
-        grid = (tiles < fill ? tiles : fill) * a.blocks;
-    }
-    kernel<<<(unsigned)grid, 64 * WAVES, lds, ctx->stream>>>(a);
-    SPP_HIP(hipGetLastError());
-    return SPP_OK;
-}
-
-template <class T, int Mode>
-static int launch_hidden(spp_ctx* ctx, HiddenArgs& a) {
-    bool done;
-    SPP_TRY((try_held<T, Mode>(ctx, a, &done)));
-    if (done) return SPP_OK;
-    if (a.steps <= 2) return launch_wide<T, Mode, 2, 8>(ctx, a);
-    if (a.steps <= 4) return launch_wide<T, Mode, 4, 8>(ctx, a);
-    if (a.steps <= 6) return launch_wide<T, Mode, 6, 4>(ctx, a);
-    if (a.steps <= 8) return launch_wide<T, Mode, 8, 4>(ctx, a);
-    auto kernel = hidden_tile_kernel<T, Mode>;
-    static LdsLimit limit;
-    SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), 2 * kTileBuffer));
-    int64_t tiles = 0;
-    for (int j = 0; j < a.t.n_lists; ++j) tiles += (a.t.n[j] + (int64_t)kTileRows - 1) / kTileRows;
-    constexpr int cols = Mode == kProduct ? 128 : 64;
-    const int64_t want = tiles * ((a.H + cols - 1) / cols), most = (int64_t)ctx->num_cu * 64;
-    kernel<<<(unsigned)(want < most ? want : most), kTileBlock, 2 * kTileBuffer, ctx->stream>>>(a);
-    SPP_HIP(hipGetLastError());
-    return SPP_OK;
-}
-
-// The checks of the three entries, and the launch.
-template <int Mode>
-static int hidden(const char* who, spp_ctx* ctx, const spp_row_list* lists, const spp_row_list* grads, int32_t n_lists, const void* d_weights,
-                  int32_t n_groups, int32_t D, int32_t H, int32_t type, int32_t activation, uint32_t flags) {
-    SPP_CHECK(ctx && d_weights, SPP_E_ARG, "%s: null argument", who);
-    SPP_CHECK((uintptr_t)d_weights % 16 == 0, SPP_E_ARG, "%s: weights must be 16-byte aligned", who);
-    HiddenArgs a;
-    memset(&a, 0, sizeof(a));
-    int64_t most = 0;
-    SPP_TRY(row_table(who, lists, n_lists, n_groups, D, H, type, a.t, &most));
-    if (Mode != kProduct) {
-        SPP_CHECK(H <= SPP_MAX_HIDDEN / 2, SPP_E_ARG, "%s: H = %d (1 .. %d)", who, H, SPP_MAX_HIDDEN / 2);
-        SPP_CHECK(activation == SPP_SILU || activation == SPP_GELU || activation == SPP_SIGMOID, SPP_E_ARG, "%s: activation %d", who, activation);
-    }
-    if (Mode == kGatedGrad) {
-        RowTable p;
-        int64_t also = 0;
-        SPP_CHECK(grads || n_lists == 0, SPP_E_ARG, "%s: null argument", who);
-        SPP_TRY(row_table(who, grads, n_lists, n_groups, D, 2 * H, type, p, &also));
-        for (int j = 0; j < n_lists; ++j)
-            SPP_CHECK(lists[j].d_rows == grads[j].d_rows && lists[j].n == grads[j].n && lists[j].d_n == grads[j].d_n && lists[j].group == grads[j].group,
-                      SPP_E_ARG, "%s: list %d: the gradient's rows, count or group are not the list's", who, j);
-        for (int j = 0; j < n_lists; ++j) { a.dp[j] = p.y[j]; a.dp_ld[j] = p.ld[j]; }
-    }
-    if (most > 0) {
-        a.w = static_cast<const uint8_t*>(d_weights);
-        a.D = D; a.H = H; a.rb = fp8_bytes(D); a.cb = fp8_code_bytes(D); a.steps = fp8_blocks(D); a.act = activation;
-        SPP_HIP(hipSetDevice(ctx->device));
-        ScopedTimer timer(ctx, SPP_T_LAYER, ctx->stream);
-        SPP_TRY(type == SPP_F32 ? (launch_hidden<float, Mode>(ctx, a)) : type == SPP_F16 ? (launch_hidden<_Float16, Mode>(ctx, a))
-                                                                                          : (launch_hidden<__bf16, Mode>(ctx, a)));
-    }
-    if (flags & SPP_SYNC) SPP_HIP(hipStreamSynchronize(ctx->stream));
-    return SPP_OK;
-}
-
-}  // namespace spp
+// The product of hidden rows in 8 bits with weights in the same format.
+#include "spp_hidden_kernels.h"
 
 extern "C" int spp_fp8_product(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
                                int32_t D, int32_t H, int32_t type, uint32_t flags) {
     return spp::hidden<spp::kProduct>("spp_fp8_product", ctx, lists, nullptr, n_lists, d_weights, n_groups, D, H, type, 0, flags);
-}
-
-extern "C" int spp_fp8_gated(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
-                             int32_t D, int32_t H, int32_t type, int32_t activation, uint32_t flags) {
-    return spp::hidden<spp::kGated>("spp_fp8_gated", ctx, lists, nullptr, n_lists, d_weights, n_groups, D, H, type, activation, flags);
-}
-
-extern "C" int spp_fp8_gated_grad(spp_ctx* ctx, const spp_row_list* lists, const spp_row_list* grads, int32_t n_lists, const void* d_weights,
-                                  int32_t n_groups, int32_t D, int32_t H, int32_t type, int32_t activation, uint32_t flags) {
-    return spp::hidden<spp::kGatedGrad>("spp_fp8_gated_grad", ctx, lists, grads, n_lists, d_weights, n_groups, D, H, type, activation, flags);
 }
