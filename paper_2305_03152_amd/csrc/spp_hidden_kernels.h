@@ -5,9 +5,16 @@
 
 namespace spp {
 
-// A workgroup takes 128 rows of X by 128 columns: of the product, or 64 of the gate's and the same 64 of the other factor.  Steps of 128
+// Bytes behind a row in LDS, its scales among them.  The wavefront reads 16 bytes of 16 rows and four places each, eight lanes at a time and of these
+// half from one place and half from the next: rows an even number of 16 bytes apart, but not of 32, put them in banks of their own (16
+// bytes behind a row each read took twice its time).
+constexpr int kLdsPad = 32;
+
+// ---- W and X in LDS --------------------------------------------------------------------------------
+
+// The form for rows of any length.  A workgroup takes 128 rows of X by 128 columns: of the product, or 64 of the gate's and the same 64 of the other factor.  Steps of 128
 // columns of X and W go through LDS, the next asked for while one is multiplied.
-constexpr int kTileRows = 128, kTileBlock = 256, kTileLd = kFp8Block + 16;
+constexpr int kTileRows = 128, kTileBlock = 256, kTileLd = kFp8Block + kLdsPad;
 constexpr int kTileBuffer = 2 * kTileRows * kTileLd + 2 * kTileRows;       // rows of X, rows of W, their scales
 
 template <class T, int Mode>
@@ -114,7 +121,7 @@ template <class T, int Mode, int KS, int RN, bool Lines>
 __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int TB = kHeldWaves * 16 * RN, MR = Mode == kProduct ? 64 : 128;       // rows of X per workgroup, rows of W per 64 columns
-    constexpr int kLs = 128 * KS + 16;                 // bytes of a row of W in LDS: codes, zeros up to whole steps, scales; an odd number of 16
+    constexpr int kLs = 128 * KS + kLdsPad;            // bytes of a row of W in LDS: codes, zeros up to whole steps, scales
     constexpr bool kAhead = KS * RN <= 4, kExact = sizeof(T) == 4, kDirect = !Lines && Mode == kGatedGrad;
     const Lists lists(a.t, TB);
     const int total = lists.total(), groups = group_of_lane(a.t);
@@ -180,9 +187,9 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
                     int h = 64 * (t0 + (int)(r / MR)) + 4 * (int)(r & 15) + (int)(r >> 4 & 3);
                     h = h < a.H ? h : a.H - 1;
                     const uint8_t* from = w + (int64_t)(MR == 128 && (r & 64) ? a.H + h : h) * a.rb;
-                    const int at = c == lv - 1 ? a.cb : 16 * (int)c;
-                    v[k] = *reinterpret_cast<const u32x4*>(from + (c == lv - 1 || at < a.cb ? at : 0));
-                    if (c < lv - 1 && at >= a.cb) v[k] = u32x4{0, 0, 0, 0};
+                    const int at = c >= 8 * KS ? a.cb : 16 * (int)c;
+                    v[k] = *reinterpret_cast<const u32x4*>(from + (c >= 8 * KS || at < a.cb ? at : 0));
+                    if (c < 8 * KS && at >= a.cb) v[k] = u32x4{0, 0, 0, 0};
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
@@ -286,7 +293,7 @@ static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
     const int ht = (a.H + 63) / 64, row = a.H * (int)sizeof(T);
     a.out_lds = Lines || Mode == kGatedGrad ? 0 : 16 * RN * RowsOut<T, RN>::kPitch;
     if (!Lines && Mode != kGatedGrad && row <= kHeldRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
-    const int64_t need = (int64_t)ht * MR * (128 * KS + 16), most_lds = kHeldLds - (int64_t)kHeldWaves * a.out_lds;
+    const int64_t need = (int64_t)ht * MR * (128 * KS + kLdsPad), most_lds = kHeldLds - (int64_t)kHeldWaves * a.out_lds;
     *done = need <= most_lds;
     if (!*done) return SPP_OK;
     a.w_lds = (int)need;
@@ -335,7 +342,7 @@ template <class T, int Mode, int KS, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, KS > 4 ? 1 : 2) hidden_wide_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int RN = 2, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
-    constexpr int kLs = 128 * KS + 16, lv = kLs / 16;         // bytes and vectors of a row of X in LDS: codes, zeros up to whole steps, scales
+    constexpr int kLs = 128 * KS + kLdsPad, lv = kLs / 16;         // bytes and vectors of a row of X in LDS: codes, zeros up to whole steps, scales
     constexpr int kVec = (TB * lv + threads - 1) / threads;
     constexpr bool kExact = sizeof(T) == 4;
     constexpr int kDepth = KS >= 4 ? 1 : 2;         // tiles in registers, as many as there is room for
@@ -389,7 +396,7 @@ __global__ void __launch_bounds__(64 * WAVES, KS > 4 ? 1 : 2) hidden_wide_kernel
     for (int k = 0; k < kVec; ++k) {
         const uint32_t i = k * threads + threadIdx.x, r = i / lv, v = i - r * lv;
         const bool scale = v == 8 * KS;
-        row_of[k] = r < TB && (scale || 16 * (int)v < a.cb) ? (int)r : -1;
+        row_of[k] = r < TB && (scale || (v < 8 * KS && 16 * (int)v < a.cb)) ? (int)r : -1;
         from[k] = row_of[k] < 0 ? 0 : r * a.rb + (scale ? a.cb : 16 * v);
     }
     struct Tile { int list, here, group; int64_t r0; };
@@ -489,7 +496,7 @@ template <class T, int Mode, int KS, int WAVES>
 static int launch_wide(spp_ctx* ctx, HiddenArgs& a) {
     constexpr int TB = 32, cols = WAVES * (Mode == kProduct ? 64 : 32);
     auto kernel = hidden_wide_kernel<T, Mode, KS, WAVES>;
-    constexpr int lds = 2 * TB * (128 * KS + 16);
+    constexpr int lds = 2 * TB * (128 * KS + kLdsPad);
     static LdsLimit limit;
     SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), lds));
     int64_t tiles = 0;
