@@ -453,7 +453,9 @@ static int grad_shape(const GradArgs& a, Use use) {
         return h > 64 ? use(GradShape<F, T, 2, 4, 4>()) : use(GradShape<F, T, 1, 4, 4>());
     }
     if (a.D > 64) {
-        if (h > 128) return h > 192 ? use(GradShape<F, T, 4, 2, 4>()) : use(GradShape<F, T, 3, 2, 4>());
+        // (six wavefronts: of 16-column pieces and one product the registers would not hold the chunks ahead)
+        if constexpr (F::columns == 16 && Pieces<T>::n == 1) { if (h > 128) return use(GradShape<F, T, 4, 2, 4>()); }
+        else if (h > 128) return h > 192 ? use(GradShape<F, T, 4, 2, 4>()) : use(GradShape<F, T, 3, 2, 4>());
         return h > 64 ? use(GradShape<F, T, 2, 2, 4>()) : use(GradShape<F, T, 1, 2, 4>());
     }
     if (h > 128) return h > 192 ? use(GradShape<F, T, 4, 1, 4>()) : use(GradShape<F, T, 3, 1, 4>());

@@ -225,6 +225,93 @@ __device__ __forceinline__ void combine(int act, f32x4 (&one)[N], f32x4 (&two)[N
     }
 }
 
+// A buffer that begins with a tile's first row, of `bytes` bytes: what is read behind them is 0, what is written there is dropped, so that a
+// tile of fewer rows takes the same path as any other, and without a branch.
+__device__ __forceinline__ auto rows_buffer(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
+}
+constexpr uint32_t kNowhere = 0x80000000u;       // an offset behind every buffer
+constexpr int kPastL2 = 2;                       // a store that is not kept in the L2
+template <int Kind, class V>
+__device__ __forceinline__ void buffer_store(V v, __amdgpu_buffer_rsrc_t to, uint32_t at) {
+    if constexpr (sizeof(V) == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, (int)at, 0, Kind);
+    else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), to, (int)at, 0, Kind);
+    else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), to, (int)at, 0, Kind);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), to, (int)at, 0, Kind);
+}
+template <class V>
+__device__ __forceinline__ V buffer_load(__amdgpu_buffer_rsrc_t from, uint32_t at) {
+    if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0));
+    else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(from, (int)at, 0, 0));
+    else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(from, (int)at, 0, 0));
+    else return __builtin_bit_cast(V, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, (int)at, 0, 0));
+}
+
+// A tile of a matrix of results by way of such a buffer: 16 RN rows, of which `here` are there, and of each N columns from h0 + N m on.
+// Whole vectors where these are aligned and end with the row or before, else element by element.  All of it is branches that a whole
+// wavefront takes: where a kernel's values fill the registers the compiler (of ROCm 7.2) has copied some of them at the end of a masked
+// piece of code before it restored the mask, and the lanes that were masked out lost theirs.
+template <class T, int RN, int N>
+struct Tile {
+    typedef T V __attribute__((ext_vector_type(N)));
+    __amdgpu_buffer_rsrc_t at;
+    uint32_t step;               // bytes from a row to the next
+    int      h, H;
+    bool     whole;
+    uint32_t first;              // the lane's first element
+    // `front`: columns of the matrix before these `columns`; a row has `all`
+    __device__ __forceinline__ Tile(const T* y, int64_t ld, int64_t r0, int here, int h0, int front, int columns, int all) {
+        step = (uint32_t)ld * (uint32_t)sizeof(T);
+        at = rows_buffer(y + r0 * ld, (uint32_t)(here - 1) * step + (uint32_t)all * (uint32_t)sizeof(T));
+        h = h0 + N * (lane_id() & 15);
+        H = columns;
+        whole = columns % N == 0 && ((uint32_t)(uintptr_t)y | step | (uint32_t)(front * (int)sizeof(T))) % sizeof(V) == 0;
+        first = 4 * (uint32_t)(lane_id() >> 4) * step + (uint32_t)(front + h) * (uint32_t)sizeof(T);
+    }
+    template <class Use> __device__ __forceinline__ void each(Use use) const {
+#pragma unroll
+        for (int c = 0; c < RN; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) use(c, i, (uint32_t)(16 * c + i) * step);
+    }
+    // v(c, n): column n of the lane's rows of the c-th sixteen
+    template <int Kind = 0, class Get> __device__ __forceinline__ void put(Get v) const {
+        if (whole) {
+            const uint32_t from = h < H ? first : kNowhere;
+            each([&](int c, int i, uint32_t row) {
+                V x;
+#pragma unroll
+                for (int n = 0; n < N; ++n) x[n] = (T)v(c, n)[i];
+                buffer_store<Kind>(x, at, from + row);
+            });
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const uint32_t from = h + n < H ? first + n * (uint32_t)sizeof(T) : kNowhere;
+                each([&](int c, int i, uint32_t row) { buffer_store<Kind>((T)v(c, n)[i], at, from + row); });
+            }
+        }
+    }
+    __device__ __forceinline__ void get(f32x4 (&v)[RN][N]) const {
+        if (whole) {
+            const uint32_t from = h < H ? first : kNowhere;
+            each([&](int c, int i, uint32_t row) {
+                const V x = buffer_load<V>(at, from + row);
+#pragma unroll
+                for (int n = 0; n < N; ++n) v[c][n][i] = (float)x[n];
+            });
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const uint32_t from = h + n < H ? first + n * (uint32_t)sizeof(T) : kNowhere;
+                each([&](int c, int i, uint32_t row) { v[c][n][i] = (float)buffer_load<T>(at, from + row); });
+            }
+        }
+    }
+};
+// Whether a tile's rows span what a buffer can.
+static inline bool spans(int64_t ld, int bytes, int rows) { return (rows + 1) * ld * bytes < (1ll << 31); }
+
 // A list's matrices of results: Y, read or written, and dP.  `row`: of the list; `have`: rows that are there from it on.
 template <class T, int Mode>
 struct Results {

@@ -122,11 +122,11 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int TB = kHeldWaves * 16 * RN, MR = Mode == kProduct ? 64 : 128;       // rows of X per workgroup, rows of W per 64 columns
     constexpr int kLs = 128 * KS + kLdsPad;            // bytes of a row of W in LDS: codes, zeros up to whole steps, scales
-    constexpr bool kAhead = KS * RN <= 4, kExact = sizeof(T) == 4, kDirect = !Lines && Mode == kGatedGrad;
+    constexpr bool kExact = sizeof(T) == 4, kAhead = KS * RN <= (kExact && (Mode == kGatedGrad || KS > 2) ? 2 : 4);
     const Lists lists(a.t, TB);
     const int total = lists.total(), groups = group_of_lane(a.t);
     if (total == 0) return;
-    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = lane_id(), m = l & 15, q = l >> 4;
     const int ht = (a.H + 63) / 64;
     int parts = a.fill / total;                        // few rows: the columns of the result are dealt out too
     parts = parts < 1 ? 1 : parts > ht ? ht : parts;
@@ -210,30 +210,25 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
             }
         if (kAhead && item + share.step < share.end) { it = find(item + share.step); ask_rows(it); }
         if (mine <= 0) continue;
+        const int rows = mine < 16 * RN ? mine : 16 * RN;
         const Results<T, Mode> res(a, list);
-        T* const y = (Mode == kGatedGrad ? res.p : res.y);
-        const int64_t ld = Mode == kGatedGrad ? res.pld : res.ld;
-        constexpr int kOuts = Mode == kGatedGrad ? 2 : 1;
-        RowsOut<T, RN> out[kOuts];
-        if constexpr (!Lines && !kDirect) {
-#pragma unroll
-            for (int k = 0; k < kOuts; ++k) {
-                out[k].lds = lds + a.w_lds + (wave * kOuts + k) * a.out_lds;
-                out[k].rows = mine < 16 * RN ? mine : 16 * RN;
-                out[k].step = ld * (int64_t)sizeof(T);
-                out[k].y = reinterpret_cast<char*>(y + r0 * ld + k * a.H + 64 * t0);
-                out[k].bytes = ((64 * t1 < a.H ? 64 * t1 : a.H) - 64 * t0) * (int)sizeof(T);
-                out[k].run = kOuts == 1 && out[k].bytes == out[k].step && 16 * RN * out[k].bytes + 16 <= a.out_lds;
-                out[k].begin();
-            }
+        T* const y = res.y;
+        const int64_t ld = res.ld;
+        RowsOut<T, RN> out;
+        if constexpr (!Lines && Mode != kGatedGrad) {
+            out.lds = lds + a.w_lds + wave * a.out_lds;
+            out.rows = rows;
+            out.step = ld * (int64_t)sizeof(T);
+            out.y = reinterpret_cast<char*>(y + r0 * ld + 64 * t0);
+            out.bytes = ((64 * t1 < a.H ? 64 * t1 : a.H) - 64 * t0) * (int)sizeof(T);
+            out.run = out.bytes == out.step && 16 * RN * out.bytes + 16 <= a.out_lds;
+            out.begin();
         }
         for (int t = t0; t < t1; ++t) {
             const uint8_t* tile_w = lds + (t - t0) * MR * kLs;
-            const bool whole = mine >= 16 * RN && 64 * t + 64 <= a.H;
             f32x4 dy[RN][4];
             if constexpr (Mode == kGatedGrad) {
-#pragma unroll
-                for (int c = 0; c < RN; ++c) res.get(a, r0 + 16 * c + 4 * q, mine - 16 * c - 4 * q, 64 * t + 4 * m, dy[c]);
+                Tile<T, RN, 4>(res.y, res.ld, r0, rows, 64 * t, 0, a.H, a.H).get(dy);
             }
             f32x4 acc[MR / 64][RN][4];
 #pragma unroll
@@ -257,28 +252,16 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
             }
 #pragma unroll
             for (int c = 0; c < RN; ++c) combine<Mode>(a.act, acc[0][c], acc[MR / 64 - 1][c], dy[c]);
-            if constexpr (Lines) {
-#pragma unroll
-                for (int k = 0; k < kOuts; ++k)
-#pragma unroll
-                    for (int c = 0; c < RN; ++c) {
-                        T* at = y + (r0 + 16 * c + 4 * q) * ld + k * a.H;
-                        if (whole) put_whole<T>(at + 64 * t + 4 * m, ld, acc[k][c]);
-                        else put_tile<T>(at, ld, mine - 16 * c - 4 * q, 64 * t + 4 * m, a.H, true, acc[k][c]);
-                    }
-            } else if constexpr (kDirect) {
-#pragma unroll
-                for (int c = 0; c < RN; ++c) {
-                    res.put(a, r0 + 16 * c + 4 * q, mine - 16 * c - 4 * q, 64 * t + 4 * m, acc[0][c]);
-                    res.put_second(a, r0 + 16 * c + 4 * q, mine - 16 * c - 4 * q, 64 * t + 4 * m, acc[1][c]);
-                }
+            if constexpr (Mode == kGatedGrad) {
+                constexpr int kind = Lines ? kPastL2 : 0;
+                Tile<T, RN, 4>(res.p, res.pld, r0, rows, 64 * t, 0, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
+                Tile<T, RN, 4>(res.p, res.pld, r0, rows, 64 * t, a.H, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[1][c][n]; });
+            } else if constexpr (Lines) {
+                Tile<T, RN, 4>(y, ld, r0, rows, 64 * t, 0, a.H, a.H).template put<kPastL2>([&](int c, int n) { return acc[0][c][n]; });
             } else {
-#pragma unroll
-                for (int k = 0; k < kOuts; ++k) {
-                    out[k].put(t - t0, acc[k]);
-                    if (!out[k].run) out[k].flush_lines(t - t0, t == t0, t + 1 == t1);
-                    else if (t + 1 == t1) out[k].flush_run();
-                }
+                out.put(t - t0, acc[0]);
+                if (!out.run) out.flush_lines(t - t0, t == t0, t + 1 == t1);
+                else if (t + 1 == t1) out.flush_run();
             }
         }
     }
@@ -311,7 +294,6 @@ static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
 }
 template <class T, int Mode>
 static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
-    *done = false;
     // rows that begin with a line each are stored as they come, 128 or 256 bytes of a row at a time
     bool lines = Mode != kGatedGrad || a.H * sizeof(T) % 128 == 0;
     for (int j = 0; j < a.t.n_lists; ++j) {
@@ -337,18 +319,21 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
 // The form for weights that LDS does not hold.  A wavefront keeps 64 rows of W in registers (32 of the gate's and the same 32 of the other
 // factor), all columns of them, and a workgroup goes over its share of the rows of X, 32 at a time, which its wavefronts read from LDS:
 // W is read once per workgroup, and per product half as much from LDS as with X in registers and W in LDS.  The workgroups that have the same
-// rows and other columns share an XCD's L2 and take the rows in the same order at the same time.
+// rows and other columns share an XCD's L2 and take the rows in the same order at the same time.  With one wavefront per SIMD nothing else
+// works while it waits, so that a tile's work is one piece of code without branches, the next tile's way to LDS in the middle of its products.
+// Rows of X at a time, in sixteens: one where the registers would not hold what two need.  No kernel here may spill registers: the compiler (of
+// ROCm 7.2) has lost some of those that it had to put away where a kernel fills all 512.
+template <int Mode, int KS> constexpr int kWideRows = Mode == kGatedGrad && KS == 8 ? 1 : 2;
 template <class T, int Mode, int KS, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, KS > 4 ? 1 : 2) hidden_wide_kernel(HiddenArgs a) {
+__global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    constexpr int RN = 2, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
-    constexpr int kLs = 128 * KS + kLdsPad, lv = kLs / 16;         // bytes and vectors of a row of X in LDS: codes, zeros up to whole steps, scales
-    constexpr int kVec = (TB * lv + threads - 1) / threads;
+    constexpr int RN = kWideRows<Mode, KS>, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
+    constexpr int kLs = 128 * KS + kLdsPad;                   // bytes of a row of X in LDS: codes, zeros up to whole steps, scales
+    constexpr int kVec = (TB * (8 * KS + 1) + threads - 1) / threads;
     constexpr bool kExact = sizeof(T) == 4;
-    constexpr int kDepth = KS >= 4 ? 1 : 2;         // tiles in registers, as many as there is room for
     const Lists lists(a.t, TB);
     const int total = lists.total(), groups = group_of_lane(a.t);
-    const int wave = threadIdx.x >> 6, l = lane_id(), m = l & 15, q = l >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = lane_id(), m = l & 15, q = l >> 4;
     // which columns, which rows
     int block, at, end, step;
     if (a.shares > 0) {
@@ -389,112 +374,114 @@ __global__ void __launch_bounds__(64 * WAVES, KS > 4 ? 1 : 2) hidden_wide_kernel
         held_group = group;
     };
 
-    // X: the thread's vectors of a tile, by row and place; those of the zeros between codes and scales stay as they are
-    uint32_t from[kVec];
-    int row_of[kVec];                                         // or -1
+    // X: where the thread's vectors of a tile come from and go to; the zeros between codes and scales are never written
+    uint32_t places[kVec];                                    // 16 bits each
+    static_assert(TB * kLs <= 65536, "");
+    {
+        const uint32_t per = (uint32_t)a.cb / 16 + 1, all = TB * per;
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) {
-        const uint32_t i = k * threads + threadIdx.x, r = i / lv, v = i - r * lv;
-        const bool scale = v == 8 * KS;
-        row_of[k] = r < TB && (scale || (v < 8 * KS && 16 * (int)v < a.cb)) ? (int)r : -1;
-        from[k] = row_of[k] < 0 ? 0 : r * a.rb + (scale ? a.cb : 16 * v);
+        for (int k = 0; k < kVec; ++k) {
+            uint32_t i = k * threads + threadIdx.x;
+            i = i < all ? i : all - 1;
+            const uint32_t r = i / per, v = i - r * per;
+            places[k] = (r * (uint32_t)a.rb + 16 * v) | (r * kLs + (v + 1 < per ? 16 * v : 128 * KS)) << 16;
+        }
     }
-    struct Tile { int list, here, group; int64_t r0; };
-    u32x4 ahead[kDepth][kVec];
-    Tile tiles[kDepth];
-    auto find = [&](int tile) {
-        Tile t;
-        t.list = lists.list_of(tile);
-        t.r0 = (int64_t)(tile - lists.first_tile(t.list)) * TB;
-        const int64_t left = lists.rows_in(t.list) - t.r0;
+    struct Piece { int list, here, group; int64_t r0; };
+    const uint8_t* x_list = nullptr;                          // of the list of the tile that was asked for last
+    int x_until = at, x_first = 0, x_rows = 0, x_group = 0, x_of = 0;
+    u32x4 ahead[kVec];
+    auto find = [&](int tile) {                               // behind the last tile the last one again
+        tile = tile < end ? tile : end - 1;
+        if (tile >= x_until) {
+            x_of = lists.list_of(tile);
+            x_first = lists.first_tile(x_of);
+            x_until = __builtin_amdgcn_readlane(lists.upto, x_of);
+            x_rows = lists.rows_in(x_of);
+            x_group = __builtin_amdgcn_readlane(groups, x_of);
+            x_list = a.t.rows[x_of];
+        }
+        Piece t;
+        t.list = x_of; t.group = x_group;
+        t.r0 = (int64_t)(tile - x_first) * TB;
+        const int64_t left = x_rows - t.r0;
         t.here = left < TB ? (int)left : TB;
-        t.group = __builtin_amdgcn_readlane(groups, t.list);
         return t;
     };
-    // Behind the last tile the last one again.
-    auto ask = [&](int u, int tile) {
-        tiles[u] = find(tile < end ? tile : end - 1);
-        const uint8_t* x = a.t.rows[tiles[u].list] + tiles[u].r0 * a.rb;
-        uint32_t off[kVec];
+    auto ask = [&](const Piece& t) {
+        const auto x = rows_buffer(x_list + t.r0 * a.rb, (uint32_t)(t.here * a.rb));
 #pragma unroll
-        for (int k = 0; k < kVec; ++k) off[k] = from[k];
-        if (tiles[u].here < TB)
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const int over = row_of[k] - (tiles[u].here - 1);
-                off[k] -= over > 0 ? (uint32_t)(over * a.rb) : 0;
-            }
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) ahead[u][k] = *reinterpret_cast<const u32x4*>(x + off[k]);
+        for (int k = 0; k < kVec; ++k) ahead[k] = __builtin_amdgcn_raw_buffer_load_b128(x, (int)(places[k] & 0xFFFF), 0, 0);
     };
-    auto keep = [&](int u, uint8_t* to) {
+    auto keep = [&](uint8_t* buf) {
 #pragma unroll
-        for (int k = 0; k < kVec; ++k)
-            if (row_of[k] >= 0) reinterpret_cast<u32x4*>(to)[k * threads + threadIdx.x] = ahead[u][k];
+        for (int k = 0; k < kVec; ++k) *reinterpret_cast<u32x4*>(buf + (places[k] >> 16)) = ahead[k];
     };
-    ask(0, at);
-    hold(tiles[0].group);
-    Tile now = tiles[0];
+    Piece now = find(at);
+    ask(now);
     __syncthreads();
-    keep(0, lds);
-    ask(0, at + step);
-    if (kDepth > 1) ask(kDepth - 1, at + 2 * step);
-    for (int tile = at, j = 0; tile < end; tile += 2 * step, j += 2) {
+    keep(lds);
+    hold(now.group);
+    Piece next = find(at + step);
+    ask(next);
+    int out_list = -1;
+    T *y = nullptr, *p = nullptr;                             // the list's Y and dP
+    int64_t ld = 0, pld = 0;
+    for (int tile = at, j = 0; tile < end; tile += step, ++j) {
+        __syncthreads();                                      // this tile is in LDS, and the one before has been read by all
+        if (now.group != held_group) hold(now.group);
+        if (now.list != out_list) {
+            out_list = now.list;
+            y = static_cast<T*>(a.t.y[now.list]);
+            ld = a.t.ld[now.list];
+            if constexpr (Mode == kGatedGrad) { p = static_cast<T*>(a.dp[now.list]); pld = a.dp_ld[now.list]; }
+        }
+        const Piece after = find(tile + 2 * step);
+        const uint8_t* x = lds + (j & 1) * buffer;
+        uint8_t* const other = lds + (~j & 1) * buffer;
+        constexpr int N = cols / 16;                          // columns of a lane
+        f32x4 dy[RN][N];
+        if constexpr (Mode == kGatedGrad) Tile<T, RN, N>(y, ld, now.r0, now.here, h0, 0, a.H, a.H).get(dy);
+        f32x4 acc[RN][4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (tile + u * step >= end) break;
-            __syncthreads();                                  // this tile is in LDS, and the one before has been read by all
-            if (now.group != held_group) hold(now.group);
-            const uint8_t* x = lds + u * buffer;
-            constexpr int mask = kDepth - 1;
-            const Tile next = tiles[u & mask];
-            f32x4 acc[RN][4];
+        for (int c = 0; c < RN; ++c)
 #pragma unroll
-            for (int c = 0; c < RN; ++c)
-#pragma unroll
-                for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
-            steps_of<KS>([&](auto index) {
-                constexpr int s = decltype(index)::value;
-                Operand xv[RN];
-#pragma unroll
-                for (int c = 0; c < RN; ++c) {
-                    const uint8_t* p = x + (16 * c + m) * kLs;
-                    xv[c].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
-                    xv[c].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
-                    xv[c].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
-                }
-                multiply<kExact, (s & 3)>(acc, xv, w[s]);
-                // while the matrix cores work
-                if (s == (KS > 2 ? 1 : 0)) keep(u & mask, lds + (u ^ 1) * buffer);
-                if (s == (KS > 3 ? 2 : KS - 1)) ask(u & mask, tile + (u + 1 + kDepth) * step);
-            });
-            const Results<T, Mode> out(a, now.list);
-            const bool whole = now.here == TB && h0 + cols <= a.H && out.wide;
+            for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+        steps_of<KS>([&](auto index) {
+            constexpr int s = decltype(index)::value;
+            Operand xv[RN];
 #pragma unroll
             for (int c = 0; c < RN; ++c) {
-                const int64_t row = now.r0 + 16 * c + 4 * q;
-                const int have = now.here - 16 * c - 4 * q;
-                if constexpr (Mode == kProduct) {
-                    if (whole) put_whole<T>(out.y + row * out.ld + h0 + 4 * m, out.ld, acc[c]);
-                    else out.put(a, row, have, h0 + 4 * m, acc[c]);
-                } else {
-                    f32x4(&one)[2] = reinterpret_cast<f32x4(&)[2]>(acc[c][0]);
-                    f32x4(&two)[2] = reinterpret_cast<f32x4(&)[2]>(acc[c][2]);
-                    f32x4 dy[2];
-                    if constexpr (Mode == kGatedGrad) out.get(a, row, have, h0 + 2 * m, dy);
-                    combine<Mode>(a.act, one, two, dy);
-                    out.put(a, row, have, h0 + 2 * m, one);
-                    if constexpr (Mode == kGatedGrad) out.put_second(a, row, have, h0 + 2 * m, two);
-                }
+                const uint8_t* p = x + (16 * c + m) * kLs;
+                xv[c].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
+                xv[c].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
+                xv[c].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
             }
-            now = next;
+            multiply<kExact, (s & 3)>(acc, xv, w[s]);
+            if (s == (KS > 2 ? 1 : 0)) keep(other);
+            if (s == (KS > 3 ? 2 : KS - 1)) ask(after);
+        });
+#pragma unroll
+        for (int c = 0; c < RN; ++c)
+            if constexpr (Mode != kProduct)
+                combine<Mode>(a.act, reinterpret_cast<f32x4(&)[2]>(acc[c][0]), reinterpret_cast<f32x4(&)[2]>(acc[c][2]), reinterpret_cast<f32x4(&)[2]>(dy[c][0]));
+        if constexpr (Mode == kGatedGrad) {
+            Tile<T, RN, N>(p, pld, now.r0, now.here, h0, 0, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][n]; });
+            Tile<T, RN, N>(p, pld, now.r0, now.here, h0, a.H, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][N + n]; });
+        } else {
+            // whole lines past the L2 (200k rows 256 -> 1024 in bf16: 121 us with plain stores, 79 so)
+            const Tile<T, RN, N> to(y, ld, now.r0, now.here, h0, 0, a.H, a.H);
+            if (Mode == kProduct && (((uint32_t)(uintptr_t)y | to.step) & 127) == 0) to.template put<kPastL2>([&](int c, int n) { return acc[c][n]; });
+            else to.put([&](int c, int n) { return acc[c][n]; });
         }
+        now = next;
+        next = after;
     }
 }
 
 template <class T, int Mode, int KS, int WAVES>
 static int launch_wide(spp_ctx* ctx, HiddenArgs& a) {
-    constexpr int TB = 32, cols = WAVES * (Mode == kProduct ? 64 : 32);
+    constexpr int TB = 16 * kWideRows<Mode, KS>, cols = WAVES * (Mode == kProduct ? 64 : 32);
     auto kernel = hidden_wide_kernel<T, Mode, KS, WAVES>;
     constexpr int lds = 2 * TB * (128 * KS + kLdsPad);
     static LdsLimit limit;
@@ -517,14 +504,16 @@ static int launch_wide(spp_ctx* ctx, HiddenArgs& a) {
 
 template <class T, int Mode>
 static int launch_hidden(spp_ctx* ctx, HiddenArgs& a) {
-    bool done;
-    SPP_TRY((try_held<T, Mode>(ctx, a, &done)));
+    bool done = false, near = true;                      // whether 32 rows of results are within what a buffer spans
+    for (int j = 0; j < a.t.n_lists; ++j)
+        near = near && spans(a.t.ld[j], sizeof(T), 32) && (Mode != kGatedGrad || spans(a.dp_ld[j], sizeof(T), 32));
+    if (near) SPP_TRY((try_held<T, Mode>(ctx, a, &done)));
     if (done) return SPP_OK;
-    switch (a.steps) {
+    if (near) switch (a.steps) {
         case 1: return launch_wide<T, Mode, 1, 8>(ctx, a);
         case 2: return launch_wide<T, Mode, 2, 8>(ctx, a);
         case 3: return launch_wide<T, Mode, 3, 8>(ctx, a);
-        case 4: return launch_wide<T, Mode, 4, 8>(ctx, a);
+        case 4: return launch_wide<T, Mode, 4, Mode == kGatedGrad ? 4 : 8>(ctx, a);
         case 5: return launch_wide<T, Mode, 5, 4>(ctx, a);
         case 6: return launch_wide<T, Mode, 6, 4>(ctx, a);
         case 7: return launch_wide<T, Mode, 7, 4>(ctx, a);

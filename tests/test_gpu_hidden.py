@@ -58,7 +58,7 @@ def _split(w, H, D):
 def test_product_of_one_list(ctx, dtype, n, D, H):
     rng = np.random.default_rng(n * 7 + D * 3 + H)
     rows, w = _rows(rng, n, D), _rows(rng, H, D, D ** -0.5)
-    y = spp.fp8_product(ctx, _dev(rows), _dev(w), D, dtype=dtype)
+    y = spp.fp8_product(ctx, _dev(rows), _dev(w), D, out=torch.full((n, H), float("nan"), dtype=dtype, device=DEV))
     _close(y, *R.sums(R.values(rows, D), R.values(w, D), _bits(dtype)), dtype)
 
 
@@ -71,8 +71,8 @@ def test_gated_layer_of_one_list_and_its_gradient(ctx, dtype, n, D, H):
     act = ("silu", "gelu", "sigmoid")[(n + D + H) % 3]
     dy = torch.from_numpy(rng.standard_normal((n, H))).to(dtype)
     xd, wd, dyd = _dev(rows), _dev(w), dy.to(DEV)
-    dp = torch.empty(n, 2 * H, dtype=dtype, device=DEV)
-    y = spp.fp8_gated(ctx, xd, wd, D, activation=act, dtype=dtype)
+    dp = torch.full((n, 2 * H), float("nan"), dtype=dtype, device=DEV)
+    y = spp.fp8_gated(ctx, xd, wd, D, activation=act, out=torch.full((n, H), float("nan"), dtype=dtype, device=DEV))
     _close(y, *R.gated(x, wg, wu, act, _bits(dtype)), dtype)
     spp.fp8_gated_grad(ctx, [(xd, n, None, dyd)], [(xd, n, None, dp)], wd, D, activation=act)
     _close(dp, *R.gated_grad(x, wg, wu, dy.double().numpy(), act, _bits(dtype)), dtype)
