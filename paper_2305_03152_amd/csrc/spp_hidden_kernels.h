@@ -447,19 +447,31 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
         for (int c = 0; c < RN; ++c)
 #pragma unroll
             for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
-        steps_of<KS>([&](auto index) {
+        // The next tile goes to LDS and the one behind it is asked for during the products.  One wavefront per SIMD also reads each step's rows
+        // before the products of the step before; the compiler, short of registers, would put every load right before its use (390k rows
+        // 1024 -> 1024 490 us, 400 so).
+        constexpr bool kOrdered = WAVES == 4;
+        Operand xv[kOrdered ? 2 : 1][RN];
+        auto read = [&](auto index) {
             constexpr int s = decltype(index)::value;
-            Operand xv[RN];
 #pragma unroll
             for (int c = 0; c < RN; ++c) {
                 const uint8_t* p = x + (16 * c + m) * kLs;
-                xv[c].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
-                xv[c].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
-                xv[c].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
+                xv[kOrdered ? s & 1 : 0][c].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
+                xv[kOrdered ? s & 1 : 0][c].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
+                xv[kOrdered ? s & 1 : 0][c].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
             }
-            multiply<kExact, (s & 3)>(acc, xv, w[s]);
+        };
+        if constexpr (kOrdered) read(std::integral_constant<int, 0>());
+        steps_of<KS>([&](auto index) {
+            constexpr int s = decltype(index)::value;
+            if constexpr (!kOrdered) read(index);
+            else if constexpr (s + 1 < KS) read(std::integral_constant<int, s + 1>());
+            if (kOrdered) __builtin_amdgcn_sched_barrier(0);
+            multiply<kExact, (s & 3)>(acc, xv[kOrdered ? s & 1 : 0], w[s]);
             if (s == (KS > 2 ? 1 : 0)) keep(other);
-            if (s == (KS > 3 ? 2 : KS - 1)) ask(after);
+            if (s == (KS > 2 ? 2 : KS - 1)) ask(after);
+            if (kOrdered) __builtin_amdgcn_sched_barrier(0);
         });
 #pragma unroll
         for (int c = 0; c < RN; ++c)
