@@ -117,7 +117,9 @@ __global__ void __launch_bounds__(kTileBlock) hidden_tile_kernel(HiddenArgs a) {
 // the result 64 at a time (64 of the gate's and the same 64 of the other factor); a workgroup's wavefronts share W and wait for each other only
 // where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.
 constexpr int kHeldWaves = 8, kHeldBlock = 64 * kHeldWaves;
-template <class T, int Mode, int KS, int RN, bool Lines>
+// How results leave: rows that begin with a line each straight from registers past the L2, others by way of LDS, or straight too.
+enum HeldOut { kLines, kRagged, kStraight };
+template <class T, int Mode, int KS, int RN, int Out>
 __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int TB = kHeldWaves * 16 * RN, MR = Mode == kProduct ? 64 : 128;       // rows of X per workgroup, rows of W per 64 columns
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
         T* const y = res.y;
         const int64_t ld = res.ld;
         RowsOut<T, RN> out;
-        if constexpr (!Lines && Mode != kGatedGrad) {
+        if constexpr (Out == kRagged) {
             out.lds = lds + a.w_lds + wave * a.out_lds;
             out.rows = rows;
             out.step = ld * (int64_t)sizeof(T);
@@ -253,11 +255,12 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
 #pragma unroll
             for (int c = 0; c < RN; ++c) combine<Mode>(a.act, acc[0][c], acc[MR / 64 - 1][c], dy[c]);
             if constexpr (Mode == kGatedGrad) {
-                constexpr int kind = Lines ? kPastL2 : 0;
+                constexpr int kind = Out == kLines ? kPastL2 : 0;
                 Tile<T, RN, 4>(res.p, res.pld, r0, rows, 64 * t, 0, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
                 Tile<T, RN, 4>(res.p, res.pld, r0, rows, 64 * t, a.H, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[1][c][n]; });
-            } else if constexpr (Lines) {
-                Tile<T, RN, 4>(y, ld, r0, rows, 64 * t, 0, a.H, a.H).template put<kPastL2>([&](int c, int n) { return acc[0][c][n]; });
+            } else if constexpr (Out != kRagged) {
+                constexpr int kind = Out == kLines ? kPastL2 : 0;
+                Tile<T, RN, 4>(y, ld, r0, rows, 64 * t, 0, a.H, a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
             } else {
                 out.put(t - t0, acc[0]);
                 if (!out.run) out.flush_lines(t - t0, t == t0, t + 1 == t1);
@@ -269,13 +272,13 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
 
 constexpr int kHeldLds = 163840;         // all of a CU's
 constexpr int kHeldRowOut = 768;         // bytes of rows that go out in one run
-template <class T, int Mode, int KS, bool Lines>
+template <class T, int Mode, int KS, int Out>
 static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
-    constexpr int RN = KS <= 2 && (Lines || Mode == kGatedGrad) ? 2 : 1, MR = Mode == kProduct ? 64 : 128, TB = kHeldWaves * 16 * RN;
-    auto kernel = hidden_held_kernel<T, Mode, KS, RN, Lines>;
+    constexpr int RN = KS <= 2 && Out != kRagged ? 2 : 1, MR = Mode == kProduct ? 64 : 128, TB = kHeldWaves * 16 * RN;
+    auto kernel = hidden_held_kernel<T, Mode, KS, RN, Out>;
     const int ht = (a.H + 63) / 64, row = a.H * (int)sizeof(T);
-    a.out_lds = Lines || Mode == kGatedGrad ? 0 : 16 * RN * RowsOut<T, RN>::kPitch;
-    if (!Lines && Mode != kGatedGrad && row <= kHeldRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
+    a.out_lds = Out != kRagged ? 0 : 16 * RN * RowsOut<T, RN>::kPitch;
+    if (Out == kRagged && row <= kHeldRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
     const int64_t need = (int64_t)ht * MR * (128 * KS + kLdsPad), most_lds = kHeldLds - (int64_t)kHeldWaves * a.out_lds;
     *done = need <= most_lds;
     if (!*done) return SPP_OK;
@@ -303,13 +306,25 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
     }
     auto with = [&](auto steps) {
         constexpr int KS = decltype(steps)::value;
-        return lines ? launch_held<T, Mode, KS, true>(ctx, a, done) : launch_held<T, Mode, KS, false>(ctx, a, done);
+        // the gradient's two halves would need twice the LDS, and beside long rows of X the results are few
+        if constexpr (KS > 6 && sizeof(T) == 4) return (int)SPP_OK;          // (registers)
+        else if constexpr (KS > 4) {
+            // with few columns most wavefronts of the other form would have none: 200k rows 1024 -> 24 68 and 56 us, 640 -> 47 49 and 39; of 16 bits
+            // 640 -> 128 42 and 49, of 32 85 and 72
+            if (sizeof(T) == 2 && a.H > 64) return (int)SPP_OK;
+            return launch_held<T, Mode, KS, kStraight>(ctx, a, done);
+        }
+        else return lines ? launch_held<T, Mode, KS, kLines>(ctx, a, done) : launch_held<T, Mode, KS, Mode == kGatedGrad ? kStraight : kRagged>(ctx, a, done);
     };
     switch (a.steps) {
         case 1: return with(std::integral_constant<int, 1>());
         case 2: return with(std::integral_constant<int, 2>());
         case 3: return with(std::integral_constant<int, 3>());
         case 4: return with(std::integral_constant<int, 4>());
+        case 5: return with(std::integral_constant<int, 5>());
+        case 6: return with(std::integral_constant<int, 6>());
+        case 7: return with(std::integral_constant<int, 7>());
+        case 8: return with(std::integral_constant<int, 8>());
     }
     return SPP_OK;
 }
