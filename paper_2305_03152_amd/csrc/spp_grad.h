@@ -338,14 +338,16 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
                 bf16x8 bx[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) bx[c] = column8<S::lx>(gx + row * S::lx + col + wd + 16 * c);
+                // the next rows of dY are read during the products of these
+                auto read = [&](int e) { return column8<S::ly>(gy + (e / FH * S::rows + row) * S::ly + col + wh + 16 * (e % FH)); };
+                bf16x8 ay[2];
+                ay[0] = read(0);
 #pragma unroll
-                for (int p = 0; p < P; ++p)
+                for (int e = 0; e < P * FH; ++e) {
+                    if (e + 1 < P * FH) ay[(e + 1) & 1] = read(e + 1);
 #pragma unroll
-                    for (int f = 0; f < FH; ++f) {
-                        const bf16x8 ay = column8<S::ly>(gy + (p * S::rows + row) * S::ly + col + wh + 16 * f);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ay, bx[c], acc[f][c], 0, 0, 0);
-                    }
+                    for (int c = 0; c < 4; ++c) acc[e % FH][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ay[e & 1], bx[c], acc[e % FH][c], 0, 0, 0);
+                }
             }
         }
     }
