@@ -272,9 +272,9 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
 
 constexpr int kHeldLds = 163840;         // all of a CU's
 constexpr int kHeldRowOut = 768;         // bytes of rows that go out in one run
-template <class T, int Mode, int KS, int Out>
+template <class T, int Mode, int KS, int RN, int Out>
 static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
-    constexpr int RN = KS <= 2 && Out != kRagged ? 2 : 1, MR = Mode == kProduct ? 64 : 128, TB = kHeldWaves * 16 * RN;
+    constexpr int MR = Mode == kProduct ? 64 : 128, TB = kHeldWaves * 16 * RN;
     auto kernel = hidden_held_kernel<T, Mode, KS, RN, Out>;
     const int ht = (a.H + 63) / 64, row = a.H * (int)sizeof(T);
     a.out_lds = Out != kRagged ? 0 : 16 * RN * RowsOut<T, RN>::kPitch;
@@ -306,15 +306,29 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
     }
     auto with = [&](auto steps) {
         constexpr int KS = decltype(steps)::value;
-        // the gradient's two halves would need twice the LDS, and beside long rows of X the results are few
-        if constexpr (KS > 6 && sizeof(T) == 4) return (int)SPP_OK;          // (registers)
-        else if constexpr (KS > 4) {
+        constexpr int RN = KS <= 2 ? 2 : 1;
+        if constexpr (KS > 6 && sizeof(T) == 4) {
+            return (int)SPP_OK;                              // (registers)
+        } else if constexpr (KS > 4) {
             // with few columns most wavefronts of the other form would have none: 200k rows 1024 -> 24 68 and 56 us, 640 -> 47 49 and 39; of 16 bits
             // 640 -> 128 42 and 49, of 32 85 and 72
             if (sizeof(T) == 2 && a.H > 64) return (int)SPP_OK;
-            return launch_held<T, Mode, KS, kStraight>(ctx, a, done);
+            return launch_held<T, Mode, KS, RN, kStraight>(ctx, a, done);
+        } else if (lines) {
+            return launch_held<T, Mode, KS, RN, kLines>(ctx, a, done);
+        } else if constexpr (Mode != kProduct) {
+            // beside two products the LDS that rows need is worth more to W and to a second sixteen rows of X (1M rows 172 -> 100 in bf16 by way of
+            // LDS 163 us, so 115; in fp32 235 and 193)
+            return launch_held<T, Mode, KS, RN, kStraight>(ctx, a, done);
+        } else {
+            // 300k rows 256 -> 86, -> 172 in bf16 with one sixteen 40 and 44 us, with two 31 and 38; 128 -> 86 in fp32 41 and 34, in bf16 24 and 26
+            // (and two steps in fp32 fill the registers)
+            if constexpr (KS == (sizeof(T) == 4 ? 1 : 2)) {
+                SPP_TRY((launch_held<T, Mode, KS, 2, kRagged>(ctx, a, done)));
+                if (*done) return (int)SPP_OK;
+            }
+            return launch_held<T, Mode, KS, 1, kRagged>(ctx, a, done);
         }
-        else return lines ? launch_held<T, Mode, KS, kLines>(ctx, a, done) : launch_held<T, Mode, KS, Mode == kGatedGrad ? kStraight : kRagged>(ctx, a, done);
     };
     switch (a.steps) {
         case 1: return with(std::integral_constant<int, 1>());
