@@ -468,6 +468,7 @@ int  spp_fp8_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64
  *                    2H for H it gives the gradients of Wg and Wu, one behind the other.
  *     X and W are the values that the rows stand for; sums and activations are formed in fp32 and rounded once to Y's type.  The gradient
  *     of the rows of a layer is the product of dY (dP) in 8 bits by the transposed weights (of Wg and Wu, one behind the other).
+ *     Of rows of other origin a value below 2^-126 may count as 0.
  *     Rows from *d_n on are neither read nor written, nor what lies between rows of Y; recording as in (6). */
 int  spp_fp8_product(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
                      int32_t D, int32_t H, int32_t type, uint32_t flags);

@@ -479,3 +479,119 @@ def test_rows_of_any_length_and_address(ctx, dtype, n, D, H, pad, offset):
     near(dp, torch.cat([dy.float() * u * s * (1 + g * (1 - s)), dy.float() * g * s], 1))
     between(pbuf, 2 * H)
     between(buf, H)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("further", [0, 1])
+@pytest.mark.parametrize("n,D,H", [(70, 100, 70), (70, 700, 300), (33, 1000, 47)])
+def test_rows_of_results_gigabytes_apart(ctx, dtype, further, n, D, H):
+    """33 rows within 2^31 bytes by a hair, and not by a hair: offsets of 32 bits from a tile's first row, and of 64."""
+    es = torch.empty(0, dtype=dtype).element_size()
+    ld = (2 ** 31 - 1) // (33 * es) + further
+    rng = np.random.default_rng(D + H)
+    rows, w = _rows(rng, n, D), _rows(rng, 2 * H, D, D ** -0.5)
+    x, (wg, wu) = R.values(rows, D), _split(w, H, D)
+    xd, wd = _dev(rows), _dev(w)
+    buf = torch.full((n * ld,), 7.0, dtype=dtype, device=DEV)
+    y, p = buf.as_strided((n, H), (ld, 1)), buf.as_strided((n, 2 * H), (ld, 1), H)
+    spp.fp8_product(ctx, xd, wd[:H], D, out=y)
+    _close(y, *R.sums(x, wg, _bits(dtype)), dtype)
+    spp.fp8_gated(ctx, xd, wd, D, out=y)
+    _close(y, *R.gated(x, wg, wu, "silu", _bits(dtype)), dtype)
+    dy = torch.from_numpy(rng.standard_normal((n, H))).to(dtype)
+    y.copy_(dy)
+    spp.fp8_gated_grad(ctx, [(xd, n, None, y)], [(xd, n, None, p)], wd, D)
+    _close(p, *R.gated_grad(x, wg, wu, dy.double().numpy(), "silu", _bits(dtype)), dtype)
+    assert torch.equal(y.cpu(), dy)
+    g = spp.fp8_weight_grad(ctx, [(xd, n, None, p)], 2 * H, D)[0]
+    v = p.double().cpu().numpy()
+    _close(g, v.T @ x, 3 * n * 2.0 ** -23 * (np.abs(v).T @ np.abs(x)), torch.float32)
+    y.fill_(7.0)
+    p.fill_(7.0)
+    assert all(bool((part == 7).all()) for part in buf.split(1 << 28))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D,H", [(300, 70), (300, 700), (640, 47), (1200, 70)])
+def test_scales_that_quantising_does_not_give(ctx, dtype, D, H):
+    """A scale of 2^-127 to 2^113, and NaN: a value below 2^-126 may count as zero, which moves a sum by as much times the other factor."""
+    rng = np.random.default_rng(D)
+    n, at = 40, R.code_bytes(D)
+    rows, w = _rows(rng, n, D), _rows(rng, H, D, D ** -0.5)
+    rows[0, at:at + 2] = 0
+    rows[1, at + 1] = 255
+    rows[2, at] = 240
+    rows[3, at:at + 3] = (1, 2, 3)
+    rows[4, at:at + 3] = (9, 127, 0)
+    w[5, at:at + 2] = 0
+    w[6, at + 2] = 255
+    xd, wd = _dev(rows), _dev(w)
+    x, wv = R.values(rows, D), R.values(w, D)
+    y = spp.fp8_product(ctx, xd, wd, D, dtype=dtype)
+    assert y[1].isnan().all() and y[:, 6].isnan().all()
+    keep, cols = np.arange(n) != 1, np.arange(H) != 6
+    x, wv = x[keep], wv[cols]
+    want, bound = R.sums(x, wv, _bits(dtype))
+    lost = 2.0 ** -126 * (np.abs(wv).sum(1)[None] + np.abs(x).sum(1)[:, None])
+    _close(y.cpu()[keep][:, cols], want, bound + lost + 2.0 ** -126, dtype)
+    v = torch.from_numpy(rng.standard_normal((n, H))).to(dtype)
+    v[1] = 0
+    clean = rows.copy()
+    clean[1] = 0
+    g = spp.fp8_weight_grad(ctx, [(_dev(clean), n, None, v.to(DEV))], H, D)[0]
+    v = v.double().numpy()
+    x = R.values(clean, D)
+    _close(g, v.T @ x, 3 * n * 2.0 ** -23 * (np.abs(v).T @ np.abs(x)) + 2.0 ** -126 * (1 + np.abs(v).sum(0)[:, None]), torch.float32)
+
+
+def test_the_same_rows_under_several_matrices_and_in_several_lists(ctx):
+    """One hidden matrix, a list for each of five groups, and the same list three times: as separate calls."""
+    rng = np.random.default_rng(21)
+    n, D, H, G = 333, 160, 70, 5
+    xd, w = _dev(_rows(rng, n, D)), _dev(_rows(rng, G * 2 * H, D, D ** -0.5)).view(G, 2 * H, -1)
+    groups = [0, 1, 2, 3, 4, 2, 2]
+    y = [torch.zeros(n, H, dtype=torch.bfloat16, device=DEV) for _ in groups]
+    dy = [torch.randn(n, H, device=DEV).to(torch.bfloat16) for _ in groups]
+    p = [torch.zeros(n, 2 * H, dtype=torch.bfloat16, device=DEV) for _ in groups]
+    spp.fp8_gated_multi(ctx, [(xd, n, None, v, g) for v, g in zip(y, groups)], w, D)
+    spp.fp8_gated_grad(ctx, [(xd, n, None, v, g) for v, g in zip(dy, groups)], [(xd, n, None, v, g) for v, g in zip(p, groups)], w, D)
+    one = torch.empty(n, 2 * H, dtype=torch.bfloat16, device=DEV)
+    for j, g in enumerate(groups):
+        assert torch.equal(y[j], spp.fp8_gated(ctx, xd, w[g].contiguous(), D))
+        spp.fp8_gated_grad(ctx, [(xd, n, None, dy[j])], [(xd, n, None, one)], w[g].contiguous(), D)
+        assert torch.equal(p[j], one)
+    dw = spp.fp8_weight_grad(ctx, [(xd, n, None, v, g) for v, g in zip(p, groups)], 2 * H, D, groups=G)
+    x = R.values(xd.cpu().numpy(), D)
+    for g in range(G):
+        v = np.concatenate([p[j].double().cpu().numpy() for j in range(len(groups)) if groups[j] == g])
+        xs = np.concatenate([x] * groups.count(g))
+        _close(dw[g], v.T @ xs, 3 * len(v) * 2.0 ** -23 * (np.abs(v).T @ np.abs(xs)), torch.float32)
+
+
+def test_two_contexts_at_once(ctx):
+    """Two streams work at the same time, each context with a workspace of its own: as one after the other."""
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    cs = [spp.Context(0, s) for s in sides]
+    n, D, H = 30000, 200, 150
+    x = [torch.randn(n, D, device=DEV) for _ in cs]
+    wf = [torch.randn(2 * H, D, device=DEV) * D ** -0.5 for _ in cs]
+    dy = torch.randn(n, H, device=DEV)
+    def step(c, k, dp):
+        rows, w = spp.fp8_quantize(c, x[k], sync=False), spp.fp8_quantize(c, wf[k], sync=False)
+        y = spp.fp8_gated(c, rows, w, D, dtype=torch.float32, sync=False)
+        spp.fp8_gated_grad(c, [(rows, n, None, dy)], [(rows, n, None, dp)], w, D, sync=False)
+        return rows, w, y, dp, spp.fp8_weight_grad(c, [(rows, n, None, dp)], 2 * H, D, sync=False)
+    torch.cuda.synchronize()
+    want = []
+    for k in range(2):
+        want.append(step(ctx, k, torch.empty(n, 2 * H, device=DEV)))
+        ctx.sync()
+    dps = [torch.empty(n, 2 * H, device=DEV) for _ in range(8)]
+    torch.cuda.synchronize()
+    got = [step(cs[j % 2], j % 2, dps[j]) for j in range(8)]
+    for s in sides:
+        s.synchronize()
+    for j, g in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(g, want[j % 2]))
+    for c in cs:
+        c.close()
