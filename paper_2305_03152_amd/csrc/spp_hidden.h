@@ -248,24 +248,30 @@ __device__ __forceinline__ V buffer_load(__amdgpu_buffer_rsrc_t from, uint32_t a
 }
 
 // A tile of a matrix of results by way of such a buffer: 16 RN rows, of which `here` are there, and of each N columns from h0 + N m on.
-// Whole vectors where these are aligned and end with the row or before, else element by element.  All of it is branches that a whole
-// wavefront takes: where a kernel's values fill the registers the compiler (of ROCm 7.2) has copied some of them at the end of a masked
-// piece of code before it restored the mask, and the lanes that were masked out lost theirs.
-template <class T, int RN, int N>
+// Whole vectors where all begin at multiples of four bytes, which is all that the instructions ask for; the last columns of a row where they
+// are no whole vector, and 16-bit matrices at odd places, go element by element (1M rows 172 -> 86, every column by element: gated layer in
+// fp32 212 us, its gradient 477; so 174 and 360).  All of it is branches that a whole wavefront takes: where a kernel's values fill the
+// registers the compiler (of ROCm 7.2) has copied some of them at the end of a masked piece of code before it restored the mask, and the
+// lanes that were masked out lost theirs.
+template <class T, int RN, int N, bool Whole = false>        // Whole: the caller knows that all are whole vectors
 struct Tile {
     typedef T V __attribute__((ext_vector_type(N)));
     __amdgpu_buffer_rsrc_t at;
     uint32_t step;               // bytes from a row to the next
-    int      h, H;
-    bool     whole;
+    int      h0, h, H;
+    int      single;             // columns from this one on go element by element
+    int      last;               // of the tile's
     uint32_t first;              // the lane's first element
     // `front`: columns of the matrix before these `columns`; a row has `all`
     __device__ __forceinline__ Tile(const T* y, int64_t ld, int64_t r0, int here, int h0, int front, int columns, int all) {
         step = (uint32_t)ld * (uint32_t)sizeof(T);
         at = rows_buffer(y + r0 * ld, (uint32_t)(here - 1) * step + (uint32_t)all * (uint32_t)sizeof(T));
         h = h0 + N * (lane_id() & 15);
+        this->h0 = h0;
         H = columns;
-        whole = columns % N == 0 && ((uint32_t)(uintptr_t)y | step | (uint32_t)(front * (int)sizeof(T))) % sizeof(V) == 0;
+        const bool vectors = sizeof(T) == 4 || N == 1 || ((uint32_t)(uintptr_t)y | step | (uint32_t)(front * (int)sizeof(T))) % 4 == 0;
+        single = Whole ? columns : vectors ? columns / N * N : 0;
+        last = h0 + 16 * N < columns ? h0 + 16 * N : columns;
         first = 4 * (uint32_t)(lane_id() >> 4) * step + (uint32_t)(front + h) * (uint32_t)sizeof(T);
     }
     template <class Use> __device__ __forceinline__ void each(Use use) const {
@@ -276,25 +282,26 @@ struct Tile {
     }
     // v(c, n): column n of the lane's rows of the c-th sixteen
     template <int Kind = 0, class Get> __device__ __forceinline__ void put(Get v) const {
-        if (whole) {
-            const uint32_t from = h < H ? first : kNowhere;
+        if (Whole || single > h0) {
+            const uint32_t from = h < single ? first : kNowhere;
             each([&](int c, int i, uint32_t row) {
                 V x;
 #pragma unroll
                 for (int n = 0; n < N; ++n) x[n] = (T)v(c, n)[i];
                 buffer_store<Kind>(x, at, from + row);
             });
-        } else {
+        }
+        if (!Whole && single < last) {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const uint32_t from = h + n < H ? first + n * (uint32_t)sizeof(T) : kNowhere;
+                const uint32_t from = h >= single && h + n < H ? first + n * (uint32_t)sizeof(T) : kNowhere;
                 each([&](int c, int i, uint32_t row) { buffer_store<Kind>((T)v(c, n)[i], at, from + row); });
             }
         }
     }
     __device__ __forceinline__ void get(f32x4 (&v)[RN][N]) const {
-        if (whole) {
-            const uint32_t from = h < H ? first : kNowhere;
+        if (Whole || single >= last) {
+            const uint32_t from = h < single ? first : kNowhere;
             each([&](int c, int i, uint32_t row) {
                 const V x = buffer_load<V>(at, from + row);
 #pragma unroll

@@ -117,13 +117,15 @@ __global__ void __launch_bounds__(kTileBlock) hidden_tile_kernel(HiddenArgs a) {
 // the result 64 at a time (64 of the gate's and the same 64 of the other factor); a workgroup's wavefronts share W and wait for each other only
 // where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.
 constexpr int kHeldWaves = 8, kHeldBlock = 64 * kHeldWaves;
+// Bytes of a row of W in LDS: codes, zeros up to whole steps, scales; or values (bf16, exact), decoded on their way there.
+template <int KS, bool Values> constexpr int held_row() { return (Values ? 256 : 128) * KS + kLdsPad; }
 // How results leave: rows that begin with a line each straight from registers past the L2, others by way of LDS, or straight too.
 enum HeldOut { kLines, kRagged, kStraight };
-template <class T, int Mode, int KS, int RN, int Out>
+template <class T, int Mode, int KS, int RN, int Out, bool Values>
 __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int TB = kHeldWaves * 16 * RN, MR = Mode == kProduct ? 64 : 128;       // rows of X per workgroup, rows of W per 64 columns
-    constexpr int kLs = 128 * KS + kLdsPad;            // bytes of a row of W in LDS: codes, zeros up to whole steps, scales
+    constexpr int kLs = held_row<KS, Values>();
     constexpr bool kExact = sizeof(T) == 4, kAhead = KS * RN <= (kExact && (Mode == kGatedGrad || KS > 2) ? 2 : 4);
     const Lists lists(a.t, TB);
     const int total = lists.total(), groups = group_of_lane(a.t);
@@ -176,12 +178,13 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
         const int64_t r0 = it.r0 + wave * 16 * RN;
         if (group != held_group || t0 != held_from) {
             const uint8_t* w = a.w + (int64_t)group * a.H * (MR / 64) * a.rb;
-            constexpr uint32_t lv = kLs / 16;
+            constexpr uint32_t lv = Values ? 8 * KS : kLs / 16;
             const uint32_t all = (uint32_t)(t1 - t0) * MR * lv;
             __syncthreads();
             // eight vectors of a thread under way together
             for (uint32_t i0 = threadIdx.x; i0 < all; i0 += 8 * kHeldBlock) {
                 u32x4 v[8];
+                uint8_t scale[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const uint32_t i = i0 + k * kHeldBlock < all ? i0 + k * kHeldBlock : all - 1;
@@ -192,10 +195,22 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
                     const int at = c >= 8 * KS ? a.cb : 16 * (int)c;
                     v[k] = *reinterpret_cast<const u32x4*>(from + (c >= 8 * KS || at < a.cb ? at : 0));
                     if (c < 8 * KS && at >= a.cb) v[k] = u32x4{0, 0, 0, 0};
+                    if constexpr (Values) scale[k] = from[a.cb + (int)(c / 8)];
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (i0 + k * kHeldBlock < all) reinterpret_cast<u32x4*>(lds)[i0 + k * kHeldBlock] = v[k];
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t i = i0 + k * kHeldBlock;
+                    if (i >= all) continue;
+                    if constexpr (Values) {          // a step's 16-byte pieces in the order in which lanes take them: of four quarters the first, ..
+                        const uint32_t r = i / lv, c = i - r * lv;
+                        uint8_t* to = lds + r * kLs + 256 * (c / 8) + 128 * (c / 4 & 1) + 16 * (c & 3);
+                        const float s = mx4_scale(scale[k]);
+                        *reinterpret_cast<bf16x8*>(to) = eight_of(v[k].x, v[k].y, s);
+                        *reinterpret_cast<bf16x8*>(to + 64) = eight_of(v[k].z, v[k].w, s);
+                    } else {
+                        reinterpret_cast<u32x4*>(lds)[i] = v[k];
+                    }
+                }
             }
             held_group = group; held_from = t0;
             __syncthreads();
@@ -210,6 +225,13 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
                 x[s][c].hi = at + 64 < a.cb ? ahead[s][c][1] : u32x4{0, 0, 0, 0};
                 x[s][c].scale = ahead_scale[s / 4][c];
             }
+        Decoded xd[Values ? KS : 1][RN];
+        if constexpr (Values)
+            steps_of<KS>([&](auto step) {
+                constexpr int s = decltype(step)::value;
+#pragma unroll
+                for (int c = 0; c < RN; ++c) xd[s][c] = decode<(s & 3)>(x[s][c]);
+            });
         if (kAhead && item + share.step < share.end) { it = find(item + share.step); ask_rows(it); }
         if (mine <= 0) continue;
         const int rows = mine < 16 * RN ? mine : 16 * RN;
@@ -230,7 +252,7 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
             const uint8_t* tile_w = lds + (t - t0) * MR * kLs;
             f32x4 dy[RN][4];
             if constexpr (Mode == kGatedGrad) {
-                Tile<T, RN, 4>(res.y, res.ld, r0, rows, 64 * t, 0, a.H, a.H).get(dy);
+                Tile<T, RN, 4, Out == kLines>(res.y, res.ld, r0, rows, 64 * t, 0, a.H, a.H).get(dy);
             }
             f32x4 acc[MR / 64][RN][4];
 #pragma unroll
@@ -241,26 +263,39 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
                     for (int f = 0; f < 4; ++f) acc[k][c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
                 steps_of<KS>([&](auto step) {
                     constexpr int s = decltype(step)::value;
-                    Operand w[4];
+                    if constexpr (Values) {
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        const uint8_t* p = tile_w + (64 * k + 16 * f + m) * kLs;
-                        w[f].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
-                        w[f].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
-                        w[f].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
+                        for (int f = 0; f < 4; ++f) {
+                            const uint8_t* p = tile_w + (64 * k + 16 * f + m) * kLs + 256 * s + 16 * q;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const bf16x8 w = *reinterpret_cast<const bf16x8*>(p + 64 * j);
+#pragma unroll
+                                for (int c = 0; c < RN; ++c) acc[k][c][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xd[s][c].v[j], w, acc[k][c][f], 0, 0, 0);
+                            }
+                        }
+                    } else {
+                        Operand w[4];
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) {
+                            const uint8_t* p = tile_w + (64 * k + 16 * f + m) * kLs;
+                            w[f].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
+                            w[f].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
+                            w[f].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
+                        }
+                        multiply<kExact, (s & 3)>(acc[k], x[s], w);
                     }
-                    multiply<kExact, (s & 3)>(acc[k], x[s], w);
                 });
             }
 #pragma unroll
             for (int c = 0; c < RN; ++c) combine<Mode>(a.act, acc[0][c], acc[MR / 64 - 1][c], dy[c]);
             if constexpr (Mode == kGatedGrad) {
-                constexpr int kind = Out == kLines ? kPastL2 : 0;
-                Tile<T, RN, 4>(res.p, res.pld, r0, rows, 64 * t, 0, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
-                Tile<T, RN, 4>(res.p, res.pld, r0, rows, 64 * t, a.H, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[1][c][n]; });
+                                constexpr int kind = Out == kLines ? kPastL2 : 0;
+                Tile<T, RN, 4, Out == kLines>(res.p, res.pld, r0, rows, 64 * t, 0, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
+                Tile<T, RN, 4, Out == kLines>(res.p, res.pld, r0, rows, 64 * t, a.H, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[1][c][n]; });
             } else if constexpr (Out != kRagged) {
                 constexpr int kind = Out == kLines ? kPastL2 : 0;
-                Tile<T, RN, 4>(y, ld, r0, rows, 64 * t, 0, a.H, a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
+                Tile<T, RN, 4, Out == kLines>(y, ld, r0, rows, 64 * t, 0, a.H, a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
             } else {
                 out.put(t - t0, acc[0]);
                 if (!out.run) out.flush_lines(t - t0, t == t0, t + 1 == t1);
@@ -272,14 +307,14 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
 
 constexpr int kHeldLds = 163840;         // all of a CU's
 constexpr int kHeldRowOut = 768;         // bytes of rows that go out in one run
-template <class T, int Mode, int KS, int RN, int Out>
-static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
+template <class T, int Mode, int KS, int RN, int Out, bool Values>
+static int launch_held_as(spp_ctx* ctx, HiddenArgs& a, bool* done) {
     constexpr int MR = Mode == kProduct ? 64 : 128, TB = kHeldWaves * 16 * RN;
-    auto kernel = hidden_held_kernel<T, Mode, KS, RN, Out>;
+    auto kernel = hidden_held_kernel<T, Mode, KS, RN, Out, Values>;
     const int ht = (a.H + 63) / 64, row = a.H * (int)sizeof(T);
     a.out_lds = Out != kRagged ? 0 : 16 * RN * RowsOut<T, RN>::kPitch;
     if (Out == kRagged && row <= kHeldRowOut && a.out_lds < 16 * RN * row + 16) a.out_lds = 16 * RN * row + 16;
-    const int64_t need = (int64_t)ht * MR * (128 * KS + kLdsPad), most_lds = kHeldLds - (int64_t)kHeldWaves * a.out_lds;
+    const int64_t need = (int64_t)ht * MR * held_row<KS, Values>(), most_lds = kHeldLds - (int64_t)kHeldWaves * a.out_lds;
     *done = need <= most_lds;
     if (!*done) return SPP_OK;
     a.w_lds = (int)need;
@@ -295,39 +330,71 @@ static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
+// Whether W is held as values: in fp32, where the code that decodes a row of W for 16 RN rows of X takes longer than its products, of the
+// gated layer, and of the product where RN is 1; not for few rows, which have W but once.  200k rows in fp32, W as codes and as values: gated 172 -> 100
+// 65 and 54 us, 128 -> 256 85 and 71, 512 -> 64 56 and 49; the product 172 -> 100 38 and 33, 300 -> 86 43 and 40, with two sixteens 100 -> 64 18
+// and 20; the gated gradient 172 -> 100 110 both.
+template <class T, int Mode, int KS, int RN, int Out>
+static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool few, bool* done) {
+    if constexpr (sizeof(T) == 4 && KS <= 4 && ((Mode == kGated && (RN == 2 || KS > 2)) || (Mode == kProduct && RN == 1 && (Out == kRagged || KS > 2)))) {
+        if (!few) SPP_TRY((launch_held_as<T, Mode, KS, RN, Out, true>(ctx, a, done)));
+        if (*done) return SPP_OK;
+    }
+    return launch_held_as<T, Mode, KS, RN, Out, false>(ctx, a, done);
+}
 template <class T, int Mode>
 static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
-    // rows that begin with a line each are stored as they come, 128 or 256 bytes of a row at a time
-    bool lines = Mode != kGatedGrad || a.H * sizeof(T) % 128 == 0;
+    // rows of whole vectors that begin with a line each are stored as they come, 128 or 256 bytes of a row at a time
+    bool lines = Mode == kGatedGrad ? a.H * sizeof(T) % 128 == 0 : a.H % 4 == 0;
+    int64_t pairs = 0;                                   // tiles of two sixteens
     for (int j = 0; j < a.t.n_lists; ++j) {
         void* const y = Mode == kGatedGrad ? a.dp[j] : a.t.y[j];
         const int64_t ld = Mode == kGatedGrad ? a.dp_ld[j] : a.t.ld[j];
         lines = lines && ((uintptr_t)y | (uint64_t)(ld * (int64_t)sizeof(T))) % 128 == 0;
+        if (Mode == kGatedGrad) lines = lines && ((uintptr_t)a.t.y[j] | (uint64_t)(a.t.ld[j] * (int64_t)sizeof(T))) % 4 == 0;       // dY
+        pairs += (a.t.n[j] + 32 * kHeldWaves - 1) / (32 * kHeldWaves);
     }
+    // Few rows: tiles of two sixteens and 64 columns are no more than there are CUs.  One sixteen then: 16k rows 256 -> 256 in bf16 9.1 and 7.3 us,
+    // gated 11.2 and 9.5, its gradient 15.7 and 12.7; 24k, which are more tiles, 8.2 and 8.8, 11.6 and 13.0, 17.1 and 18.4.
+    const bool few = pairs * ((a.H + 63) / 64) <= ctx->num_cu;
     auto with = [&](auto steps) {
         constexpr int KS = decltype(steps)::value;
-        constexpr int RN = KS <= 2 ? 2 : 1;
+        auto put = [&](auto out) {
+            constexpr int Out = decltype(out)::value;
+            if constexpr (KS <= 2) {
+                if (!few) return launch_held<T, Mode, KS, 2, Out>(ctx, a, few, done);
+            }
+            return launch_held<T, Mode, KS, 1, Out>(ctx, a, few, done);
+        };
         if constexpr (KS > 6 && sizeof(T) == 4) {
             return (int)SPP_OK;                              // (registers)
         } else if constexpr (KS > 4) {
             // with few columns most wavefronts of the other form would have none: 200k rows 1024 -> 24 68 and 56 us, 640 -> 47 49 and 39; of 16 bits
             // 640 -> 128 42 and 49, of 32 85 and 72
             if (sizeof(T) == 2 && a.H > 64) return (int)SPP_OK;
-            return launch_held<T, Mode, KS, RN, kStraight>(ctx, a, done);
+            return launch_held<T, Mode, KS, 1, kStraight>(ctx, a, few, done);
         } else if (lines) {
-            return launch_held<T, Mode, KS, RN, kLines>(ctx, a, done);
-        } else if constexpr (Mode != kProduct) {
+            return put(std::integral_constant<int, kLines>());
+        } else if constexpr (Mode == kGatedGrad) {
+            // One sixteen: with two, what the CUs have under way is more than the L2 holds, and lines that two stores share leave it in between.
+            // 1M rows with two and one in bf16 172 -> 100 290 and 249 us, 100 -> 172 456 and 422, in fp32 455 and 438, 711 and 681; 16k 172 -> 100 16 and
+            // 12, 19 and 16.  But two where these are one tile a CU and one sixteen would be a few more: 40k 17.5 and 22, 24 and 30, 64k 21 and 27, 27 and 39
+            if constexpr (KS <= 2) {
+                if (2 * pairs > ctx->num_cu && pairs <= ctx->num_cu) return launch_held<T, Mode, KS, 2, kStraight>(ctx, a, few, done);
+            }
+            return launch_held<T, Mode, KS, 1, kStraight>(ctx, a, few, done);
+        } else if constexpr (Mode == kGated) {
             // beside two products the LDS that rows need is worth more to W and to a second sixteen rows of X (1M rows 172 -> 100 in bf16 by way of
             // LDS 163 us, so 115; in fp32 235 and 193)
-            return launch_held<T, Mode, KS, RN, kStraight>(ctx, a, done);
+            return put(std::integral_constant<int, kStraight>());
         } else {
             // 300k rows 256 -> 86, -> 172 in bf16 with one sixteen 40 and 44 us, with two 31 and 38; 128 -> 86 in fp32 41 and 34, in bf16 24 and 26
-            // (and two steps in fp32 fill the registers)
+            // (and two steps in fp32 fill the registers); straight from registers, 1M rows 172 -> 100 in bf16 95 us and so 87, 128 -> 250 226 and 145
             if constexpr (KS == (sizeof(T) == 4 ? 1 : 2)) {
-                SPP_TRY((launch_held<T, Mode, KS, 2, kRagged>(ctx, a, done)));
+                if (!few) SPP_TRY((launch_held<T, Mode, KS, 2, kRagged>(ctx, a, few, done)));
                 if (*done) return (int)SPP_OK;
             }
-            return launch_held<T, Mode, KS, 1, kRagged>(ctx, a, done);
+            return launch_held<T, Mode, KS, 1, kRagged>(ctx, a, few, done);
         }
     };
     switch (a.steps) {

@@ -595,3 +595,23 @@ def test_two_contexts_at_once(ctx):
         assert all(torch.equal(a, b) for a, b in zip(g, want[j % 2]))
     for c in cs:
         c.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,H", [(172, 100), (100, 86), (128, 256), (300, 47), (500, 64)])
+def test_the_same_bits_for_few_rows_and_for_many(ctx, dtype, D, H):
+    """A row's results do not depend on how many other rows the call has, whatever form its kernel takes for them."""
+    rng = np.random.default_rng(D + H)
+    n = 70000
+    xd, w = _dev(_rows(rng, 4096, D)), _dev(_rows(rng, 2 * H, D, D ** -0.5))
+    xd = xd.repeat(-(-n // 4096), 1)[:n].contiguous()
+    dy = torch.randn(n, H, generator=torch.Generator(DEV).manual_seed(1), device=DEV).to(dtype)
+    def results(count):
+        dp = torch.full((count, 2 * H), float("nan"), dtype=dtype, device=DEV)
+        spp.fp8_gated_grad(ctx, [(xd[:count], count, None, dy[:count])], [(xd[:count], count, None, dp)], w, D)
+        return spp.fp8_product(ctx, xd[:count], w[:H], D, dtype=dtype), spp.fp8_gated(ctx, xd[:count], w, D, dtype=dtype), dp
+    want = results(n)
+    assert not any(bool(t.isnan().any()) for t in want)
+    for count in (1, 3, 100, 4000, 20000, 40000, 66000):
+        for got, t in zip(results(count), want):
+            assert torch.equal(got, t[:count]), count
