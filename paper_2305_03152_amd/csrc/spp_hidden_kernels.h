@@ -12,8 +12,9 @@ constexpr int kLdsPad = 32;
 
 // ---- W and X in LDS --------------------------------------------------------------------------------
 
-// The form for rows of any length.  A workgroup takes 128 rows of X by 128 columns: of the product, or 64 of the gate's and the same 64 of the other factor.  Steps of 128
-// columns of X and W go through LDS, the next asked for while one is multiplied.
+// The form for rows of any length.  A workgroup takes 128 rows of X by 128 columns: of the product, or 64 of the gate's and the same 64 of the other
+// factor.  Steps of 128 columns of X and W go through LDS, the next asked for while one is multiplied: bound by that turn, a wait and a barrier a
+// step.  In bf16 300k rows 1100 -> 256 385 us, 440 TFLOP/s; 50k 4096 -> 256 292, gated 473.
 constexpr int kTileRows = 128, kTileBlock = 256, kTileLd = kFp8Block + kLdsPad;
 constexpr int kTileBuffer = 2 * kTileRows * kTileLd + 2 * kTileRows;       // rows of X, rows of W, their scales
 
@@ -115,7 +116,9 @@ __global__ void __launch_bounds__(kTileBlock) hidden_tile_kernel(HiddenArgs a) {
 
 // The form for weights that LDS holds.  A wavefront keeps its 16 RN rows of X in registers, all columns of them, and goes over the columns of
 // the result 64 at a time (64 of the gate's and the same 64 of the other factor); a workgroup's wavefronts share W and wait for each other only
-// where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.
+// where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.  Bound by HBM for many rows: 2.5M rows
+// 256 -> 256 in bf16 390 us, 5.0 TB/s, which the same reads and writes without the products take too; the gated layer, whose activation keeps the
+// vector pipe busy half the time, 446, its gradient 925 (4.9 TB/s; without arithmetic 885).  In fp32 the product 658, the gated layer 798.
 constexpr int kHeldWaves = 8, kHeldBlock = 64 * kHeldWaves;
 // Bytes of a row of W in LDS: codes, zeros up to whole steps, scales; or values (bf16, exact), decoded on their way there.
 template <int KS, bool Values> constexpr int held_row() { return (Values ? 256 : 128) * KS + kLdsPad; }
@@ -417,6 +420,8 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
 // W is read once per workgroup, and per product half as much from LDS as with X in registers and W in LDS.  The workgroups that have the same
 // rows and other columns share an XCD's L2 and take the rows in the same order at the same time.  With one wavefront per SIMD nothing else
 // works while it waits, so that a tile's work is one piece of code without branches, the next tile's way to LDS in the middle of its products.
+// Bound by the matrix pipe, its waits for LDS and a clock that it lowers: 380k rows 1024 -> 1024 in bf16 394 us, 2.0 PFLOP/s, gated to 512 428; in fp32
+// 832 and 842, by the decoding beside it.
 // Rows of X at a time, in sixteens: one where the registers would not hold what two need.  No kernel here may spill registers: the compiler (of
 // ROCm 7.2) has lost some of those that it had to put away where a kernel fills all 512.
 template <int Mode, int KS> constexpr int kWideRows = Mode == kGatedGrad && KS == 8 ? 1 : 2;
@@ -544,7 +549,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
 #pragma unroll
             for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
         // The next tile goes to LDS and the one behind it is asked for during the products.  One wavefront per SIMD also reads each step's rows
-        // before the products of the step before; the compiler, short of registers, would put every load right before its use (390k rows
+        // before the products of the step before; the compiler, short of registers, would put every load right before its use (380k rows
         // 1024 -> 1024 490 us, 400 so).
         constexpr bool kOrdered = WAVES == 4;
         Operand xv[kOrdered ? 2 : 1][RN];
