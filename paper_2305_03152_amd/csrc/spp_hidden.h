@@ -299,21 +299,25 @@ struct Tile {
             }
         }
     }
-    __device__ __forceinline__ void get(f32x4 (&v)[RN][N]) const {
+    // Asked for, and the values of what came: where the compiler may not move code, the first use is what waits.
+    __device__ __forceinline__ void ask(V (&x)[RN][4]) const {
         if (Whole || single >= last) {
             const uint32_t from = h < single ? first : kNowhere;
-            each([&](int c, int i, uint32_t row) {
-                const V x = buffer_load<V>(at, from + row);
-#pragma unroll
-                for (int n = 0; n < N; ++n) v[c][n][i] = (float)x[n];
-            });
+            each([&](int c, int i, uint32_t row) { x[c][i] = buffer_load<V>(at, from + row); });
         } else {
+            each([&](int c, int i, uint32_t row) {
+                struct { T v[N]; } e;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const uint32_t from = h + n < H ? first + n * (uint32_t)sizeof(T) : kNowhere;
-                each([&](int c, int i, uint32_t row) { v[c][n][i] = (float)buffer_load<T>(at, from + row); });
-            }
+                for (int n = 0; n < N; ++n) e.v[n] = buffer_load<T>(at, (h + n < H ? first + n * (uint32_t)sizeof(T) : kNowhere) + row);
+                x[c][i] = __builtin_bit_cast(V, e);
+            });
         }
+    }
+    static __device__ __forceinline__ void values(const V (&x)[4], f32x4 (&v)[N]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n][i] = (float)x[i][n];
     }
 };
 // Whether a tile's rows span what a buffer can.

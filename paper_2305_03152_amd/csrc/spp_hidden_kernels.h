@@ -253,10 +253,9 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
         }
         for (int t = t0; t < t1; ++t) {
             const uint8_t* tile_w = lds + (t - t0) * MR * kLs;
-            f32x4 dy[RN][4];
-            if constexpr (Mode == kGatedGrad) {
-                Tile<T, RN, 4, Out == kLines>(res.y, res.ld, r0, rows, 64 * t, 0, a.H, a.H).get(dy);
-            }
+            typedef Tile<T, RN, 4, Out == kLines> Rows;
+            typename Rows::V raw[RN][4];
+            if constexpr (Mode == kGatedGrad) Rows(res.y, res.ld, r0, rows, 64 * t, 0, a.H, a.H).ask(raw);
             f32x4 acc[MR / 64][RN][4];
 #pragma unroll
             for (int k = 0; k < MR / 64; ++k) {
@@ -291,14 +290,18 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
                 });
             }
 #pragma unroll
-            for (int c = 0; c < RN; ++c) combine<Mode>(a.act, acc[0][c], acc[MR / 64 - 1][c], dy[c]);
+            for (int c = 0; c < RN; ++c) {
+                f32x4 dy[4];
+                if constexpr (Mode == kGatedGrad) Rows::values(raw[c], dy);
+                combine<Mode>(a.act, acc[0][c], acc[MR / 64 - 1][c], dy);
+            }
             if constexpr (Mode == kGatedGrad) {
                                 constexpr int kind = Out == kLines ? kPastL2 : 0;
-                Tile<T, RN, 4, Out == kLines>(res.p, res.pld, r0, rows, 64 * t, 0, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
-                Tile<T, RN, 4, Out == kLines>(res.p, res.pld, r0, rows, 64 * t, a.H, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[1][c][n]; });
+                Rows(res.p, res.pld, r0, rows, 64 * t, 0, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
+                Rows(res.p, res.pld, r0, rows, 64 * t, a.H, a.H, 2 * a.H).template put<kind>([&](int c, int n) { return acc[1][c][n]; });
             } else if constexpr (Out != kRagged) {
                 constexpr int kind = Out == kLines ? kPastL2 : 0;
-                Tile<T, RN, 4, Out == kLines>(y, ld, r0, rows, 64 * t, 0, a.H, a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
+                Rows(y, ld, r0, rows, 64 * t, 0, a.H, a.H).template put<kind>([&](int c, int n) { return acc[0][c][n]; });
             } else {
                 out.put(t - t0, acc[0]);
                 if (!out.run) out.flush_lines(t - t0, t == t0, t + 1 == t1);
@@ -424,11 +427,11 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
 // 832 and 842, by the decoding beside it.
 // Rows of X at a time, in sixteens: one where the registers would not hold what two need.  No kernel here may spill registers: the compiler (of
 // ROCm 7.2) has lost some of those that it had to put away where a kernel fills all 512.
-template <int Mode, int KS> constexpr int kWideRows = Mode == kGatedGrad && KS == 8 ? 1 : 2;
+template <class T, int Mode, int KS> constexpr int kWideRows = Mode == kGatedGrad && KS == 8 && sizeof(T) == 4 ? 1 : 2;
 template <class T, int Mode, int KS, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    constexpr int RN = kWideRows<Mode, KS>, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
+    constexpr int RN = kWideRows<T, Mode, KS>, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
     constexpr int kLs = 128 * KS + kLdsPad;                   // bytes of a row of X in LDS: codes, zeros up to whole steps, scales
     constexpr int kVec = (TB * (8 * KS + 1) + threads - 1) / threads;
     constexpr bool kExact = sizeof(T) == 4;
@@ -488,9 +491,9 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
             places[k] = (r * (uint32_t)a.rb + 16 * v) | (r * kLs + (v + 1 < per ? 16 * v : 128 * KS)) << 16;
         }
     }
-    struct Piece { int list, here, group; int64_t r0; };
+    struct Piece { int list, here, r0; };
     const uint8_t* x_list = nullptr;                          // of the list of the tile that was asked for last
-    int x_until = at, x_first = 0, x_rows = 0, x_group = 0, x_of = 0;
+    int x_until = at, x_first = 0, x_rows = 0, x_of = 0;
     u32x4 ahead[kVec];
     auto find = [&](int tile) {                               // behind the last tile the last one again
         tile = tile < end ? tile : end - 1;
@@ -499,18 +502,16 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
             x_first = lists.first_tile(x_of);
             x_until = __builtin_amdgcn_readlane(lists.upto, x_of);
             x_rows = lists.rows_in(x_of);
-            x_group = __builtin_amdgcn_readlane(groups, x_of);
             x_list = a.t.rows[x_of];
         }
         Piece t;
-        t.list = x_of; t.group = x_group;
-        t.r0 = (int64_t)(tile - x_first) * TB;
-        const int64_t left = x_rows - t.r0;
-        t.here = left < TB ? (int)left : TB;
+        t.list = x_of;
+        t.r0 = (tile - x_first) * TB;                         // (below the list's rows, which are at most 2^31 - 1)
+        t.here = x_rows - t.r0 < TB ? x_rows - t.r0 : TB;
         return t;
     };
     auto ask = [&](const Piece& t) {
-        const auto x = rows_buffer(x_list + t.r0 * a.rb, (uint32_t)(t.here * a.rb));
+        const auto x = rows_buffer(x_list + (int64_t)t.r0 * a.rb, (uint32_t)(t.here * a.rb));
 #pragma unroll
         for (int k = 0; k < kVec; ++k) ahead[k] = __builtin_amdgcn_raw_buffer_load_b128(x, (int)(places[k] & 0xFFFF), 0, 0);
     };
@@ -522,27 +523,29 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
     ask(now);
     __syncthreads();
     keep(lds);
-    hold(now.group);
+    hold(__builtin_amdgcn_readlane(groups, now.list));
     Piece next = find(at + step);
     ask(next);
     int out_list = -1;
     T *y = nullptr, *p = nullptr;                             // the list's Y and dP
-    int64_t ld = 0, pld = 0;
+    int ld = 0, pld = 0;                                      // (32 rows are below 2^31 bytes)
     for (int tile = at, j = 0; tile < end; tile += step, ++j) {
         __syncthreads();                                      // this tile is in LDS, and the one before has been read by all
-        if (now.group != held_group) hold(now.group);
         if (now.list != out_list) {
+            const int group = __builtin_amdgcn_readlane(groups, now.list);
+            if (group != held_group) hold(group);
             out_list = now.list;
             y = static_cast<T*>(a.t.y[now.list]);
-            ld = a.t.ld[now.list];
-            if constexpr (Mode == kGatedGrad) { p = static_cast<T*>(a.dp[now.list]); pld = a.dp_ld[now.list]; }
+            ld = (int)a.t.ld[now.list];
+            if constexpr (Mode == kGatedGrad) { p = static_cast<T*>(a.dp[now.list]); pld = (int)a.dp_ld[now.list]; }
         }
         const Piece after = find(tile + 2 * step);
         const uint8_t* x = lds + (j & 1) * buffer;
         uint8_t* const other = lds + (~j & 1) * buffer;
         constexpr int N = cols / 16;                          // columns of a lane
-        f32x4 dy[RN][N];
-        if constexpr (Mode == kGatedGrad) Tile<T, RN, N>(y, ld, now.r0, now.here, h0, 0, a.H, a.H).get(dy);
+        typedef Tile<T, RN, N> Rows;
+        typename Rows::V raw[RN][4];
+        if constexpr (Mode == kGatedGrad) Rows(y, ld, now.r0, now.here, h0, 0, a.H, a.H).ask(raw);
         f32x4 acc[RN][4];
 #pragma unroll
         for (int c = 0; c < RN; ++c)
@@ -553,6 +556,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
         // 1024 -> 1024 490 us, 400 so).
         constexpr bool kOrdered = WAVES == 4;
         Operand xv[kOrdered ? 2 : 1][RN];
+        uint32_t scales[kOrdered ? 2 : 1][RN];                // of four steps
         auto read = [&](auto index) {
             constexpr int s = decltype(index)::value;
 #pragma unroll
@@ -560,7 +564,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
                 const uint8_t* p = x + (16 * c + m) * kLs;
                 xv[kOrdered ? s & 1 : 0][c].lo = *reinterpret_cast<const u32x4*>(p + 128 * s + 16 * q);
                 xv[kOrdered ? s & 1 : 0][c].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
-                xv[kOrdered ? s & 1 : 0][c].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
+                if constexpr (s % 4 == 0) scales[kOrdered ? s / 4 & 1 : 0][c] = *reinterpret_cast<const uint32_t*>(p + 128 * KS + s);
             }
         };
         if constexpr (kOrdered) read(std::integral_constant<int, 0>());
@@ -569,6 +573,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
             if constexpr (!kOrdered) read(index);
             else if constexpr (s + 1 < KS) read(std::integral_constant<int, s + 1>());
             if (kOrdered) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int c = 0; c < RN; ++c) xv[kOrdered ? s & 1 : 0][c].scale = scales[kOrdered ? s / 4 & 1 : 0][c];
             multiply<kExact, (s & 3)>(acc, xv[kOrdered ? s & 1 : 0], w[s]);
             if (s == (KS > 2 ? 1 : 0)) keep(other);
             if (s == (KS > 2 ? 2 : KS - 1)) ask(after);
@@ -576,14 +582,17 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
         });
 #pragma unroll
         for (int c = 0; c < RN; ++c)
-            if constexpr (Mode != kProduct)
-                combine<Mode>(a.act, reinterpret_cast<f32x4(&)[2]>(acc[c][0]), reinterpret_cast<f32x4(&)[2]>(acc[c][2]), reinterpret_cast<f32x4(&)[2]>(dy[c][0]));
+            if constexpr (Mode != kProduct) {
+                f32x4 dy[N];
+                if constexpr (Mode == kGatedGrad) Rows::values(raw[c], dy);
+                combine<Mode>(a.act, reinterpret_cast<f32x4(&)[2]>(acc[c][0]), reinterpret_cast<f32x4(&)[2]>(acc[c][2]), dy);
+            }
         if constexpr (Mode == kGatedGrad) {
-            Tile<T, RN, N>(p, pld, now.r0, now.here, h0, 0, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][n]; });
-            Tile<T, RN, N>(p, pld, now.r0, now.here, h0, a.H, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][N + n]; });
+            Rows(p, pld, now.r0, now.here, h0, 0, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][n]; });
+            Rows(p, pld, now.r0, now.here, h0, a.H, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][N + n]; });
         } else {
             // whole lines past the L2 (200k rows 256 -> 1024 in bf16: 121 us with plain stores, 79 so)
-            const Tile<T, RN, N> to(y, ld, now.r0, now.here, h0, 0, a.H, a.H);
+            const Rows to(y, ld, now.r0, now.here, h0, 0, a.H, a.H);
             if (Mode == kProduct && (((uint32_t)(uintptr_t)y | to.step) & 127) == 0) to.template put<kPastL2>([&](int c, int n) { return acc[c][n]; });
             else to.put([&](int c, int n) { return acc[c][n]; });
         }
@@ -594,7 +603,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
 
 template <class T, int Mode, int KS, int WAVES>
 static int launch_wide(spp_ctx* ctx, HiddenArgs& a) {
-    constexpr int TB = 16 * kWideRows<Mode, KS>, cols = WAVES * (Mode == kProduct ? 64 : 32);
+    constexpr int TB = 16 * kWideRows<T, Mode, KS>, cols = WAVES * (Mode == kProduct ? 64 : 32);
     auto kernel = hidden_wide_kernel<T, Mode, KS, WAVES>;
     constexpr int lds = 2 * TB * (128 * KS + kLdsPad);
     static LdsLimit limit;
