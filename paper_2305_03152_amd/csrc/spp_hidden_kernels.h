@@ -423,8 +423,8 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
 // W is read once per workgroup, and per product half as much from LDS as with X in registers and W in LDS.  The workgroups that have the same
 // rows and other columns share an XCD's L2 and take the rows in the same order at the same time.  With one wavefront per SIMD nothing else
 // works while it waits, so that a tile's work is one piece of code without branches, the next tile's way to LDS in the middle of its products.
-// Bound by the matrix pipe, its waits for LDS and a clock that it lowers: 380k rows 1024 -> 1024 in bf16 394 us, 2.0 PFLOP/s, gated to 512 428; in fp32
-// 832 and 842, by the decoding beside it.
+// Bound by the matrix pipe, its waits for LDS and a clock that it lowers: 380k rows 1024 -> 1024 in bf16 394 us, 2.0 PFLOP/s, gated to 512 415, its
+// gradient 578; in fp32, by the decoding beside it, 833, 830 and 1240.
 // Rows of X at a time, in sixteens: one where the registers would not hold what two need.  No kernel here may spill registers: the compiler (of
 // ROCm 7.2) has lost some of those that it had to put away where a kernel fills all 512.
 template <class T, int Mode, int KS> constexpr int kWideRows = Mode == kGatedGrad && KS == 8 && sizeof(T) == 4 ? 1 : 2;
