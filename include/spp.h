@@ -466,7 +466,8 @@ int  spp_fp8_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64
  *                    are formed again from the rows, as in the forward pass.  dP must not overlap dY.
  *       weight grad  dW[g] = sum over the lists j of group g of dY_j^T X_j, as spp_mx4_weight_grad in everything else.  With grads and
  *                    2H for H it gives the gradients of Wg and Wu, one behind the other.
- *     X and W are the values that the rows stand for; sums and activations are formed in fp32 and rounded once to Y's type.  The gradient
+ *     X and W are the values that the rows stand for; products are exact, sums and activations are formed in fp32, and what is written is
+ *     rounded once to Y's type, whatever that is.  The gradient
  *     of the rows of a layer is the product of dY (dP) in 8 bits by the transposed weights (of Wg and Wu, one behind the other).
  *     Of rows of other origin a value below 2^-126 may count as 0.
  *     Rows from *d_n on are neither read nor written, nor what lies between rows of Y; recording as in (6). */

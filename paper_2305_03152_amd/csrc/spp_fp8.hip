@@ -3,7 +3,7 @@
 //   block of 128 columns, a = max |x| of what is finite:  e = the smallest integer with a <= 448 2^e, at least -117 and at most 119,
 //   code = nearest E4M3 to x / 2^e, ties to even, 448 for what lies above (of more than 448 2^119 only);  NaN for what is not finite.
 //
-// The scale is a power of two, so that the matrix instructions take it, and rounded up, so that nothing saturates: an E4M3's
+// The scale is a power of two, so that a code under it is exact in bf16, and rounded up, so that nothing saturates: an E4M3's
 // relative step is the same under any scale, and a block has 15 powers of two below its largest value before its steps widen.
 // A block's lanes find its largest value together: sixteen of 8 columns each, of rows of up to 64 and 32 columns eight and four, so
 // that fewer are idle.

@@ -4,12 +4,12 @@
 //   gated        Y_j = act(X_j Wg[g_j]^T) * (X_j Wu[g_j]^T)         W[g] = Wg, then Wu, H rows each
 //   its gradient [dY_j * u * act'(g) | dY_j * act(g)]               g and u formed again from X_j and W[g_j], as in the forward pass
 //
-// Codes are E4M3 and scales powers of two: a product has 8 bits.  Results of 16 bits are formed by the matrix instruction for 8-bit floats,
-// which takes the scales; a code itself is its value rounded by up to 2^-4.  The instruction adds the products of eight neighbouring columns after cutting each off at 2^-13 of the power of two of
-// the largest (measured: beside 2^16 an addend of 2^3 counts and one of 2^2 does not), everything else in fp32: normally distributed rows
-// come out 1.4e-5 off, where rounding the result to bf16 costs 1.7e-3 and to fp16 2e-4.  Results of 32 bits, which would show it, are formed by
-// the bf16 instruction, at half the rate, of values decoded in registers: a code under a scale is exact in bf16, the products are
-// exact and the sums fp32.  The activation is computed in fp32, and what is written is rounded once.
+// Codes are E4M3 and scales powers of two: a code under a scale is exact in bf16, so the
+// values are decoded in registers and multiplied by the bf16 instruction: products are exact, sums fp32, whatever the type of the result.  The
+// instruction for 8-bit floats would take the codes and the scales themselves, at twice the rate, but it adds the products of eight
+// neighbouring columns after cutting each off at 2^-13 of the power of two of the largest (measured: beside 2^16 an addend of 2^3 counts and one of
+// 2^2 does not): where large terms cancel each other, the small ones, which are then the result, are lost.  The activation is computed in
+// fp32, and what is written is rounded once.
 #pragma once
 
 #include "spp_fp8.h"
@@ -57,10 +57,7 @@ struct Operand {
     u32x4 lo, hi;
     uint32_t scale;
 };
-__device__ __forceinline__ i32x8 codes_of(const Operand& o) {
-    return i32x8{(int)o.lo.x, (int)o.lo.y, (int)o.lo.z, (int)o.lo.w, (int)o.hi.x, (int)o.hi.y, (int)o.hi.z, (int)o.hi.w};
-}
-// The values of eight of them.
+// The values of eight of its codes.
 __device__ __forceinline__ bf16x8 eight_of(uint32_t a, uint32_t b, float s) {
     const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false), v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true),
                  v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, false), v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true);
@@ -73,27 +70,18 @@ __device__ __forceinline__ Decoded decode(const Operand& o) {
     return Decoded{{eight_of(o.lo.x, o.lo.y, s), eight_of(o.lo.z, o.lo.w, s), eight_of(o.hi.x, o.hi.y, s), eight_of(o.hi.z, o.hi.w, s)}};
 }
 // acc[c][f] += X[c] W[f]^T over a step, rows of X as rows of the result.
-template <bool Exact, int Byte, int RN, int FN>
+template <int Byte, int RN, int FN>
 __device__ __forceinline__ void multiply(f32x4 (&acc)[RN][FN], const Operand (&x)[RN], const Operand (&w)[FN]) {
-    if constexpr (Exact) {
-        Decoded xd[RN];
+    Decoded xd[RN];
 #pragma unroll
-        for (int c = 0; c < RN; ++c) xd[c] = decode<Byte>(x[c]);
+    for (int c = 0; c < RN; ++c) xd[c] = decode<Byte>(x[c]);
 #pragma unroll
-        for (int f = 0; f < FN; ++f) {
-            const Decoded wd = decode<Byte>(w[f]);
+    for (int f = 0; f < FN; ++f) {
+        const Decoded wd = decode<Byte>(w[f]);
 #pragma unroll
-            for (int c = 0; c < RN; ++c)
+        for (int c = 0; c < RN; ++c)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[c][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xd[c].v[j], wd.v[j], acc[c][f], 0, 0, 0);
-        }
-    } else {
-#pragma unroll
-        for (int f = 0; f < FN; ++f)
-#pragma unroll
-            for (int c = 0; c < RN; ++c)
-                acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes_of(x[c]), codes_of(w[f]), acc[c][f], 0, 0, Byte, (int)x[c].scale,
-                                                                             Byte, (int)w[f].scale);
+            for (int j = 0; j < 4; ++j) acc[c][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xd[c].v[j], wd.v[j], acc[c][f], 0, 0, 0);
     }
 }
 

@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kTileBlock) hidden_tile_kernel(HiddenArgs a) {
             for (int c = 0; c < 2; ++c) xv[c] = operand_at(32 * wave + 16 * c + m);
 #pragma unroll
             for (int f = 0; f < 8; ++f) wv[f] = operand_at(kTileRows + 16 * f + m);
-            multiply<sizeof(T) == 4, 0>(acc, xv, wv);
+            multiply<0>(acc, xv, wv);
         }
         const Results<T, Mode> out(a, list);
 #pragma unroll
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int TB = kHeldWaves * 16 * RN, MR = Mode == kProduct ? 64 : 128;       // rows of X per workgroup, rows of W per 64 columns
     constexpr int kLs = held_row<KS, Values>();
-    constexpr bool kExact = sizeof(T) == 4, kAhead = KS * RN <= (kExact && (Mode == kGatedGrad || KS > 2) ? 2 : 4);
+    constexpr bool kAhead = KS * RN <= (Mode == kGatedGrad || KS > 2 ? 2 : 4);
     const Lists lists(a.t, TB);
     const int total = lists.total(), groups = group_of_lane(a.t);
     if (total == 0) return;
@@ -285,7 +285,8 @@ __global__ void __launch_bounds__(kHeldBlock) hidden_held_kernel(HiddenArgs a) {
                             w[f].hi = *reinterpret_cast<const u32x4*>(p + 128 * s + 64 + 16 * q);
                             w[f].scale = *reinterpret_cast<const uint32_t*>(p + 128 * KS + 4 * (s / 4));
                         }
-                        multiply<kExact, (s & 3)>(acc[k], x[s], w);
+                        multiply<(s & 3)>(acc[k], x[s], w);
+                        if constexpr (KS > 6) __builtin_amdgcn_sched_barrier(0);      // W of steps to come would take the registers that there are
                     }
                 });
             }
@@ -342,7 +343,7 @@ static int launch_held_as(spp_ctx* ctx, HiddenArgs& a, bool* done) {
 // and 20; the gated gradient 172 -> 100 110 both.
 template <class T, int Mode, int KS, int RN, int Out>
 static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool few, bool* done) {
-    if constexpr (sizeof(T) == 4 && KS <= 4 && ((Mode == kGated && (RN == 2 || KS > 2)) || (Mode == kProduct && RN == 1 && (Out == kRagged || KS > 2)))) {
+    if constexpr (KS <= 4 && ((Mode == kGated && (RN == 2 || KS > 2)) || (Mode == kProduct && RN == 1 && (Out == kRagged || KS > 2)))) {
         if (!few) SPP_TRY((launch_held_as<T, Mode, KS, RN, Out, true>(ctx, a, done)));
         if (*done) return SPP_OK;
     }
@@ -372,12 +373,12 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
             }
             return launch_held<T, Mode, KS, 1, Out>(ctx, a, few, done);
         };
-        if constexpr (KS > 6 && sizeof(T) == 4) {
+        if constexpr (KS > 6 && Mode == kGatedGrad) {
             return (int)SPP_OK;                              // (registers)
         } else if constexpr (KS > 4) {
-            // with few columns most wavefronts of the other form would have none: 200k rows 1024 -> 24 68 and 56 us, 640 -> 47 49 and 39; of 16 bits
-            // 640 -> 128 42 and 49, of 32 85 and 72
-            if (sizeof(T) == 2 && a.H > 64) return (int)SPP_OK;
+            // with few columns most wavefronts of the other form would have none: 200k rows 1024 -> 24 in bf16 120 and 67 us, 640 -> 128 80 and 64, of 16
+            // bits 640 -> 192 81 and 86
+            if (sizeof(T) == 2 && a.H > 128) return (int)SPP_OK;
             return launch_held<T, Mode, KS, 1, kStraight>(ctx, a, few, done);
         } else if (lines) {
             return put(std::integral_constant<int, kLines>());
@@ -396,7 +397,7 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
         } else {
             // 300k rows 256 -> 86, -> 172 in bf16 with one sixteen 40 and 44 us, with two 31 and 38; 128 -> 86 in fp32 41 and 34, in bf16 24 and 26
             // (and two steps in fp32 fill the registers); straight from registers, 1M rows 172 -> 100 in bf16 95 us and so 87, 128 -> 250 226 and 145
-            if constexpr (KS == (sizeof(T) == 4 ? 1 : 2)) {
+            if constexpr (KS == 1) {
                 if (!few) SPP_TRY((launch_held<T, Mode, KS, 2, kRagged>(ctx, a, few, done)));
                 if (*done) return (int)SPP_OK;
             }
@@ -434,7 +435,6 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
     constexpr int RN = kWideRows<T, Mode, KS>, TB = 16 * RN, threads = 64 * WAVES, cols = Mode == kProduct ? 64 : 32;
     constexpr int kLs = 128 * KS + kLdsPad;                   // bytes of a row of X in LDS: codes, zeros up to whole steps, scales
     constexpr int kVec = (TB * (8 * KS + 1) + threads - 1) / threads;
-    constexpr bool kExact = sizeof(T) == 4;
     const Lists lists(a.t, TB);
     const int total = lists.total(), groups = group_of_lane(a.t);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = lane_id(), m = l & 15, q = l >> 4;
@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
             if (kOrdered) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int c = 0; c < RN; ++c) xv[kOrdered ? s & 1 : 0][c].scale = scales[kOrdered ? s / 4 & 1 : 0][c];
-            multiply<kExact, (s & 3)>(acc, xv[kOrdered ? s & 1 : 0], w[s]);
+            multiply<(s & 3)>(acc, xv[kOrdered ? s & 1 : 0], w[s]);
             if (s == (KS > 2 ? 1 : 0)) keep(other);
             if (s == (KS > 2 ? 2 : KS - 1)) ask(after);
             if (kOrdered) __builtin_amdgcn_sched_barrier(0);
