@@ -15,8 +15,6 @@
 #include "spp_fp8.h"
 #include "spp_rows_out.h"
 
-#include <type_traits>
-
 namespace spp {
 
 enum HiddenMode { kProduct, kGated, kGatedGrad };
@@ -39,15 +37,6 @@ struct HiddenArgs {
 
 // Lane j has list j's group: fetched byte by byte where it is needed, it would make the wavefront wait for all that it has under way.
 __device__ __forceinline__ int group_of_lane(const RowTable& t) { return lane_id() < t.n_lists ? t.group[lane_id()] : 0; }
-
-// f(0), f(1) .. with the index as a constant.
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void steps_of(F f) {
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>());
-        steps_of<N, I + 1>(f);
-    }
-}
 
 // ---- operands -------------------------------------------------------------------------------------
 

@@ -35,13 +35,16 @@ __device__ __forceinline__ i32x8 mx4_operand(u32x4 v) {
 // of what moves, written once, past the L2, which reads of the next rows would otherwise share with it (2.56M rows 128 -> 256 301 us
 // with plain stores, 250 so, both from a cached X).  Bound by HBM for narrow rows: 2.56M rows 128 -> 256 in bf16 264 us, 5.6 TB/s;
 // 400k rows 256 -> 1024 157 us, 5.7 TB/s; for wide ones by the wavefronts' waits for each other at every 64 columns: 390k
-// rows 768 -> 1024 225 to 230 us, 2.7 PFLOP/s.  Two rows of 16 per wavefront, three where kManyRows says so: one reads W from LDS twice as
+// rows 768 -> 1024 225 to 236 us, 2.6 to 2.7 PFLOP/s.  Two rows of 16 per wavefront, three where kManyRows says so: one reads W from LDS twice as
 // often, four (768 -> 1024) leave a wavefront per SIMD.  Eight wavefronts share a stream of W, four where rows are short (256 -> 1024
 // 167 and 157 us, 768 -> 1024 with two rows of 16 250 and 279).
 template <class T, int KS, int RN, int WAVES, bool Stream, bool Lines>
 __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t ws[];
     constexpr int TB = WAVES * 16 * RN, threads = 64 * WAVES;
+    // No kernel here puts registers away in scratch memory.  Where X has eighteen operands its scales lie four steps to a register; there, and of three
+    // steps off the lines, W's operands are not read ahead of their step, which would take more registers than there are.
+    constexpr bool kPacked = KS * RN == 18, kInTurn = kPacked || (KS == 3 && RN == 2 && Stream && !Lines && sizeof(T) == 2);
     constexpr int kVec = (64 * ((KS * 4 * 17 + 15) / 16) + threads - 1) / threads;       // vectors of 64 rows of W per thread
     const Lists lists(a.t, TB);
     const int total = lists.total();
@@ -137,13 +140,15 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
             __syncthreads();
         }
         u32x4 xv[KS][RN];
-        uint32_t xc[KS][RN];
+        uint32_t xc[kPacked ? (KS + 3) / 4 : KS][RN];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int c = 0; c < RN; ++c) {
                 const bool in = 4 * s + q < a.nb;
-                xc[s][c] = in ? ahead_scale[s][c] >> (8 * q) : 127u;
+                const uint32_t scale = in ? ahead_scale[s][c] >> (8 * q) : 127u;
+                if constexpr (kPacked) xc[s / 4][c] = (s & 3 ? xc[s / 4][c] : 0u) | (scale & 255u) << (8 * (s & 3));
+                else xc[s][c] = scale;
                 xv[s][c] = in ? ahead[s][c] : u32x4{0, 0, 0, 0};
             }
         if (kAhead && item + share.step < share.end) { it = find(item + share.step); ask_rows(it); }
@@ -156,8 +161,8 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
 #pragma unroll
                 for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (mine > 0)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
+                steps_of<KS>([&](auto step) {
+                    constexpr int s = decltype(step)::value;
                     u32x4 wv[4];
                     uint32_t wc[4];
 #pragma unroll
@@ -173,8 +178,9 @@ __global__ void __launch_bounds__(64 * WAVES) mx4_rows_kernel(ProductArgs a) {
 #pragma unroll
                         for (int c = 0; c < RN; ++c)
                             acc[c][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(xv[s][c]), mx4_operand(wv[f]), acc[c][f], 4, 4,
-                                                                                         0, (int)xc[s][c], 0, (int)wc[f]);
-                }
+                                                                                         kPacked ? s & 3 : 0, (int)xc[kPacked ? s / 4 : s][c], 0, (int)wc[f]);
+                    if constexpr (kInTurn) __builtin_amdgcn_sched_barrier(0);
+                });
             if (Stream && t + 1 < t1) keep(ws + ((t + 1) & 1) * (64 * a.ls + 64));
             if constexpr (Lines) {
                 if (mine >= 16 * RN && 64 * t + 64 <= a.H) {
@@ -318,7 +324,7 @@ static int launch_product(spp_ctx* ctx, const ProductArgs& a) {
 constexpr int kHeldW = 65536;            // LDS for a W that stays: two workgroups fit a CU
 // Rows per CU from which wide rows with a result of 16 bits go 48 to a wavefront instead of 32: W is read from LDS two thirds as
 // often, but tiles are larger and the last round of them emptier.  768 -> 1024, 32 and 48: 100k rows 75 and 92 us, 200k 149 both, 300k
-// 209 and 200, 390k 247 and 230, 800k 533 and 489; 500 -> 1024: 100k 58 and 71, 200k 111 both, 390k 191 and 176, 800k 410 and 387.
+// 195 and 169, 390k 266 and 236, 800k 515 and 477; 500 -> 1024: 100k 58 and 71, 200k 111 both, 390k 191 and 176, 800k 410 and 387.
 // (150k rows, a round less: 110 and 100, not taken.)  In fp32 the stores bound both: 390k rows 355 and 362.
 constexpr int kManyRows = 2 * 8 * 48;
 constexpr int kRowOut = 768;             // bytes of Y's rows that go out in one run

@@ -9,6 +9,7 @@
 #include "spp_device.h"
 
 #include <atomic>
+#include <type_traits>
 
 namespace spp {
 
@@ -66,6 +67,15 @@ struct Share {
 __device__ __forceinline__ unsigned own_piece() {
     const unsigned x = blockIdx.x & 7, more = gridDim.x & 7;
     return x * (gridDim.x >> 3) + (x < more ? x : more) + (blockIdx.x >> 3);
+}
+
+// f(0), f(1) .. with the index as a constant.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void steps_of(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        steps_of<N, I + 1>(f);
+    }
 }
 
 // A vector at an address that is aligned to its elements only: one access all the same.
