@@ -463,7 +463,8 @@ int  spp_fp8_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64
  *                    G_j = X_j Wg[g_j]^T, U_j = X_j Wu[g_j]^T        H at most SPP_MAX_HIDDEN / 2
  *       gated grad   dP_j = [dY_j * U_j * act'(G_j) | dY_j * act(G_j)]
  *                    lists: d_y is dY_j, read; grads: the same rows, n, d_n and groups, d_y is dP_j [n, 2H], written, ld >= 2H.  G and U
- *                    are formed again from the rows, as in the forward pass.  dP must not overlap dY.
+ *                    are formed again from the rows, as in the forward pass.  No dP may overlap a dY (as the
+ *                    matrices of n rows that they are; columns of one buffer may lie side by side): SPP_E_ARG.
  *       weight grad  dW[g] = sum over the lists j of group g of dY_j^T X_j, as spp_mx4_weight_grad in everything else.  With grads and
  *                    2H for H it gives the gradients of Wg and Wu, one behind the other.
  *     X and W are the values that the rows stand for; products are exact, sums and activations are formed in fp32, and what is written is

@@ -1047,7 +1047,7 @@ def fp8_gated_grad(ctx: Context, lists, grads, weights: torch.Tensor, D: int, ac
 
     lists: the rows that the layer read, each with dY_j [n, H] as its y.  grads: the same rows, counts and groups, each with the
     matrix [n, 2H] that dP_j is written to as its y; fp8_weight_grad of it is the gradient of the weights.  G and U are formed
-    again from the rows.  dP must not overlap dY.
+    again from the rows.  A dP that overlaps a dY is refused; columns of one buffer may lie side by side.
     """
     act = _activation(activation)
     lists, groups, H = _fp8_weights(lists, weights, D, 2)

@@ -653,6 +653,35 @@ static int launch_hidden(spp_ctx* ctx, HiddenArgs& a) {
     return SPP_OK;
 }
 
+// Whether two matrices of rows share a byte: n rows of `bytes` bytes each, `step` bytes from a row to the next.  Rows of the same step, and of steps that differ where
+// one matrix has no gaps, exactly: columns of one buffer may lie side by side.  Of two with gaps and other steps the first 4096 rows are looked at.
+struct Span {
+    uint64_t at;
+    int64_t  n, bytes, step;
+    uint64_t end() const { return at + (uint64_t)(n - 1) * step + bytes; }
+};
+static inline bool overlap(Span a, Span b) {
+    if (a.n == 0 || b.n == 0) return false;
+    if (a.n == 1) a.step = a.bytes;
+    if (b.n == 1) b.step = b.bytes;
+    if (a.at >= b.end() || b.at >= a.end()) return false;
+    // a row from `from` of `bytes` bytes against rows: the first that ends behind its beginning begins before its end
+    auto meets = [](uint64_t from, int64_t bytes, const Span& s) {
+        const uint64_t i = from < s.at + s.bytes ? 0 : (from - s.at - s.bytes) / s.step + 1;
+        return (int64_t)i < s.n && s.at + i * s.step < from + bytes;
+    };
+    if (a.step == a.bytes) return meets(a.at, a.n * a.bytes, b);
+    if (b.step == b.bytes) return meets(b.at, b.n * b.bytes, a);
+    if (a.at > b.at) { const Span c = a; a = b; b = c; }
+    if (a.step == b.step) {                              // b's first row lies among a's, and all others as it does
+        const uint64_t d = (b.at - a.at) % a.step;
+        return (int64_t)d < a.bytes || ((int64_t)d + b.bytes > a.step && (int64_t)((b.at - a.at) / a.step) + 1 < a.n);
+    }
+    for (int64_t i = 0; i < b.n && i < 4096; ++i)
+        if (meets(b.at + i * b.step, b.bytes, a)) return true;
+    return false;
+}
+
 // The checks of the three entries, and the launch.
 template <int Mode>
 static int hidden(const char* who, spp_ctx* ctx, const spp_row_list* lists, const spp_row_list* grads, int32_t n_lists, const void* d_weights,
@@ -663,10 +692,7 @@ static int hidden(const char* who, spp_ctx* ctx, const spp_row_list* lists, cons
     memset(&a, 0, sizeof(a));
     int64_t most = 0;
     SPP_TRY(row_table(who, lists, n_lists, n_groups, D, H, type, a.t, &most));
-    if (Mode != kProduct) {
-        SPP_CHECK(H <= SPP_MAX_HIDDEN / 2, SPP_E_ARG, "%s: H = %d (1 .. %d)", who, H, SPP_MAX_HIDDEN / 2);
-        SPP_CHECK(activation == SPP_SILU || activation == SPP_GELU || activation == SPP_SIGMOID, SPP_E_ARG, "%s: activation %d", who, activation);
-    }
+    if (Mode != kProduct) SPP_CHECK(H <= SPP_MAX_HIDDEN / 2, SPP_E_ARG, "%s: H = %d (1 .. %d)", who, H, SPP_MAX_HIDDEN / 2);
     if (Mode == kGatedGrad) {
         RowTable p;
         int64_t also = 0;
@@ -675,8 +701,27 @@ static int hidden(const char* who, spp_ctx* ctx, const spp_row_list* lists, cons
         for (int j = 0; j < n_lists; ++j)
             SPP_CHECK(lists[j].d_rows == grads[j].d_rows && lists[j].n == grads[j].n && lists[j].d_n == grads[j].d_n && lists[j].group == grads[j].group,
                       SPP_E_ARG, "%s: list %d: the gradient's rows, count or group are not the list's", who, j);
+        auto span = [&](const spp_row_list& l, int cols) {
+            const int64_t es = (int64_t)type_bytes(type);
+            return Span{(uint64_t)(uintptr_t)l.d_y, l.n, cols * es, l.ld * es};
+        };
+        uint64_t lo = ~0ull, hi = 0;                     // all dY lie there: most gradients, in buffers of their own, need no closer look
+        for (int j = 0; j < n_lists; ++j)
+            if (lists[j].n > 0) {
+                const Span s = span(lists[j], H);
+                lo = s.at < lo ? s.at : lo;
+                hi = s.end() > hi ? s.end() : hi;
+            }
+        for (int k = 0; k < n_lists; ++k) {
+            const Span dp = span(grads[k], 2 * H);
+            if (dp.n == 0 || dp.at >= hi || dp.end() <= lo) continue;
+            for (int j = 0; j < n_lists; ++j)
+                SPP_CHECK(!overlap(span(lists[j], H), dp), SPP_E_ARG, "%s: the gradient of list %d overlaps the dY of list %d", who, k, j);
+        }
         for (int j = 0; j < n_lists; ++j) { a.dp[j] = p.y[j]; a.dp_ld[j] = p.ld[j]; }
     }
+    if (Mode != kProduct)
+        SPP_CHECK(activation == SPP_SILU || activation == SPP_GELU || activation == SPP_SIGMOID, SPP_E_ARG, "%s: activation %d", who, activation);
     if (most > 0) {
         a.w = static_cast<const uint8_t*>(d_weights);
         a.D = D; a.H = H; a.rb = fp8_bytes(D); a.cb = fp8_code_bytes(D); a.steps = fp8_blocks(D); a.act = activation;
