@@ -121,6 +121,7 @@ struct GradShape {
     static constexpr int nx = (rows * row_pieces + threads - 1) / threads;
 };
 
+// Some shapes take up to 466 of 512 registers: no code here is masked behind the first product but what a whole wavefront does or does not.
 template <class F, class T, int WH, int WD, int FH>
 __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
     typedef GradShape<F, T, WH, WD, FH> S;
@@ -193,12 +194,13 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
 #pragma unroll
             for (int k = 0; k < S::ny; ++k) {
                 const int i = k * S::threads + (int)threadIdx.x, r = i / (S::th / S::ve);
-                if (r >= left) py[k] -= (uint32_t)((r - left + 1) * (int)ld);
+                py[k] -= (uint32_t)(max(r - left + 1, 0) * (int)ld);
             }
 #pragma unroll
             for (int k = 0; k < S::nx; ++k) {
                 const int i = k * S::threads + (int)threadIdx.x, r = i / RP < S::rows ? i / RP : S::rows - 1;
-                if (r >= left) { px[k] -= (uint32_t)((r - left + 1) * a.rb); ps[k] -= (uint32_t)((r - left + 1) * a.rb); }
+                const uint32_t back = (uint32_t)(max(r - left + 1, 0) * a.rb);
+                px[k] -= back; ps[k] -= back;
             }
         }
         if (ld < (1 << 24) && (wide || (left > S::rows && a.H >= S::ve))) {
@@ -229,11 +231,21 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
     auto put = [&](int u, int buffer) {
         __bf16* gy = lds + buffer * S::buffer;
         __bf16* gx = gy + P * S::rows * S::ly;
+        if (here[u] < S::rows) {                           // the list's last chunk: rows behind its last are zeros
+#pragma unroll
+            for (int k = 0; k < S::ny; ++k) ry[u][k] &= (k * S::threads + (int)threadIdx.x) / (S::th / S::ve) < here[u] ? ~0u : 0u;
+#pragma unroll
+            for (int k = 0; k < S::nx; ++k) {
+                const uint32_t there = (k * S::threads + (int)threadIdx.x) / RP < here[u] ? ~0u : 0u;
+                rx[u][k] &= there;
+                rs[u][k] &= there;                         // (2^-127: not NaN)
+            }
+        }
 #pragma unroll
         for (int k = 0; k < S::ny; ++k) {
             const int i = k * S::threads + (int)threadIdx.x;
             const int r = i / (S::th / S::ve), h = i % (S::th / S::ve) * S::ve;
-            const u32x4 raw = r < here[u] ? ry[u][k] : u32x4{0, 0, 0, 0};
+            const u32x4 raw = ry[u][k];
             if constexpr (P == 1) {
                 *reinterpret_cast<u32x4*>(gy + r * S::ly + h) = raw;
             } else {
@@ -274,9 +286,9 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
         for (int k = 0; k < S::nx; ++k) {
             const int i = k * S::threads + (int)threadIdx.x;
             const int r = i / RP;
-            if (S::rows * RP % S::threads && r >= S::rows) continue;
-            const float s = r < here[u] ? mx4_scale(rs[u][k]) : 0.0f;
-            u32x4 c = r < here[u] ? rx[u][k] : u32x4{0, 0, 0, 0};
+            if (S::rows * RP % S::threads && __builtin_amdgcn_readfirstlane(r) >= S::rows) continue;       // a wavefront's are, or are not: 64 divide them
+            const float s = mx4_scale(rs[u][k]);
+            u32x4 c = rx[u][k];
             __bf16* to_x = gx + r * S::lx + i % RP * S::columns;
             if constexpr (S::columns == 32) {
                 // 16 lanes' pieces of 16 bytes, 64 bytes apart, in banks of their own: half of the lanes begin with the second
@@ -301,18 +313,21 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
+    // By way of a buffer, whose range check takes the place of masks: what lies behind H or D goes nowhere.
     auto flush = [&](int g) {
         // from values made anew: addresses worked out ahead of the loop would take the registers that it needs
         const int lane = spp::here(l);
-        float* out = a.direct ? a.dw : a.pieces + (int64_t)(split + g) * a.H * a.D;
+        const int64_t size = (int64_t)a.H * a.D, piece = (int64_t)(split + __builtin_amdgcn_readfirstlane(g)) * size;
+        const uint32_t h = h0 + wh + 4 * (lane >> 4), d = d0 + wd + (lane & 15);
+        const auto out = rows_buffer(a.direct ? a.dw : a.pieces + piece, (uint32_t)size * 4);         // at most 2^30 bytes
 #pragma unroll
         for (int f = 0; f < FH; ++f)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int h = h0 + wh + 16 * f + 4 * (lane >> 4) + i, d = d0 + wd + 16 * c + (lane & 15);
-                    if (h < a.H && d < a.D) out[(int64_t)h * a.D + d] = acc[f][c][i];
+                    const uint32_t at = ((h + 16 * f + i) * (uint32_t)a.D + d + 16 * c) * 4;
+                    buffer_store<0>(acc[f][c][i], out, (h + 16 * f + i < (uint32_t)a.H) & (d + 16 * c < (uint32_t)a.D) ? at : kNowhere);
                 }
     };
     const int n = to - from;

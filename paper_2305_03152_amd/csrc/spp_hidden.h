@@ -202,29 +202,7 @@ __device__ __forceinline__ void combine(int act, f32x4 (&one)[N], f32x4 (&two)[N
     }
 }
 
-// A buffer that begins with a tile's first row, of `bytes` bytes: what is read behind them is 0, what is written there is dropped, so that a
-// tile of fewer rows takes the same path as any other, and without a branch.
-__device__ __forceinline__ auto rows_buffer(const void* p, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
-}
-constexpr uint32_t kNowhere = 0x80000000u;       // an offset behind every buffer
-constexpr int kPastL2 = 2;                       // a store that is not kept in the L2
-template <int Kind, class V>
-__device__ __forceinline__ void buffer_store(V v, __amdgpu_buffer_rsrc_t to, uint32_t at) {
-    if constexpr (sizeof(V) == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, (int)at, 0, Kind);
-    else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), to, (int)at, 0, Kind);
-    else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), to, (int)at, 0, Kind);
-    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), to, (int)at, 0, Kind);
-}
-template <class V>
-__device__ __forceinline__ V buffer_load(__amdgpu_buffer_rsrc_t from, uint32_t at) {
-    if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0));
-    else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(from, (int)at, 0, 0));
-    else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(from, (int)at, 0, 0));
-    else return __builtin_bit_cast(V, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, (int)at, 0, 0));
-}
-
-// A tile of a matrix of results by way of such a buffer: 16 RN rows, of which `here` are there, and of each N columns from h0 + N m on.
+// A tile of a matrix of results by way of a buffer (rows_buffer) that begins with its first row: 16 RN rows, of which `here` are there, and of each N columns from h0 + N m on.
 // Whole vectors where all begin at multiples of four bytes, which is all that the instructions ask for; the last columns of a row where they
 // are no whole vector, and 16-bit matrices at odd places, go element by element (1M rows 172 -> 86, every column by element: gated layer in
 // fp32 212 us, its gradient 477; so 174 and 360).  All of it is branches that a whole wavefront takes: where a kernel's values fill the

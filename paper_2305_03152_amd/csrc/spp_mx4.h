@@ -81,6 +81,28 @@ __device__ __forceinline__ void steps_of(F f) {
 // A vector at an address that is aligned to its elements only: one access all the same.
 template <class V> struct Loose { V v; } __attribute__((packed, aligned(2)));
 
+// A buffer of `bytes` bytes, e.g. a tile's rows from its first on: what is read behind them is 0, what is written there is dropped, so that a
+// tile of fewer rows takes the same path as any other, and without a branch.
+__device__ __forceinline__ auto rows_buffer(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
+}
+constexpr uint32_t kNowhere = 0x80000000u;       // an offset behind every buffer
+constexpr int kPastL2 = 2;                       // a store that is not kept in the L2
+template <int Kind, class V>
+__device__ __forceinline__ void buffer_store(V v, __amdgpu_buffer_rsrc_t to, uint32_t at) {
+    if constexpr (sizeof(V) == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, (int)at, 0, Kind);
+    else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), to, (int)at, 0, Kind);
+    else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), to, (int)at, 0, Kind);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), to, (int)at, 0, Kind);
+}
+template <class V>
+__device__ __forceinline__ V buffer_load(__amdgpu_buffer_rsrc_t from, uint32_t at) {
+    if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0));
+    else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(from, (int)at, 0, 0));
+    else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(from, (int)at, 0, 0));
+    else return __builtin_bit_cast(V, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, (int)at, 0, 0));
+}
+
 // Lists of packed rows, each with a matrix Y of its own: the operands of the product and of its gradient.
 constexpr int kRowLists = SPP_MAX_ROW_LISTS;
 static_assert(kRowLists == kWave, "a wavefront's lanes hold a list each");
