@@ -389,12 +389,13 @@ int  spp_mx4_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64
  *                                                              written (a group without rows: zeros)
  *     X and W are the values that the packed rows stand for; sums are formed in fp32 and rounded once to Y's type.  The
  *     gradient is that of the product by W's values; the rows are data and have none.  In it an fp32 Y below 2^-110 counts to
- *     within 2^-133, and an X beyond fp32 (scale byte 254, which quantising does not give) as infinite.  It adds in an order
- *     that the lists' counts and groups, D, H, the type and the GPU's number of CUs decide: the same rows give the same bits,
- *     whatever the buffers' n.  It keeps some 64 MiB, or one matrix if that is more, and one matrix per group of device
- *     memory with the context.  A call may be recorded into a HIP graph: what it keeps for that stays where it is, also when
- *     later calls need more, until the context is destroyed.  The context has to outlive the graph, and replays are ordered
- *     with the context's other calls, whose memory they share.
+ *     within 2^-133, and an X beyond fp32 (scale byte 254, which quantising does not give) as infinite.  A sum in fp32 is of at
+ *     most 32768 rows (16384 in fp16, 10912 in fp32), these sums are added in 64 bits.  It adds in an order that the lists' counts
+ *     and groups, D, H, the type and the GPU's number of CUs decide: the same rows give the same bits, whatever the buffers' n.
+ *     It keeps some 64 MiB, or one matrix if that is more, and one matrix per group of device memory with the context, twice as
+ *     much where a workgroup may have more rows than one such sum.  A call may be recorded into a HIP graph: what it keeps for
+ *     that stays where it is, also when later calls need more, until the context is destroyed.  The context has to outlive the
+ *     graph, and replays are ordered with the context's other calls, whose memory they share.
  *     d_rows 16-byte aligned; Y aligned to its type, ld >= H elements from a row to the next (16-byte aligned rows take
  *     the wide path).  Rows from *d_n on are neither read nor written, whatever they hold.  H is 1 .. SPP_MAX_HIDDEN. */
 typedef struct {

@@ -3,7 +3,7 @@
 //   dW[g] = sum over the lists j of group g of dY_j^T X_j        dY_j [n_j, H] fp32, fp16 or bf16, X_j [n_j, D] in few bits, dW fp32
 //
 // What a code and a scale stand for is exact in bf16, as is an fp16 as the sum of two bf16 and an fp32 of at least 2^-110 as that of three:
-// the products of the matrix instruction are exact and are added in fp32, the sums of the runs in 64 bits.  Of a smaller fp32 the bits
+// the products of the matrix instruction are exact and are added in fp32, up to kGradChain times, those sums in 64 bits.  Of a smaller fp32 the bits
 // below 2^-133, the smallest bf16, are lost: off by less than 2^-133 each, whatever X.
 
 #pragma once
@@ -58,13 +58,14 @@ constexpr int kGradPad = 16;         // elements behind an LDS row: the four row
 
 struct GradArgs {
     RowTable t;
-    float*   pieces;       // [splits + groups][H * D]
+    void*    pieces;       // [splits + groups][H * D], fp32 or fp64
     float*   dw;           // [groups][H * D]
     int32_t  D, H, nb, rb; // nb: pieces of a row (GradMx4, GradFp8)
     int32_t  splits, tiles_d;        // runs that the grid and the pieces have room for
     int32_t  most;         // runs at most, by the matrix's shape
     int32_t  chunk;        // rows of a chunk
-    int32_t  direct;       // one run and one group: its sums are dW
+    int32_t  direct;       // one run and one group, within a chain: its sums are dW
+    int32_t  wide;         // runs that may be longer than a chain: pieces in 64 bits
 };
 
 constexpr int kFewGradRows = 128;
@@ -75,6 +76,13 @@ __host__ __device__ __forceinline__ int grad_runs(int64_t chunks, int rows, int 
     const int64_t half = (chunks + 1) / 2;
     return half < most ? (int)half : most;
 }
+
+// The additions that an accumulator takes at most.  Rows that are alike are rounded alike: where dW filled the CUs, so that a group's rows were one
+// run, 800k of them were off by 1.5e-3 in bf16 and 4e-3 in fp32, and by more the more they were.  Behind a chain of so many a run adds what it has to its
+// piece in 64 bits and begins anew: reading and writing a piece is 1 MB a workgroup (256 x 256) beside some 25 MB of operands (1M rows of
+// 2048 with 2048 gradients in bf16 7642 and 7764 us), and runs are as long only where there are many rows for the CUs (2.5M rows of 256 with 512
+// gradients in bf16 have 610 additions a run).
+constexpr int kGradChain = 1024;
 
 // dY as bf16 numbers that add up to it exactly (above): one, two of an fp16, three of an fp32.  Cut off rather than rounded, so that no
 // finite value becomes infinite; what is not finite is its first piece alone.
@@ -111,6 +119,7 @@ struct GradShape {
     static constexpr int P = Pieces<T>::n, wh = WH, wd = WD, fh = FH;
     static constexpr int rows = P == 1 ? 64 : 32;                    // of a chunk: two buffers of it fit the LDS
     static constexpr int threads = 64 * WH * WD;
+    static constexpr int chain = kGradChain / (rows / 32 * P);       // in chunks
     static constexpr int th = 16 * FH * WH, td = 64 * WD;            // the tile of dW: a wavefront has 16 FH x 64 of it
     static constexpr int ly = th + kGradPad, lx = td + kGradPad;     // elements of an LDS row
     static constexpr int buffer = rows * (P * ly + lx);              // elements of a buffer
@@ -313,26 +322,49 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[f][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
-    // By way of a buffer, whose range check takes the place of masks: what lies behind H or D goes nowhere.
-    auto flush = [&](int g) {
+    // By way of a buffer, whose range check takes the place of masks: what lies behind H or D goes nowhere.  `more`: to what the piece has already.
+    auto flush = [&](int g, bool more) {
         // from values made anew: addresses worked out ahead of the loop would take the registers that it needs
         const int lane = spp::here(l);
         const int64_t size = (int64_t)a.H * a.D, piece = (int64_t)(split + __builtin_amdgcn_readfirstlane(g)) * size;
         const uint32_t h = h0 + wh + 4 * (lane >> 4), d = d0 + wd + (lane & 15);
-        const auto out = rows_buffer(a.direct ? a.dw : a.pieces + piece, (uint32_t)size * 4);         // at most 2^30 bytes
+        auto place = [&](int f, int c, int i, int es) {
+            const uint32_t at = ((h + 16 * f + i) * (uint32_t)a.D + d + 16 * c) * es;
+            return (h + 16 * f + i < (uint32_t)a.H) & (d + 16 * c < (uint32_t)a.D) ? at : kNowhere;
+        };
+        if (!a.wide) {
+            const auto out = rows_buffer(a.direct ? a.dw : static_cast<float*>(a.pieces) + piece, (uint32_t)size * 4);
 #pragma unroll
-        for (int f = 0; f < FH; ++f)
+            for (int f = 0; f < FH; ++f)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t at = ((h + 16 * f + i) * (uint32_t)a.D + d + 16 * c) * 4;
-                    buffer_store<0>(acc[f][c][i], out, (h + 16 * f + i < (uint32_t)a.H) & (d + 16 * c < (uint32_t)a.D) ? at : kNowhere);
+                    for (int i = 0; i < 4; ++i) buffer_store<0>(acc[f][c][i], out, place(f, c, i, 4));
+        } else {
+            const auto out = rows_buffer(static_cast<double*>(a.pieces) + piece, (uint32_t)size * 8);       // at most 2^31 bytes
+#pragma unroll
+            for (int f = 0; f < FH; ++f)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t at[4];
+                    double v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        at[i] = place(f, c, i, 8);
+                        v[i] = 0.0;
+                    }
+                    if (more)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(double, buffer_load<u32x2>(out, at[i]));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) buffer_store<0>(__builtin_bit_cast(u32x2, v[i] + (double)acc[f][c][i]), out, at[i]);
                 }
+        }
     };
     const int n = to - from;
     clear();
-    int now = 0;
+    int now = 0, held = 0;                                           // the group, chunks in the accumulators
+    bool more = false;                                               // the group's piece has been begun
     if (n > 0) {
         load(0, from, true);
         if (S::ahead > 1) load(S::ahead - 1, from + 1, n > 1);
@@ -343,7 +375,14 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
         for (int u = 0; u < 2; ++u) {
             if (j + u >= n) break;
             constexpr int mask = S::ahead - 1;
-            if (group[u & mask] != now) { flush(now); clear(); now = group[u & mask]; }
+            if (group[u & mask] != now || (a.wide && held == S::chain)) {
+                flush(now, more);
+                clear();
+                more = group[u & mask] == now;
+                now = group[u & mask];
+                held = 0;
+            }
+            ++held;
             put(u & mask, u);
             load(u & mask, from + j + u + S::ahead, j + u + S::ahead < n);
             __syncthreads();         // the other buffer has been read by all before this one is read by any
@@ -368,7 +407,7 @@ __global__ void __launch_bounds__(64 * WH * WD) weight_grad_kernel(GradArgs a) {
             }
         }
     }
-    flush(now);
+    flush(now, more);
 }
 
 // The pieces of 256 elements side by side, four a lane, are added by a workgroup's wavefronts in turn, then the wavefronts' sums:
@@ -380,7 +419,9 @@ __host__ __device__ __forceinline__ int grad_sum_waves(int runs, int groups) {
     return each > 64 ? kSumWaves : each > 16 ? 8 : 4;
 }
 typedef double f64x4 __attribute__((ext_vector_type(4)));
+template <class V>       // of a piece
 static __global__ void __launch_bounds__(64 * kSumWaves) weight_grad_sum_kernel(GradArgs a) {
+    typedef V V4 __attribute__((ext_vector_type(4)));
     __shared__ f64x4 part[kSumWaves][kWave];
     const Lists lists(a.t, a.chunk);
     const int total = lists.total(), group = blockIdx.y, wave = threadIdx.x >> 6, l = lane_id();
@@ -397,29 +438,29 @@ static __global__ void __launch_bounds__(64 * kSumWaves) weight_grad_sum_kernel(
     const int64_t i = ((int64_t)blockIdx.x * kWave + l) * 4;
     // a vector at the matrix' end begins earlier: its last elements are the matrix' last
     const int64_t at = size < 4 ? 0 : i + 4 <= size ? i : size - 4;
-    const float* p = a.pieces + group * size + at;
+    const V* p = static_cast<const V*>(a.pieces) + group * size + at;
     f64x4 sum = {0.0, 0.0, 0.0, 0.0};
-    auto add = [&](f32x4 v) {
+    auto add = [&](V4 v) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum[k] += (double)v[k];
     };
     auto take = [&](int s) {
-        const float* from = p + (int64_t)s * size;
-        if (size >= 4) return reinterpret_cast<const Loose<f32x4>*>(from)->v;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        const V* from = p + (int64_t)s * size;
+        if (size >= 4) return reinterpret_cast<const Loose<V4>*>(from)->v;
+        V4 v = {0, 0, 0, 0};
         for (int k = 0; k < (int)size; ++k) v[k] = from[k];
         return v;
     };
     int s = lo + wave;
     for (; s + 7 * waves <= hi; s += 8 * waves) {
-        f32x4 v[8];
+        V4 v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = take(s + k * waves);
 #pragma unroll
         for (int k = 0; k < 8; ++k) add(v[k]);
     }
     for (; s + 3 * waves <= hi; s += 4 * waves) {
-        f32x4 v[4];
+        V4 v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = take(s + k * waves);
 #pragma unroll
@@ -448,9 +489,11 @@ static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
     int64_t chunks = 0;
     for (int j = 0; j < a.t.n_lists; ++j) chunks += (a.t.n[j] + (int64_t)S::rows - 1) / S::rows;
     a.splits = grad_runs(chunks, S::rows, a.most);
-    a.direct = !sum_only && a.splits == 1 && n_groups == 1;
-    if (!a.direct) SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * sizeof(float), ctx->stream));
-    a.pieces = ctx->gradws.as<float>();
+    // What the lists can hold decides the pieces' type, which does not show in the result: a run within a chain gives the same sum in either.
+    a.wide = (chunks + a.splits - 1) / a.splits > S::chain;
+    a.direct = !sum_only && !a.wide && a.splits == 1 && n_groups == 1;
+    if (!a.direct) SPP_TRY(ctx->gradws.reserve((size_t)(a.splits + n_groups) * size * (a.wide ? sizeof(double) : sizeof(float)), ctx->stream));
+    a.pieces = ctx->gradws.ptr;
     if (!sum_only) {
         SPP_TRY(limit.allow(ctx, reinterpret_cast<const void*>(kernel), S::lds));
         kernel<<<(unsigned)(a.splits * tiles), S::threads, S::lds, ctx->stream>>>(a);
@@ -458,7 +501,8 @@ static int launch_grad(spp_ctx* ctx, GradArgs& a, int n_groups, bool sum_only) {
     }
     if (a.direct) return SPP_OK;
     const int64_t sums = (size + 4 * kWave - 1) / (4 * kWave);       // at most 2^20: SPP_MAX_HIDDEN rows of SPP_MX4_MAX_COLS
-    weight_grad_sum_kernel<<<dim3((unsigned)sums, n_groups), 64 * grad_sum_waves(a.splits, n_groups), 0, ctx->stream>>>(a);
+    auto sum = a.wide ? weight_grad_sum_kernel<double> : weight_grad_sum_kernel<float>;
+    sum<<<dim3((unsigned)sums, n_groups), 64 * grad_sum_waves(a.splits, n_groups), 0, ctx->stream>>>(a);
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
