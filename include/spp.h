@@ -468,11 +468,16 @@ int  spp_fp8_dequantize(spp_ctx* ctx, const void* d_rows, int64_t n, const int64
  *                    matrices of n rows that they are; columns of one buffer may lie side by side): SPP_E_ARG.
  *       weight grad  dW[g] = sum over the lists j of group g of dY_j^T X_j, as spp_mx4_weight_grad in everything else.  With grads and
  *                    2H for H it gives the gradients of Wg and Wu, one behind the other.
- *     X and W are the values that the rows stand for; products are exact, sums and activations are formed in fp32, and what is written is
- *     rounded once to Y's type, whatever that is.  The gradient
- *     of the rows of a layer is the product of dY (dP) in 8 bits by the transposed weights (of Wg and Wu, one behind the other).
- *     Of rows of other origin a value below 2^-126 may count as 0.
- *     Rows from *d_n on are neither read nor written, nor what lies between rows of Y; recording as in (6). */
+ *     X and W are the values that the rows stand for; products are exact, sums and activations are formed in fp32, and what is written
+ *     is rounded once to Y's type, whatever that is.  Of rows of other origin a value below 2^-126 may count as 0, one beyond fp32 is
+ *     infinite.
+ *     The gradient of the rows of a layer is the product of dY (dP) in 8 bits by the transposed weights (of Wg and Wu, one behind the
+ *     other).  Scales lie along a row, in W along D and in its transpose along H: the transpose is made of the values that the
+ *     layer read (spp_fp8_dequantize), so that what is at least a 14336th of its new block's largest keeps its value, and what is less
+ *     moves by at most a 229376th of that; made of the weights before they were in 8 bits it is of other values than the layer's.  H (2H)
+ *     beyond SPP_MX4_MAX_COLS is taken in stretches of columns, whose products the caller adds.
+ *     Rows from *d_n on are neither read nor written; what lies between rows of Y is not written, and its values do not matter.
+ *     Recording as in (6). */
 int  spp_fp8_product(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,
                      int32_t D, int32_t H, int32_t type, uint32_t flags);
 int  spp_fp8_gated(spp_ctx* ctx, const spp_row_list* lists, int32_t n_lists, const void* d_weights, int32_t n_groups,

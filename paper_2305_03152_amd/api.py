@@ -989,7 +989,9 @@ def fp8_product_multi(ctx: Context, lists, weights: torch.Tensor, D: int, sync: 
     """Y_j = X_j W[group_j]^T for every list of rows in 8 bits, in one launch; `lists` is a RowLists or what makes one.
 
     weights: uint8 [groups, H, row bytes] or [H, row bytes], rows of D columns (fp8_quantize of a matrix [H, D]).  The gradient of a
-    layer's rows is this product too, of the outputs' gradient in 8 bits and the transposed weights (fp8_quantize of [D, H]).
+    layer's rows is this product too, of the outputs' gradient in 8 bits and the transposed weights: fp8_quantize of
+    fp8_dequantize(weights).T, the values that the layer read (all but the very smallest keep theirs).  Of more than 4096 outputs (2048 of
+    a gated layer) it is the sum of such products over stretches of their columns.
     """
     lists, groups, H = _fp8_weights(lists, weights, D, 1)
     if lists.lists:
