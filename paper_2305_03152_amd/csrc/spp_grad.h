@@ -48,12 +48,12 @@ struct GradFp8 {
 // transposed (ds_read_b64_tr_b16).  A chunk's operands are asked for two chunks ahead, into registers; X is unpacked to bf16 on
 // its way to LDS, dY cut into its pieces.
 //
-// Bound by HBM where dW is one tile: 2.56M rows of 128 with 256 gradients in bf16 270 us, 5.5 TB/s; fp16 430 to 445, fp32 (half the rows) 330
-// to 345, by the cutting and its two and three products.  For larger dW by the turns that writing a chunk to LDS and multiplying it take:
-// 390k rows of 768 with 1024 in bf16 580 to 610 us, 980 to 1030 TFLOP/s.  Few chunks a run leave little to overlap: 45k rows of 128 with
-// 256 in bf16 27 us, 60k of 100 with 172 in eight groups in fp32 39 (their pieces, written and read again: 18 MB beside 72 of operands).
-// Those are rows in 4 bits.  In 8: 2.5M rows of 256 with 512 gradients in bf16 763 us, 860 TFLOP/s; 380k of 1024 with 1024 803, 990; 93k of 172 with
-// 200 in eight groups in fp32 62.
+// Bound by HBM where dW is one tile: 2.56M rows of 128 with 256 gradients in bf16 280 to 300 us, 5.0 to 5.3 TB/s; fp16 480, fp32 (half the rows) 345
+// to 355, by the cutting and its two and three products.  For larger dW by the turns that writing a chunk to LDS and multiplying it take:
+// 390k rows of 768 with 1024 in bf16 590 to 600 us, 1.0 PFLOP/s.  Few chunks a run leave little to overlap: 45k rows of 128 with
+// 256 in bf16 26 us, 60k of 100 with 172 in eight groups in fp32 38 (their pieces, written and read again: 18 MB beside 72 of operands).
+// Those are rows in 4 bits.  In 8: 2.5M rows of 256 with 512 gradients in bf16 740 us, 890 TFLOP/s, in fp16 1280, half of them in fp32 950; 380k of
+// 1024 with 1024 775, 1.03 PFLOP/s; 93k of 172 with 200 in eight groups in fp32 55 to 59.
 constexpr int kGradPad = 16;         // elements behind an LDS row: the four rows that 16 lanes read at once are then 4 x 32 bytes of other banks
 
 struct GradArgs {

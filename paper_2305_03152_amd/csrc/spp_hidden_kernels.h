@@ -14,7 +14,8 @@ constexpr int kLdsPad = 32;
 
 // The form for rows of any length.  A workgroup takes 128 rows of X by 128 columns: of the product, or 64 of the gate's and the same 64 of the other
 // factor.  Steps of 128 columns of X and W go through LDS, the next asked for while one is multiplied: bound by that turn, a wait and a barrier a
-// step.  In bf16 300k rows 1100 -> 256 385 us, 440 TFLOP/s; 50k 4096 -> 256 292, gated 473.
+// step, by one workgroup a CU, whose LDS holds no second one.  In bf16 300k rows 1100 -> 256 499 us, 340 TFLOP/s; 50k 4096 -> 256 369, gated 606, its
+// gradient 620.
 constexpr int kTileRows = 128, kTileBlock = 256, kTileLd = kFp8Block + kLdsPad;
 constexpr int kTileBuffer = 2 * kTileRows * kTileLd + 2 * kTileRows;       // rows of X, rows of W, their scales
 
@@ -116,9 +117,10 @@ __global__ void __launch_bounds__(kTileBlock) hidden_tile_kernel(HiddenArgs a) {
 
 // The form for weights that LDS holds.  A wavefront keeps its 16 RN rows of X in registers, all columns of them, and goes over the columns of
 // the result 64 at a time (64 of the gate's and the same 64 of the other factor); a workgroup's wavefronts share W and wait for each other only
-// where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.  Bound by HBM for many rows: 2.5M rows
-// 256 -> 256 in bf16 390 us, 5.0 TB/s, which the same reads and writes without the products take too; the gated layer, whose activation keeps the
-// vector pipe busy half the time, 446, its gradient 925 (4.9 TB/s; without arithmetic 885).  In fp32 the product 658, the gated layer 798.
+// where the matrix changes.  X is asked for an item ahead and read once, results are written once, past the L2.  The product of many rows is bound by
+// HBM: 2.5M rows 256 -> 256 in bf16 406 us, 4.8 TB/s (the same reads and writes without the products 390).  The gated layer, 717, is by the
+// vector pipe, which decodes W for every 32 rows of X and forms the activation (67 % busy, the matrix pipe 42 %); its gradient, 1109, by both (the same reads
+// and writes alone 885).  In fp32 the product 658, the gated layer 816.
 constexpr int kHeldWaves = 8, kHeldBlock = 64 * kHeldWaves;
 // Bytes of a row of W in LDS: codes, zeros up to whole steps, scales; or values (bf16, exact), decoded on their way there.
 template <int KS, bool Values> constexpr int held_row() { return (Values ? 256 : 128) * KS + kLdsPad; }
@@ -337,10 +339,10 @@ static int launch_held_as(spp_ctx* ctx, HiddenArgs& a, bool* done) {
     SPP_HIP(hipGetLastError());
     return SPP_OK;
 }
-// Whether W is held as values: in fp32, where the code that decodes a row of W for 16 RN rows of X takes longer than its products, of the
-// gated layer, and of the product where RN is 1; not for few rows, which have W but once.  200k rows in fp32, W as codes and as values: gated 172 -> 100
-// 65 and 54 us, 128 -> 256 85 and 71, 512 -> 64 56 and 49; the product 172 -> 100 38 and 33, 300 -> 86 43 and 40, with two sixteens 100 -> 64 18
-// and 20; the gated gradient 172 -> 100 110 both.
+// Whether W is held as values: where the code that decodes a row of W for 16 RN rows of X takes longer than its products, of the
+// gated layer, and of the product where RN is 1; not for few rows, which have W but once.  W as codes and as values, in bf16: 200k rows gated 172 -> 100
+// 51 and 42 us, 128 -> 256 56 and 47, 512 -> 64 51 and 43; the product 1M rows 172 -> 100 166 and 140, 300k 256 -> 86 55 and 43; in fp32 200k rows gated
+// 172 -> 100 65 and 54, the product 172 -> 100 38 and 33, with two sixteens 100 -> 64 18 and 20; the gated gradient 172 -> 100 110 both.
 template <class T, int Mode, int KS, int RN, int Out>
 static int launch_held(spp_ctx* ctx, HiddenArgs& a, bool few, bool* done) {
     if constexpr (KS <= 4 && ((Mode == kGated && (RN == 2 || KS > 2)) || (Mode == kProduct && RN == 1 && (Out == kRagged || KS > 2)))) {
@@ -361,8 +363,9 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
         if (Mode == kGatedGrad) lines = lines && ((uintptr_t)a.t.y[j] | (uint64_t)(a.t.ld[j] * (int64_t)sizeof(T))) % 4 == 0;       // dY
         pairs += (a.t.n[j] + 32 * kHeldWaves - 1) / (32 * kHeldWaves);
     }
-    // Few rows: tiles of two sixteens and 64 columns are no more than there are CUs.  One sixteen then: 16k rows 256 -> 256 in bf16 9.1 and 7.3 us,
-    // gated 11.2 and 9.5, its gradient 15.7 and 12.7; 24k, which are more tiles, 8.2 and 8.8, 11.6 and 13.0, 17.1 and 18.4.
+    // Few rows: tiles of two sixteens and 64 columns are no more than there are CUs.  One sixteen then: 16k rows 256 -> 256 in bf16 10.7 and 8.1 us,
+    // gated 14.2 and 12.5, its gradient 17.6 and 15.5; 24k, which are more tiles, 12.4 and 10.7, 19.2
+    // and 16.0, 24.2 and 21.5, with one sixteen and with two.
     const bool few = pairs * ((a.H + 63) / 64) <= ctx->num_cu;
     auto with = [&](auto steps) {
         constexpr int KS = decltype(steps)::value;
@@ -384,19 +387,23 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
             return put(std::integral_constant<int, kLines>());
         } else if constexpr (Mode == kGatedGrad) {
             // One sixteen: with two, what the CUs have under way is more than the L2 holds, and lines that two stores share leave it in between.
-            // 1M rows with two and one in bf16 172 -> 100 290 and 249 us, 100 -> 172 456 and 422, in fp32 455 and 438, 711 and 681; 16k 172 -> 100 16 and
-            // 12, 19 and 16.  But two where these are one tile a CU and one sixteen would be a few more: 40k 17.5 and 22, 24 and 30, 64k 21 and 27, 27 and 39
+            // 1M rows with two and one in bf16 172 -> 100 304 and 299 us, 100 -> 172 456 and 410, in fp32 449 and 419, 709 and 679; 16k 172 -> 100 19 and
+            // 14, 18 and 14.  But two where these are one tile a CU and one sixteen would be a few more: 40k 21 and 26, 23 and 26, 64k 24 and 34, 26 and 34
             if constexpr (KS <= 2) {
                 if (2 * pairs > ctx->num_cu && pairs <= ctx->num_cu) return launch_held<T, Mode, KS, 2, kStraight>(ctx, a, few, done);
             }
             return launch_held<T, Mode, KS, 1, kStraight>(ctx, a, few, done);
         } else if constexpr (Mode == kGated) {
             // beside two products the LDS that rows need is worth more to W and to a second sixteen rows of X (1M rows 172 -> 100 in bf16 by way of
-            // LDS 163 us, so 115; in fp32 235 and 193)
+            // LDS 243 us, so 167; in fp32 240 and 193)
             return put(std::integral_constant<int, kStraight>());
         } else {
-            // 300k rows 256 -> 86, -> 172 in bf16 with one sixteen 40 and 44 us, with two 31 and 38; 128 -> 86 in fp32 41 and 34, in bf16 24 and 26
-            // (and two steps in fp32 fill the registers); straight from registers, 1M rows 172 -> 100 in bf16 95 us and so 87, 128 -> 250 226 and 145
+            // Results of 16 bits and few columns straight, with two sixteens: by way of LDS and so 1M rows 172 -> 100 in bf16 130 and 104 us, 300k 128 -> 86
+            // 31 and 28, 256 -> 86 43 and 41; but 256 -> 172 53 and 59, 1M 128 -> 250 172 and 236; in fp32 172 -> 100 137 and 161, 300k 128 -> 86 34 and 46.
+            // By way of LDS with one sixteen and two 300k 128 -> 86 in bf16 38 and 31, in fp32 38 and 34 (two sixteens of two steps fill the registers)
+            if constexpr (sizeof(T) == 2 && KS <= 2) {
+                if (a.H <= 128) return put(std::integral_constant<int, kStraight>());
+            }
             if constexpr (KS == 1) {
                 if (!few) SPP_TRY((launch_held<T, Mode, KS, 2, kRagged>(ctx, a, few, done)));
                 if (*done) return (int)SPP_OK;
@@ -424,8 +431,8 @@ static int try_held(spp_ctx* ctx, HiddenArgs& a, bool* done) {
 // W is read once per workgroup, and per product half as much from LDS as with X in registers and W in LDS.  The workgroups that have the same
 // rows and other columns share an XCD's L2 and take the rows in the same order at the same time.  With one wavefront per SIMD nothing else
 // works while it waits, so that a tile's work is one piece of code without branches, the next tile's way to LDS in the middle of its products.
-// Bound by the matrix pipe, its waits for LDS and a clock that it lowers: 380k rows 1024 -> 1024 in bf16 394 us, 2.0 PFLOP/s, gated to 512 415, its
-// gradient 578; in fp32, by the decoding beside it, 833, 830 and 1240.
+// Bound by the decoding of W for every tile of rows, beside which the matrix pipe is busy 41 % of the time: 380k rows 1024 -> 1024 in bf16 770 to 820 us,
+// 1.0 PFLOP/s, gated to 512 825, its gradient 924; in fp32 832, 831 and 1240.
 // Rows of X at a time, in sixteens: one where the registers would not hold what two need.  No kernel here may spill registers: the compiler (of
 // ROCm 7.2) has lost some of those that it had to put away where a kernel fills all 512.
 template <class T, int Mode, int KS> constexpr int kWideRows = Mode == kGatedGrad && KS == 8 && sizeof(T) == 4 ? 1 : 2;
@@ -553,7 +560,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
             for (int f = 0; f < 4; ++f) acc[c][f] = f32x4{0.f, 0.f, 0.f, 0.f};
         // The next tile goes to LDS and the one behind it is asked for during the products.  One wavefront per SIMD also reads each step's rows
         // before the products of the step before; the compiler, short of registers, would put every load right before its use (380k rows
-        // 1024 -> 1024 490 us, 400 so).
+        // 1024 -> 1024 854 us, 777 so).
         constexpr bool kOrdered = WAVES == 4;
         Operand xv[kOrdered ? 2 : 1][RN];
         uint32_t scales[kOrdered ? 2 : 1][RN];                // of four steps
@@ -591,7 +598,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES > 4 ? 2 : 1) hidden_wide_ker
             Rows(p, pld, now.r0, now.here, h0, 0, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][n]; });
             Rows(p, pld, now.r0, now.here, h0, a.H, a.H, 2 * a.H).put([&](int c, int n) { return acc[c][N + n]; });
         } else {
-            // whole lines past the L2 (200k rows 256 -> 1024 in bf16: 121 us with plain stores, 79 so)
+            // whole lines past the L2 (200k rows 256 -> 1024 in bf16: 152 us with plain stores, 133 so)
             const Rows to(y, ld, now.r0, now.here, h0, 0, a.H, a.H);
             if (Mode == kProduct && (((uint32_t)(uintptr_t)y | to.step) & 127) == 0) to.template put<kPastL2>([&](int c, int n) { return acc[c][n]; });
             else to.put([&](int c, int n) { return acc[c][n]; });
