@@ -77,3 +77,22 @@ def test_the_gated_layer_and_its_gradient_of_the_same(ctx, dtype, act, n, D, H):
         bound = bound + STEP[dtype] * (np.abs(want) + bound) + (2.0 ** -25 if dtype == torch.float16 else 2.0 ** -126)
         bad = ~(np.abs(got - want) <= bound)
         assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3], got[bad][:3], want[bad][:3])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,H", [(64, 40), (256, 200), (300, 600), (1024, 300), (1100, 30)])
+def test_values_beyond_fp32_are_infinite(ctx, dtype, D, H):
+    """Scale byte 254, which quantising does not give: 448 2^127 and its kin count as infinite whatever they are multiplied by, in their row only; 1.5 2^127 does not."""
+    n, at = 20, R.code_bytes(D)
+    rows, w = R.quantize(np.ones((n, D))), R.quantize(np.full((H, D), 2.0 ** -100))
+    rows[:, at] = 127
+    rows[:, :D] = 0x38                                         # ones
+    rows[3, at], rows[3, 1:min(D, 128)], rows[3, 0] = 254, 0, 0x7E     # 448 2^127
+    rows[7, at], rows[7, 1:min(D, 128)], rows[7, 0] = 254, 0, 0xFE
+    rows[9, at], rows[9, 1:min(D, 128)], rows[9, 0] = 254, 0, 0x3C     # 1.5 2^127
+    y = spp.fp8_product(ctx, torch.from_numpy(rows).to(DEV), torch.from_numpy(w).to(DEV), D, dtype=dtype).double().cpu()
+    assert bool((y[3] == float("inf")).all()) and bool((y[7] == -float("inf")).all())
+    rest = [k for k in range(n) if k not in (3, 7, 9)]
+    assert bool(torch.isfinite(y[rest]).all())
+    want = torch.tensor(1.5 * 2.0 ** 27 + max(0, D - 128) * 2.0 ** -100, dtype=torch.float64).to(dtype).double()
+    assert bool((y[9] == want).all())
