@@ -4,12 +4,11 @@
 //   gated        Y_j = act(X_j Wg[g_j]^T) * (X_j Wu[g_j]^T)         W[g] = Wg, then Wu, H rows each
 //   its gradient [dY_j * u * act'(g) | dY_j * act(g)]               g and u formed again from X_j and W[g_j], as in the forward pass
 //
-// Codes are E4M3 and scales powers of two: a code under a scale is exact in bf16, so the
-// values are decoded in registers and multiplied by the bf16 instruction: products are exact, sums fp32, whatever the type of the result.  The
-// instruction for 8-bit floats would take the codes and the scales themselves, at twice the rate, but it adds the products of eight
-// neighbouring columns after cutting each off at 2^-13 of the power of two of the largest (measured: beside 2^16 an addend of 2^3 counts and one of
-// 2^2 does not): where large terms cancel each other, the small ones, which are then the result, are lost.  The activation is computed in
-// fp32, and what is written is rounded once.
+// Codes are E4M3 and scales powers of two: a code under a scale is exact in bf16, so the values are decoded in registers and multiplied by
+// the bf16 instruction: products are exact, sums fp32, whatever the type of the result.  The instruction for 8-bit floats would take the
+// codes and the scales themselves, at twice the rate, but it adds the products of eight neighbouring columns after cutting each off at
+// 2^-13 of the power of two of the largest (measured: beside 2^16 an addend of 2^3 counts and one of 2^2 does not): where large terms cancel
+// each other, the small ones, which are then the result, are lost.  The activation is computed in fp32, and what is written is rounded once.
 #pragma once
 
 #include "spp_fp8.h"
@@ -202,7 +201,8 @@ __device__ __forceinline__ void combine(int act, f32x4 (&one)[N], f32x4 (&two)[N
     }
 }
 
-// A tile of a matrix of results by way of a buffer (rows_buffer) that begins with its first row: 16 RN rows, of which `here` are there, and of each N columns from h0 + N m on.
+// A tile of a matrix of results by way of a buffer (rows_buffer) that begins with its first row: 16 RN rows, of which `here` are there, and of
+// each N columns from h0 + N m on.
 // Whole vectors where all begin at multiples of four bytes, which is all that the instructions ask for; the last columns of a row where they
 // are no whole vector, and 16-bit matrices at odd places, go element by element (1M rows 172 -> 86, every column by element: gated layer in
 // fp32 212 us, its gradient 477; so 174 and 360).  All of it is branches that a whole wavefront takes: where a kernel's values fill the
